@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libklotski_moe.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["moe_api.hip", "k_router.hip", "k_plan.hip", "k_misc.hip", "k_ffn_f32.hip",
-           "k_ffn_bf16.hip", "attn_api.hip", "k_attn.hip"]
+           "k_ffn_bf16.hip", "attn_api.hip", "k_attn.hip", "kv8_api.hip", "k_kv8.hip", "k_kv8_attn.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
@@ -26,7 +26,8 @@ def build(force: bool = True, verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     headers = [os.path.join(CSRC, "kernels.h"), os.path.join(CSRC, "attn_kernels.h"),
                os.path.join(CSRC, "attn_ranges.h"), os.path.join(CSRC, "tile_rules.h"),
-               os.path.join(HERE, "..", "include", "moe.h"), os.path.join(HERE, "..", "include", "moe_attn.h")]
+               os.path.join(CSRC, "kv8_kernels.h"),
+               *(os.path.join(HERE, "..", "include", h) for h in ("moe.h", "moe_attn.h", "moe_kv8.h"))]
     jobs = []
     for name in SOURCES:
         src = os.path.join(CSRC, name)

@@ -1,0 +1,139 @@
+"""The 8-bit key-value cache without a GPU: exported symbols, struct sizes, sizing, refusals that the host decides."""
+import ctypes as C
+import os
+import re
+
+import pytest
+import torch
+
+from oracle import kv8_ref as R
+from paper_2502_06888_amd import binding as B
+from paper_2502_06888_amd import kv8_binding as Q
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def cache(n_seq=2, kv=2, hd=64, max_len=128, block=32):
+    return Q.Kv8Cache.empty(n_seq, kv, hd, max_len, block, device="cpu")
+
+
+def ints(*v):
+    return torch.tensor(v, dtype=torch.int32)
+
+
+def test_library_exports_every_symbol_of_the_cache():
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "moe_kv8.h")).read(), flags=re.S)
+    names = sorted(set(re.findall(r"\b(moe_kv8_[a-z0-9_]+)\s*\(", text)))
+    lib = Q.load_library()
+    assert names == sorted(Q.KV8_EXPORTS)
+    for n in names:
+        assert hasattr(lib, n)
+    assert C.sizeof(Q.MoeKv8Cache) == 6 * 4 + 5 * 8
+    assert C.sizeof(Q.MoeKv8Step) == 4 * 4 + 3 * 8
+
+
+@pytest.mark.parametrize("field,value,status", [
+    ("n_seq", 0, B.MOE_ERR_SHAPE), ("n_seq", 65537, B.MOE_ERR_SHAPE), ("n_kv_heads", 0, B.MOE_ERR_SHAPE),
+    ("n_kv_heads", 1025, B.MOE_ERR_SHAPE), ("head_dim", 96, B.MOE_ERR_SHAPE), ("block", 8, B.MOE_ERR_SHAPE),
+    ("block", 48, B.MOE_ERR_SHAPE), ("max_len", 0, B.MOE_ERR_SHAPE), ("max_len", 100, B.MOE_ERR_SHAPE),
+    ("max_len", (1 << 20) + 32, B.MOE_ERR_SHAPE), ("reserved", 1, B.MOE_ERR_INVALID_ARG),
+])
+def test_sizes_of_the_cache_are_checked(field, value, status):
+    c = cache()
+    s = Q.Kv8Step(ints(3, 4), 2, 1, 4)
+    setattr(c.c, field, value)
+    for call in (lambda: Q.attend_workspace_bytes(c, s, 4, True), lambda: Q.evict_workspace(c, 32)):
+        with pytest.raises(B.MoeError) as e:
+            call()
+        assert e.value.status == status and e.value.message
+
+
+@pytest.mark.parametrize("rows,new,cached,offsets,status", [
+    (-1, 1, 4, True, B.MOE_ERR_SHAPE), ((1 << 20) + 1, 1, 4, True, B.MOE_ERR_SHAPE),
+    (2, -1, 4, True, B.MOE_ERR_INVALID_ARG), (2, 1, -1, True, B.MOE_ERR_INVALID_ARG),
+    (2, 1, 129, True, B.MOE_ERR_INVALID_ARG), (2, 129, 4, True, B.MOE_ERR_INVALID_ARG),     # over the slots
+    (3, 1, 4, False, B.MOE_ERR_INVALID_ARG),        # not n_seq * max_new
+    (2, 0, 4, True, B.MOE_ERR_INVALID_ARG), (0, 1, 4, True, B.MOE_ERR_INVALID_ARG),
+])
+def test_bounds_of_a_step_are_checked(rows, new, cached, offsets, status):
+    s = Q.Kv8Step(ints(3, 4), rows, new, cached, row_offsets=ints(0, 1, 2) if offsets else None)
+    with pytest.raises(B.MoeError) as e:
+        Q.attend_workspace_bytes(cache(), s, 4, True)
+    assert e.value.status == status and e.value.message
+
+
+@pytest.mark.parametrize("heads", [0, 3, 18, -2])
+def test_head_counts_are_checked(heads):
+    with pytest.raises(B.MoeError) as e:
+        Q.attend_workspace_bytes(cache(), Q.Kv8Step(ints(3, 4), 2, 1, 4), heads, False)
+    assert e.value.status == B.MOE_ERR_SHAPE
+
+
+@pytest.mark.parametrize("keep", [0, -32, 33, 160])
+def test_keep_is_a_number_of_whole_blocks(keep):
+    with pytest.raises(B.MoeError) as e:
+        Q.evict_workspace(cache(), keep)
+    assert e.value.status == B.MOE_ERR_INVALID_ARG
+
+
+def test_null_arguments_and_host_tensors_are_refused():
+    lib, c, s = Q.load_library(), cache(), Q.Kv8Step(ints(3, 4), 2, 1, 4)
+    n = C.c_int64(0)
+    assert lib.moe_kv8_attend_workspace_bytes(None, s.ref, 4, 0, C.byref(n)) == B.MOE_ERR_INVALID_ARG
+    assert lib.moe_kv8_attend_workspace_bytes(c.ref, None, 4, 0, C.byref(n)) == B.MOE_ERR_INVALID_ARG
+    assert lib.moe_kv8_attend_workspace_bytes(c.ref, s.ref, 4, 0, None) == B.MOE_ERR_INVALID_ARG
+    assert lib.moe_kv8_append(None, None, s.ref, None, None, 0, 0) == B.MOE_ERR_INVALID_ARG
+    x = torch.zeros((2, 2, 64), dtype=torch.bfloat16)
+    assert lib.moe_kv8_append(None, c.ref, s.ref, x.data_ptr(), x.data_ptr(), 128, 64) == B.MOE_ERR_INVALID_ARG
+    assert b"not device memory" in lib.moe_kv8_last_error()
+    c.c.k = 0
+    assert lib.moe_kv8_append(None, c.ref, s.ref, x.data_ptr(), x.data_ptr(), 128, 64) == B.MOE_ERR_INVALID_ARG
+    assert b"cache.k is null" in lib.moe_kv8_last_error()
+    c.c.position = None
+    assert lib.moe_kv8_evict(None, c.ref, None, 4, 32, 0, None, None, None, None, None, None, 0) == B.MOE_ERR_INVALID_ARG
+    assert b"position" in lib.moe_kv8_last_error()
+    assert lib.moe_kv8_evict(None, cache().ref, None, 4, 32, 33, None, None, None, None, None, None, 0) == B.MOE_ERR_INVALID_ARG
+    assert lib.moe_kv8_evict(None, cache().ref, None, 129, 32, 0, None, None, None, None, None, None, 0) == B.MOE_ERR_INVALID_ARG
+    for scale in (-1.0, float("nan"), float("inf")):
+        assert lib.moe_kv8_attend(None, cache().ref, s.ref, 4, None, 0, 0, scale, None, 0, 0, None, None, None, 0) == B.MOE_ERR_INVALID_ARG
+        assert b"softmax_scale" in lib.moe_kv8_last_error()
+
+
+def test_shapes_and_types_of_tensors_are_checked_by_the_binding():
+    c, s = cache(), Q.Kv8Step(ints(3, 4), 2, 1, 4)
+    good = torch.zeros((2, 2, 64), dtype=torch.bfloat16)
+    for bad in (good[:1], good.float(), good[:, :1], good[:, :, :32], good.transpose(1, 2).contiguous().transpose(1, 2)):
+        with pytest.raises(B.MoeError):
+            Q.append(c, s, bad, good, stream=object())
+        with pytest.raises(B.MoeError):
+            Q.attend(c, s, bad, good, stream=object())
+    with pytest.raises(B.MoeError):
+        Q.append(c, Q.Kv8Step(ints(3, 4, 5), 3, 1, 5), good, good, stream=object())
+    with pytest.raises(B.MoeError):
+        Q.Kv8Step(torch.zeros(2, dtype=torch.int64), 2, 1, 4)
+    with pytest.raises(B.MoeError):
+        Q.Kv8Cache(c.k, c.v[:1], c.k_scale, c.v_scale, 32)
+    with pytest.raises(B.MoeError):
+        Q.Kv8Cache(c.k, c.v, c.k_scale, c.v_scale, 16)
+
+
+def test_reference_codes_are_the_nearest_ones():
+    assert torch.equal(R.encode(R.TABLE[:127]), torch.arange(127, dtype=torch.uint8))
+    mid = (R.POSITIVE[1:] + R.POSITIVE[:-1]) / 2                     # exact ties go to the even code
+    assert bool((R.encode(mid) % 2 == 0).all())
+    assert R.encode(torch.tensor([1e9, -1e9, float("inf"), float("nan"), -0.0], dtype=torch.float64)).tolist() == [126, 254, 126, 127, 128]
+    x = torch.randn(4096, dtype=torch.float64) * 30
+    assert torch.equal(R.encode(x), x.float().to(torch.float8_e4m3fn).view(torch.uint8))
+    assert [R.least_scale(v) for v in (0.0, 448.0, 449.0, 1.0, 3e38)] == [2.0 ** -100, 1.0, 2.0, 2.0 ** -8, 2.0 ** 119]
+
+
+def test_reference_attention_of_one_visible_slot_is_its_value():
+    """A handworked case: the first token of an empty cache sees itself alone, the second the mean of equal scores."""
+    k = torch.zeros((1, 1, 16, 32), dtype=torch.uint8)
+    v = torch.full((1, 1, 16, 32), 0x38, dtype=torch.uint8)          # 1.0
+    v[0, 0, 1] = 0x40                                                # 2.0
+    s = torch.full((1, 1, 1), 0.5, dtype=torch.float64)
+    out, weight, _, _ = R.attend(k, s, v, s, torch.ones((2, 1, 32)), [0], [0, 2], 16)
+    assert torch.equal(out[0], torch.full((1, 32), 0.5, dtype=torch.float64))
+    assert torch.equal(out[1], torch.full((1, 32), 0.75, dtype=torch.float64))
+    assert weight[0, 0, :2].tolist() == [1.5, 0.5]
