@@ -192,6 +192,8 @@ moe_status moe_kv8_attend(void* stream, const moe_kv8_cache* cache, const moe_kv
         TRY(check_rows(q, "q", q_row_stride, q_head_stride, &w));
         TRY(check_rows(out, "out", out_row_stride, out_head_stride, &w));
     }
+    if (q && q == out && (weight_out || q_row_stride != out_row_stride || q_head_stride != out_head_stride))
+        return fail(MOE_ERR_INVALID_ARG, "out may be q only without weight_out and with the same strides");
     if (weight_in && !weight_out) return fail(MOE_ERR_INVALID_ARG, "weight_in without weight_out");
     if (weight_out) TRY(w.on(weight_out, "weight_out", 4));
     if (weight_in && weight_in != weight_out) TRY(w.on(weight_in, "weight_in", 4));

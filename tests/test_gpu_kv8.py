@@ -249,7 +249,7 @@ def test_attention_of_infinite_and_nan_values_stays_with_those_who_see_them():
     cache, codes, scale = filled(g, 1, kv, 64, hd, block, [40])
     cache.v[0, 0, 39, 7] = 0x7f
     codes[1][0, 0, 39, 7] = 0x7f
-    for cached, new in ([0, 40], [38, 2], [39, 1]):
+    for cached, new in ([0, 40], [38, 2], [36, 4], [32, 8], [39, 1]):
         q = rand(g, (new, heads, hd))
         out = torch.zeros((new, heads, hd), dtype=torch.bfloat16, device=DEV)
         Q.attend(cache, Q.Kv8Step(ints([cached]), new, new, cached), q.to(DEV), out)
@@ -558,8 +558,9 @@ def test_refusals_that_need_device_memory():
     shifted = torch.zeros(2 * 4 * 64 + 8, dtype=torch.bfloat16, device=DEV)[1:1 + 512].view(2, 4, 64)
     refused(lambda: Q.attend(c, s, shifted, q), B.MOE_ERR_INVALID_ARG, "aligned")
     refused(lambda: Q.attend(c, s, q, q.cpu()), B.MOE_ERR_INVALID_ARG, "device memory")
-    refused(lambda: Q.attend(c, s, q, q, w, None), B.MOE_ERR_INVALID_ARG, "weight_in")
-    refused(lambda: Q.attend(c, s, q, q, w, w, torch.empty(16, dtype=torch.uint8, device=DEV)), B.MOE_ERR_OOM, "workspace")
+    refused(lambda: Q.attend(c, s, q, q, None, w), B.MOE_ERR_INVALID_ARG, "out may be q")
+    refused(lambda: Q.attend(c, s, q, torch.zeros((2, 5, 64), dtype=torch.bfloat16, device=DEV)[:, :4], w, None), B.MOE_ERR_INVALID_ARG, "weight_in")
+    refused(lambda: Q.attend(c, s, q, q.clone(), w, w, torch.empty(16, dtype=torch.uint8, device=DEV)), B.MOE_ERR_OOM, "workspace")
     refused(lambda: Q.evict(c, ints([3, 4]), 4, 32, 0, None, w, workspace=torch.empty(16, dtype=torch.uint8, device=DEV)), B.MOE_ERR_OOM, "workspace")
     assert lib.moe_kv8_append(None, c.ref, s.ref, k.data_ptr(), k.data_ptr(), -256, 64) == B.MOE_ERR_INVALID_ARG
     Q.append(c, s, k, k)                                                     # a refused call leaves everything usable
