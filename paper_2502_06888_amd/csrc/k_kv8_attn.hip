@@ -16,16 +16,6 @@ constexpr float kEmpty = -1.0e30f;  // finite stand-in for "no slot seen yet"
 // the sums of 2^20 slots of any finite values stay finite.
 constexpr float kAbove = 28.f, kNear = 20.f;
 
-__device__ __forceinline__ int seq_of_row(const Step& s, int n_seq, int row) {
-    if (s.row_offsets == nullptr) return row / s.max_new;
-    int lo = 0, hi = n_seq - 1;  // last sequence whose rows begin at or before `row`
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (s.row_offsets[mid] <= row) lo = mid; else hi = mid - 1;
-    }
-    return lo;
-}
-
 __device__ __forceinline__ bf16x8 as_bf16x8(const u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
 __device__ __forceinline__ f32x4 mfma16(const u32x4 a, const u32x4 b, const f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
@@ -55,8 +45,10 @@ __device__ __forceinline__ void transpose4(const uint32_t (&a)[4], uint32_t (&o)
 //             weights never leave their lane: V is read by slots in that order, byte-transposed in registers.
 // A tile of 16 matrix rows serves 8 rows twice: the second half multiplies what rounding the weights to bf16 left over,
 // so the weights count with 16 bits at no matrix cost.
+constexpr int kRows = 128, kSlots = 64;  // rows and slots of a tile where there are many new tokens
+
 struct Split {
-    int per, ranges;    // slots of a range (a multiple of 128), ranges of a sequence at most
+    int per, ranges;    // slots of a range (a multiple of 128, with many new tokens of 64), ranges of a sequence at most
     int tile_rows;      // rows the buffers below hold per pair
     int score_stride;   // slots a row of `scores` holds, a multiple of 32
     float* acc;         // [pair, range, row, hd] unnormalised sums; with float2 `ml` (reference, sum of weights)
@@ -66,7 +58,7 @@ struct Split {
 };
 
 template <int HD, int NT, bool SCORES>
-__global__ __launch_bounds__(256, NT == 1 ? 4 : 3) void decode_kernel(Cache c, Step s, Attend a, Split sp) {
+__global__ __launch_bounds__(256, NT == 1 ? 4 : HD < 128 ? 3 : 2) void decode_kernel(Cache c, Step s, Attend a, Split sp) {
     constexpr int KW = HD / 16;             // words of a K row that a lane holds: HD/4 bytes
     constexpr int VT = HD / 16;             // tiles of 16 elements of the sums
     constexpr int VW = VT >= 4 ? VT / 4 : 1;  // words of a V row that a lane holds: VT bytes
@@ -167,25 +159,21 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 3) void decode_kernel(Cache c, S
         }
         if (p0 + 128 < end) load_k(p0 + 128);
         const bool whole = p0 + 32 <= q.cached + 1 && p0 + 32 <= end;  // every row sees all 32 slots
-        if (!whole) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)  // weight 0 alone would make NaN of a NaN code
-                if (p0 + (j >> 2) * 16 + grp * 4 + (j & 3) >= end)
-#pragma unroll
-                    for (int w = 0; w < VW; ++w) vr[j][w] = 0u;
-        }
-        // A NaN code of V must not reach rows that do not see its slot: weight 0 times NaN is NaN.  Where a chunk that
-        // some rows see in part holds one, the products are formed without it and put back for those who see it.
         bool odd = false;
-        if (!whole) {
+        if (!whole) {  // weight 0 times a NaN code would be NaN: such codes are taken out, and put back where they are seen
             uint32_t nan = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int w = 0; w < VW; ++w) nan |= nan_bytes(vr[j][w]);
+                for (int w = 0; w < VW; ++w) {
+                    if (p0 + (j >> 2) * 16 + grp * 4 + (j & 3) >= end) vr[j][w] = 0u;
+                    const uint32_t n = nan_bytes(vr[j][w]);
+                    vr[j][w] &= ~((n >> 7) * 0xffu);
+                    nan |= n;
+                }
             odd = __any(nan != 0);
         }
-        u32x4 pf[NT], seen[NT];
+        u32x4 pf[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             if (SCORES && col < 8 && n * 8 + col < rows) {
@@ -202,10 +190,6 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 3) void decode_kernel(Cache c, S
                     const int slot = p0 + (j >> 2) * 16 + grp * 4 + (j & 3);
                     if (slot >= limit[n] || slot >= end) x[j] = -__builtin_inff();
                 }
-                if (odd)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        seen[n][j] = (x[2 * j] == -__builtin_inff() ? 0u : 0x3f80u) | (x[2 * j + 1] == -__builtin_inff() ? 0u : 0x3f800000u);
             }
             float top = x[0];
 #pragma unroll
@@ -244,23 +228,6 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 3) void decode_kernel(Cache c, S
             for (int j = 0; j < 8; ++j) in[j >> 2][j & 3] = vr[j][w];
             transpose4(in[0], tr[0]);
             transpose4(in[1], tr[1]);
-            if (odd) {
-#pragma unroll
-                for (int b = 0; b < (VT < 4 ? VT : 4); ++b) {
-                    const uint32_t na = nan_bytes(tr[0][b]), nb = nan_bytes(tr[1][b]);
-                    // 0x38 is 1.0: bytes of ones where the code is NaN
-                    const u32x4 where = widen8((na >> 7) * 0x38u, (nb >> 7) * 0x38u, 1.f);
-                    tr[0][b] &= ~((na >> 7) * 0xffu);
-                    tr[1][b] &= ~((nb >> 7) * 0xffu);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const f32x4 hit = mfma16(seen[n], where, f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (hit[r] > 0.f) acc[n][w * 4 + b][r] = __builtin_nanf("");
-                    }
-                }
-            }
 #pragma unroll
             for (int b = 0; b < (VT < 4 ? VT : 4); ++b) {
                 const u32x4 vf = {widen2<false>(tr[0][b], vsc[0]), widen2<true>(tr[0][b], vsc[0]),
@@ -270,6 +237,18 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 3) void decode_kernel(Cache c, S
             }
         }
         if (p0 + 128 < end) load_v(p0 + 128);
+        if (odd) {
+            for (int j = p0; j < min(p0 + 32, end); ++j)
+#pragma unroll
+                for (int v = 0; v < VT; ++v) {
+                    if ((V[(int64_t)j * HD + col * VT + v] & 0x7f) != 0x7f) continue;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (j <= q.cached + (n * 8 + ((grp * 4 + r) & 7)) / G) acc[n][v][r] = __builtin_nanf("");
+                }
+        }
     }
     // the lane groups of a column, the two halves of the weights, then the wavefronts
 #pragma unroll
@@ -319,7 +298,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 3) void decode_kernel(Cache c, S
 
 // Adds up the ranges of one (pair, row): one wavefront, HD/4 lanes per range.
 template <int HD>
-__global__ __launch_bounds__(256) void merge_kernel(Cache c, Step s, Attend a, Split sp) {
+__global__ __launch_bounds__(256) void merge_kernel(Cache c, Step s, Attend a, Split sp, bool few) {
     constexpr int LPR = HD / 4, SIDE = 64 / LPR;
     const int lane = threadIdx.x & 63, sub = lane % LPR;
     const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -327,8 +306,11 @@ __global__ __launch_bounds__(256) void merge_kernel(Cache c, Step s, Attend a, S
     if (pair >= c.n_seq * c.Hkv) return;
     const int seq = pair / c.Hkv, hk = pair % c.Hkv, G = a.Hq / c.Hkv;
     const Seq q = sequence(c, s, seq);
-    const int many = (q.cached + q.n_new + sp.per - 1) / sp.per;
-    if (r >= q.n_new * G || many <= 1) return;
+    if (r >= q.n_new * G) return;
+    // few tokens: the ranges of the sequence; else those of the slots that the row's tile sees
+    const int sees = few ? q.cached + q.n_new : q.cached + min(r / kRows * kRows + kRows - 1, q.n_new * G - 1) / G + 1;
+    const int many = (sees + sp.per - 1) / sp.per;
+    if (many <= 1) return;
     const int64_t at = (int64_t)pair * sp.ranges * sp.tile_rows + r;
     float m = kEmpty, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -376,98 +358,357 @@ __global__ __launch_bounds__(256) void weights_kernel(Cache c, Step s, Attend a,
     a.weight_out[pair * c.max_len + j] = w;
 }
 
-// ---- many new tokens (first form: one score per thread) -----------------------------------------------------
+// ---- many new tokens: bound by the matrix cores ---------------------------------------------------------------
+//
+// One workgroup of four wavefronts per (sequence, key-value head, 128 rows, range of slots); a row is a (token, query
+// head of the group), so the heads that share K and V share a tile of them.  64 slots at a time are dequantised once
+// per workgroup into LDS as bf16, V transposed on the way by bytes, while the codes of the next 64 are on their way.
+// A wavefront has 32 rows: S^T[slot][row] = K Q^T and O^T[element][row] = V^T P^T, 32x32x16.  Lane l holds row l%32
+// throughout, so softmax statistics and rescaling stay in the lane, and the weights of a lane are its operand of the
+// second product as they are: slots 4*(l/32)..+3 and 8 + 4*(l/32)..+3 of each 16, the order in which V^T is laid out.
+template <int HD>
+struct TileLds {
+    static constexpr int KS = HD + 8, VS = kSlots + 8;  // 16 bytes of padding: reads of 16 bytes free of bank conflicts
+    uint16_t k[2][kSlots * KS];
+    uint16_t v[2][HD * VS];
+    int nan[2];
+};
 
-// Score of one slot (base 2): q (bf16) . K.
-__device__ __forceinline__ float score(const uint16_t* q, const uint8_t* k, float kscale, int hd, float qscale) {
-    float dot = 0.f;
-    for (int d = 0; d < hd; d += 4) {
-        const uint32_t w = *(const uint32_t*)(k + d);
-        const u32x2 x = *(const u32x2*)(q + d);
-        const uint32_t a = widen2<false>(w, kscale), b = widen2<true>(w, kscale);
-        dot = __builtin_fmaf(bf_lo(x.x), bf_lo(a), dot);
-        dot = __builtin_fmaf(bf_hi(x.x), bf_hi(a), dot);
-        dot = __builtin_fmaf(bf_lo(x.y), bf_lo(b), dot);
-        dot = __builtin_fmaf(bf_hi(x.y), bf_hi(b), dot);
+// Codes of a tile on their way into LDS.  Items of 32 bytes: HD*2 of K (a slot's 32 elements), then HD*2 of V (four
+// elements of eight slots in the order of a lane's weights), shared out over the threads.
+template <int HD>
+struct TileLoad {
+    static constexpr int kItems = HD * 2, kBoth = kItems == 256;
+    uint32_t kr[8], vr[8];
+    float ksc, vsc[1];
+
+    __device__ __forceinline__ static int k_item() { return threadIdx.x; }
+    __device__ __forceinline__ static int v_item() { return kBoth ? (int)threadIdx.x : (int)threadIdx.x - kItems; }
+    __device__ __forceinline__ static bool has_k() { return kBoth || (int)threadIdx.x < kItems; }
+    __device__ __forceinline__ static bool has_v() { return kBoth || ((int)threadIdx.x >= kItems && (int)threadIdx.x < 2 * kItems); }
+    __device__ __forceinline__ static int v_slot(int group, int j) { return (group >> 1) * 16 + (group & 1) * 4 + (j & 3) + (j >> 2) * 8; }
+
+    // slots past `total` re-read the last one
+    __device__ __forceinline__ void load(const Cache& c, const uint8_t* K, const uint8_t* V, const float* ks, const float* vs, int j0, int total) {
+        if (has_k()) {
+            const int i = k_item(), slot = min(j0 + i / (HD / 32), total - 1);
+            const u32x4* p = (const u32x4*)(K + (int64_t)slot * HD + i % (HD / 32) * 32);
+            const u32x4 a = p[0], b = p[1];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                kr[w] = a[w];
+                kr[4 + w] = b[w];
+            }
+            ksc = ks[slot >> c.logb];
+        }
+        if (has_v()) {
+            const int i = v_item(), quad = i % (HD / 4), group = i / (HD / 4);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                vr[j] = *(const uint32_t*)(V + (int64_t)min(j0 + v_slot(group, j), total - 1) * HD + quad * 4);
+            vsc[0] = vs[min(j0 + (group >> 1) * 16, total - 1) >> c.logb];
+        }
     }
-    return dot * qscale;
+    // part: some row does not see all 64 slots.  Codes past `total` and NaN codes of V then count as 0 (weight 0 times NaN
+    // would reach rows that do not see the slot); that there were NaN is noted.
+    __device__ __forceinline__ void store(TileLds<HD>& t, int buf, int j0, int total, bool part) {
+        if (has_k()) {
+            const int i = k_item();
+            u32x4* to = (u32x4*)(t.k[buf] + i / (HD / 32) * TileLds<HD>::KS + i % (HD / 32) * 32);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) to[w] = widen8(kr[2 * w], kr[2 * w + 1], ksc);
+        }
+        if (has_v()) {
+            const int i = v_item(), quad = i % (HD / 4), group = i / (HD / 4);
+            if (part) {
+                uint32_t nan = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (j0 + v_slot(group, j) >= total) vr[j] = 0u;
+                    const uint32_t n = nan_bytes(vr[j]);
+                    vr[j] &= ~((n >> 7) * 0xffu);
+                    nan |= n;
+                }
+                if (nan != 0) t.nan[buf] = j0 + 1;
+            }
+            uint32_t in[2][4], tr[2][4];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) in[j >> 2][j & 3] = vr[j];
+            transpose4(in[0], tr[0]);
+            transpose4(in[1], tr[1]);
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                *(u32x4*)(t.v[buf] + (quad * 4 + b) * TileLds<HD>::VS + group * 8) = widen8(tr[0][b], tr[1][b], vsc[0]);
+        }
+    }
+};
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ f32x16 mfma32(const u32x4 a, const u32x4 b, const f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
 }
+// Row of a 32x32 result that register r of a lane in half g holds.
+__device__ __forceinline__ int row_of(int r, int g) { return 8 * (r >> 2) + 4 * g + (r & 3); }
 
-// One workgroup per (row, query head): 256 slots at a time, one score per thread, then all threads add their part of
-// the slots to the elements they own.
-__global__ __launch_bounds__(256) void attend_plain_kernel(Cache c, Step s, Attend a, float* lse) {
-    __shared__ float p[256], red[256];
-    __shared__ float vs[256];
-    const int row = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, hk = h / (a.Hq / c.Hkv), tid = threadIdx.x;
-    const int seq = seq_of_row(s, c.n_seq, row);
+template <int HD>
+__global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend a, Split sp, int tiles) {
+    __shared__ TileLds<HD> lds;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, grp = lane >> 5;
+    // last tiles first: they see the most slots; the pairs side by side, so that the tiles of one keep to an XCD
+    const int pairs = c.n_seq * c.Hkv;
+    const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
+    const int range = rest % sp.ranges, tile = tiles - 1 - rest / sp.ranges;
+    const int seq = pair / c.Hkv, hk = pair % c.Hkv, G = a.Hq / c.Hkv;
     const Seq q = sequence(c, s, seq);
-    if (row < q.row0 || row >= q.row0 + q.n_new) return;
-    const int sees = q.cached + row - q.row0 + 1;
-    const int64_t base = (int64_t)seq * c.Hkv + hk, nb = c.max_len >> c.logb;
-    const uint8_t *K = c.codes[0] + base * c.max_len * c.hd, *V = c.codes[1] + base * c.max_len * c.hd;
-    const float *ks = c.scale[0] + base * nb, *vscale = c.scale[1] + base * nb;
-    const uint16_t* qr = a.q.p + (int64_t)row * a.q.row + (int64_t)h * a.q.head;
-    const int parts = 256 / c.hd, d = tid % c.hd, part = tid / c.hd;
-    float m = kEmpty, l = 0.f, acc = 0.f;
-    for (int j0 = 0; j0 < sees; j0 += 256) {
-        const int j = j0 + tid;
-        const float z = j < sees ? score(qr, K + (int64_t)j * c.hd, ks[j >> c.logb], c.hd, a.qscale) : kEmpty;
-        red[tid] = z;
-        vs[tid] = j < sees ? vscale[j >> c.logb] : 0.f;
-        __syncthreads();
-        for (int w = 128; w > 0; w >>= 1) {
-            if (tid < w) red[tid] = fmaxf(red[tid], red[tid + w]);
-            __syncthreads();
-        }
-        const float mn = fmaxf(m, red[0]), f = exp2f(m - mn);
-        __syncthreads();
-        m = mn;
-        red[tid] = p[tid] = j < sees ? exp2f(z - mn) : 0.f;
-        __syncthreads();
-        for (int w = 128; w > 0; w >>= 1) {
-            if (tid < w) red[tid] += red[tid + w];
-            __syncthreads();
-        }
-        l = l * f + red[0];
-        acc *= f;
-        const int most = min(256, sees - j0);
-        for (int i = part; i < most; i += parts)
-            acc = __builtin_fmaf(p[i], bf_lo(widen2<false>(V[(int64_t)(j0 + i) * c.hd + d], vs[i])), acc);
-        __syncthreads();
-    }
-    red[tid] = acc;
+    const int rows = q.n_new * G, row0 = tile * kRows;
+    if (row0 >= rows) return;
+    const int total = q.cached + q.n_new;
+    const int least = q.cached + row0 / G + 1;                                 // slots that the first row sees
+    const int sees = q.cached + min(row0 + kRows - 1, rows - 1) / G + 1;       // and the last one
+    const int first = range * sp.per, end = min(first + sp.per, sees);
+    if (first >= end) return;
+    const int64_t base = (int64_t)seq * c.Hkv + hk;
+    const uint8_t *K = c.codes[0] + base * c.max_len * HD, *V = c.codes[1] + base * c.max_len * HD;
+    const float *ks = c.scale[0] + base * (c.max_len >> c.logb), *vs = c.scale[1] + base * (c.max_len >> c.logb);
+
+    const int r = row0 + wave * 32 + col;
+    const int token = min(r, rows - 1) / G, head = hk * G + min(r, rows - 1) % G;
+    const int limit = q.cached + token + 1;
+    const int wave_least = q.cached + min(row0 + wave * 32, rows - 1) / G + 1;
+    const int wave_most = q.cached + min(row0 + wave * 32 + 31, rows - 1) / G + 1;
+    const bool active = row0 + wave * 32 < rows;
+    u32x4 qf[HD / 16];
+    const uint16_t* qp = a.q.p + (int64_t)(q.row0 + token) * a.q.row + (int64_t)head * a.q.head + grp * 8;
+#pragma unroll
+    for (int f = 0; f < HD / 16; ++f) qf[f] = *(const u32x4*)(qp + f * 16);
+    f32x16 acc[HD / 32];
+#pragma unroll
+    for (int m = 0; m < HD / 32; ++m)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[m][i] = 0.f;
+    float ref = kEmpty, sum = 0.f;
+    if (threadIdx.x < 2) lds.nan[threadIdx.x] = 0;
     __syncthreads();
-    if (tid < c.hd) {
-        for (int i = 1; i < parts; ++i) acc += red[i * c.hd + tid];
-        const __bf16 o = (__bf16)(acc / l);
-        a.out.p[(int64_t)row * a.out.row + (int64_t)h * a.out.head + tid] = __builtin_bit_cast(uint16_t, o);
+    TileLoad<HD> next;
+    next.load(c, K, V, ks, vs, first, total);
+    next.store(lds, 0, first, total, first + kSlots > least);
+    if (first + kSlots < end) next.load(c, K, V, ks, vs, first + kSlots, total);
+    __syncthreads();
+    int buf = 0;
+    for (int j0 = first; j0 < end; j0 += kSlots, buf ^= 1) {
+        if (j0 + kSlots < end) {
+            next.store(lds, buf ^ 1, j0 + kSlots, total, j0 + 2 * kSlots > least);
+            if (j0 + 2 * kSlots < end) next.load(c, K, V, ks, vs, j0 + 2 * kSlots, total);
+        }
+        if (active && j0 < wave_most) {
+            f32x16 z[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[t][i] = 0.f;
+                const uint16_t* kp = lds.k[buf] + (t * 32 + col) * TileLds<HD>::KS + grp * 8;
+#pragma unroll
+                for (int f = 0; f < HD / 16; ++f) z[t] = mfma32(*(const u32x4*)(kp + f * 16), qf[f], z[t]);
+            }
+            const bool whole = j0 + kSlots <= wave_least && j0 + kSlots <= end;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[t][i] *= a.qscale;
+            if (!whole) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int slot = j0 + t * 32 + row_of(i, grp);
+                        if (slot >= limit || slot >= end) z[t][i] = -__builtin_inff();
+                    }
+            }
+            float top = z[0][0];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, z[t][i]);
+            if (__any(top > ref - kNear)) {
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                const float now = top > ref - kNear ? fmaxf(ref, top + kAbove) : ref;
+                const float f = __builtin_amdgcn_exp2f(ref - now);
+                ref = now;
+                sum *= f;
+#pragma unroll
+                for (int m = 0; m < HD / 32; ++m)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[m][i] *= f;
+            }
+            u32x4 pf[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                float p[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    p[i] = __builtin_amdgcn_exp2f(z[u >> 1][(u & 1) * 8 + i] - ref);
+                    sum += p[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pf[u][i] = pack_bf16(p[2 * i], p[2 * i + 1]);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint16_t* vp = lds.v[buf] + col * TileLds<HD>::VS + u * 16 + grp * 8;
+#pragma unroll
+                for (int m = 0; m < HD / 32; ++m) acc[m] = mfma32(*(const u32x4*)(vp + m * 32 * TileLds<HD>::VS), pf[u], acc[m]);
+            }
+            if (lds.nan[buf] == j0 + 1) {  // NaN codes that were taken out: back in for the rows that see them
+                for (int j = j0; j < min(j0 + kSlots, end); ++j)
+#pragma unroll
+                    for (int m = 0; m < HD / 32; ++m)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (j < limit && (V[(int64_t)j * HD + m * 32 + row_of(i, grp)] & 0x7f) == 0x7f) acc[m][i] = __builtin_nanf("");
+            }
+        }
+        __syncthreads();
     }
-    if (tid == 0 && lse != nullptr) lse[(int64_t)row * a.Hq + h] = m + log2f(l);
+    sum += __shfl_xor(sum, 32, 64);
+    if (r >= rows) return;
+    const int many = (sees + sp.per - 1) / sp.per;  // ranges of this tile of rows
+    if (many > 1) {
+        const int64_t at = ((int64_t)pair * sp.ranges + range) * sp.tile_rows + r;
+#pragma unroll
+        for (int m = 0; m < HD / 32; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *(f32x4*)(sp.acc + at * HD + m * 32 + row_of(i * 4, grp)) = f32x4{acc[m][4 * i], acc[m][4 * i + 1], acc[m][4 * i + 2], acc[m][4 * i + 3]};
+        if (grp == 0) sp.ml[at] = make_float2(ref, sum);
+        return;
+    }
+    const float inv = 1.f / sum;
+    uint16_t* o = a.out.p + (int64_t)(q.row0 + token) * a.out.row + (int64_t)head * a.out.head;
+#pragma unroll
+    for (int m = 0; m < HD / 32; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u32x2 w;
+            w.x = pack_bf16(acc[m][4 * i] * inv, acc[m][4 * i + 1] * inv);
+            w.y = pack_bf16(acc[m][4 * i + 2] * inv, acc[m][4 * i + 3] * inv);
+            *(u32x2*)(o + m * 32 + row_of(i * 4, grp)) = w;
+        }
+    if (sp.final_ml != nullptr && grp == 0) sp.final_ml[(int64_t)pair * sp.tile_rows + r] = make_float2(ref, inv);
 }
 
-// One thread per slot: the weights that all rows and query heads gave it.
-__global__ __launch_bounds__(256) void weights_plain_kernel(Cache c, Step s, Attend a, const float* lse) {
-    const int chunks = (c.max_len + 255) / 256, G = a.Hq / c.Hkv;
-    const int64_t base = blockIdx.x / chunks;
-    const int j = blockIdx.x % chunks * 256 + threadIdx.x, seq = (int)(base / c.Hkv), hk = (int)(base % c.Hkv);
+// The weights of 256 slots (64 per wavefront, K in registers) from all rows that see them: S^T again, then
+// exp2(score - reference) / sum with the row's statistics, which are the lane's; added up over the rows in the lane, over
+// the lanes at the end.  32 rows of q at a time go through LDS, shared by the wavefronts.
+template <int HD>
+__global__ __launch_bounds__(256, 2) void prompt_weights_kernel(Cache c, Step s, Attend a, Split sp, int chunks) {
+    constexpr int QS = HD + 8, QI = 32 * HD / 8;  // pieces of 16 bytes of a tile of q
+    __shared__ uint16_t qt[2][32 * QS];
+    __shared__ float2 ml[2][32];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, grp = lane >> 5;
+    const int pairs = c.n_seq * c.Hkv;
+    const int pair = blockIdx.x % pairs, chunk = blockIdx.x / pairs;
+    const int seq = pair / c.Hkv, hk = pair % c.Hkv, G = a.Hq / c.Hkv;
     const Seq q = sequence(c, s, seq);
-    if (j >= q.cached + q.n_new) return;
-    float w = a.weight_in != nullptr && j < q.cached ? a.weight_in[base * c.max_len + j] : 0.f;
-    const uint8_t* K = c.codes[0] + (base * c.max_len + j) * c.hd;
-    const float ks = c.scale[0][base * (c.max_len >> c.logb) + (j >> c.logb)];
-    for (int i = max(0, j - q.cached); i < q.n_new; ++i)
-        for (int g = 0; g < G; ++g) {
-            const int64_t row = q.row0 + i, h = hk * G + g;
-            w += exp2f(score(a.q.p + row * a.q.row + h * a.q.head, K, ks, c.hd, a.qscale) - lse[row * a.Hq + h]);
+    const int total = q.cached + q.n_new, rows = q.n_new * G;
+    const int w0 = chunk * 256, j0 = w0 + wave * 64;
+    if (w0 >= total) return;
+    const int64_t base = (int64_t)seq * c.Hkv + hk;
+    const uint8_t* K = c.codes[0] + base * c.max_len * HD;
+    const float* ks = c.scale[0] + base * (c.max_len >> c.logb);
+    u32x4 kf[2][HD / 16];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int slot = min(j0 + t * 32 + col, total - 1);
+        const float sc = ks[slot >> c.logb];
+#pragma unroll
+        for (int f = 0; f < HD / 16; ++f) {
+            const u32x2 x = *(const u32x2*)(K + (int64_t)slot * HD + f * 16 + grp * 8);
+            kf[t][f] = widen8(x.x, x.y, sc);
         }
-    a.weight_out[base * c.max_len + j] = w;
+    }
+    float w[2][16];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[t][i] = 0.f;
+    const int r_first = max(0, w0 - q.cached) * G / 32 * 32;
+    u32x4 piece[QI / 256 > 0 ? QI / 256 : 1];
+    float2 piece_ml;
+    auto load = [&](int r0) {
+#pragma unroll
+        for (int i = 0; i < (QI + 255) / 256; ++i) {
+            const int at = threadIdx.x + i * 256, row = min(r0 + at / (HD / 8), rows - 1);
+            if (QI >= 256 || at < QI)
+                piece[i] = *(const u32x4*)(a.q.p + (int64_t)(q.row0 + row / G) * a.q.row + (int64_t)(hk * G + row % G) * a.q.head + at % (HD / 8) * 8);
+        }
+        if (threadIdx.x < 32) {
+            piece_ml = sp.final_ml[(int64_t)pair * sp.tile_rows + min(r0 + (int)threadIdx.x, rows - 1)];
+            if (r0 + (int)threadIdx.x >= rows) piece_ml.y = 0.f;
+        }
+    };
+    auto store = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < (QI + 255) / 256; ++i) {
+            const int at = threadIdx.x + i * 256;
+            if (QI >= 256 || at < QI) *(u32x4*)(qt[buf] + at / (HD / 8) * QS + at % (HD / 8) * 8) = piece[i];
+        }
+        if (threadIdx.x < 32) ml[buf][threadIdx.x] = piece_ml;
+    };
+    if (r_first < rows) {
+        load(r_first);
+        store(0);
+        if (r_first + 32 < rows) load(r_first + 32);
+    }
+    __syncthreads();
+    int buf = 0;
+    for (int r0 = r_first; r0 < rows; r0 += 32, buf ^= 1) {
+        if (r0 + 32 < rows) {
+            store(buf ^ 1);
+            if (r0 + 64 < rows) load(r0 + 64);
+        }
+        const int limit = q.cached + min(r0 + col, rows - 1) / G + 1;
+        const float2 e = ml[buf][col];
+        if (q.cached + min(r0 + 31, rows - 1) / G + 1 > j0) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                f32x16 z;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[i] = 0.f;
+                const uint16_t* p = qt[buf] + col * QS + grp * 8;
+#pragma unroll
+                for (int f = 0; f < HD / 16; ++f) z = mfma32(kf[t][f], *(const u32x4*)(p + f * 16), z);
+                const bool whole = r0 + 32 <= rows && j0 + t * 32 + 32 <= q.cached + r0 / G + 1;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], a.qscale, -e.x));
+                    if (whole) w[t][i] = __builtin_fmaf(x, e.y, w[t][i]);
+                    else w[t][i] += j0 + t * 32 + row_of(i, grp) < limit && r0 + col < rows ? x * e.y : 0.f;
+                }
+            }
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float x = w[t][i];
+#pragma unroll
+            for (int m = 1; m < 32; m <<= 1) x += __shfl_xor(x, m, 64);
+            const int slot = j0 + t * 32 + row_of(i, grp);
+            if (col == i && slot < total) {
+                if (a.weight_in != nullptr && slot < q.cached) x += a.weight_in[base * c.max_len + slot];
+                a.weight_out[base * c.max_len + slot] = x;
+            }
+        }
 }
 
 int64_t up256(int64_t v) { return (v + 255) & ~(int64_t)255; }
 
 // How a step is run, from its sizes and bounds.
 struct Plan {
-    int tiles;  // row tiles of decode_kernel, 0: many new tokens
+    int tiles;  // row tiles of decode_kernel; 0: many new tokens, in `row_tiles` tiles of kRows
+    int row_tiles;
     Split sp;
     int64_t o_ml, o_scores, o_final, bytes;
 };
@@ -477,18 +718,21 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
     const int64_t pairs = (int64_t)c.n_seq * c.Hkv, rows = (int64_t)s.max_new * (Hq / c.Hkv);
     const int most = (int)min((int64_t)s.max_cached + s.max_new, (int64_t)c.max_len);
     p.tiles = rows <= 8 ? 1 : rows <= 16 ? 2 : 0;
-    if (p.tiles == 0) {
-        p.bytes = weights ? up256((int64_t)s.n_rows * Hq * 4) : 0;
-        return p;
+    p.row_tiles = (int)((rows + kRows - 1) / kRows);
+    p.sp.tile_rows = p.tiles > 0 ? p.tiles * 8 : p.row_tiles * kRows;
+    int64_t per;
+    if (p.tiles > 0) {
+        per = ((int64_t)most * pairs / 2048 + 127) / 128 * 128;  // 2048 workgroups
+        per = per < 256 ? 256 : per;
+    } else {
+        int64_t want = 512 / (pairs * p.row_tiles);  // two workgroups for each compute unit
+        want = want < 1 ? 1 : want;
+        per = (most + want * kSlots - 1) / (want * kSlots) * kSlots;
+        per = per < 512 ? 512 : per;
     }
-    const int64_t want = 1024 * 2;  // workgroups
-    int64_t per = ((int64_t)most * pairs / want + 127) / 128 * 128;
-    per = per < 256 ? 256 : per;
-    int64_t ranges = (most + per - 1) / per;
-    if (ranges < 1) ranges = 1;
+    const int64_t ranges = most > per ? (most + per - 1) / per : 1;
     p.sp.per = (int)per;
     p.sp.ranges = (int)ranges;
-    p.sp.tile_rows = p.tiles * 8;
     p.sp.score_stride = (most + 31) / 32 * 32;
     int64_t o = 0;
     const int64_t items = ranges > 1 ? pairs * ranges * p.sp.tile_rows : 0;
@@ -496,7 +740,7 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
     p.o_ml = o;
     o += up256(items * 8);
     p.o_scores = o;
-    if (weights) o += up256(pairs * p.sp.tile_rows * p.sp.score_stride * 4);
+    if (weights && p.tiles > 0) o += up256(pairs * p.sp.tile_rows * p.sp.score_stride * 4);
     p.o_final = o;
     if (weights) o += up256(pairs * p.sp.tile_rows * 8);
     p.bytes = o;
@@ -504,20 +748,32 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
 }
 
 template <int HD, int NT>
-void launch_decode(hipStream_t st, const Cache& c, const Step& s, const Attend& a, const Split& sp) {
-    const dim3 grid((unsigned)((int64_t)c.n_seq * c.Hkv * sp.ranges)), block(256);
+void launch_decode(hipStream_t st, const dim3& grid, const Cache& c, const Step& s, const Attend& a, const Split& sp) {
     if (a.weight_out != nullptr)
-        hipLaunchKernelGGL((decode_kernel<HD, NT, true>), grid, block, 0, st, c, s, a, sp);
+        hipLaunchKernelGGL((decode_kernel<HD, NT, true>), grid, dim3(256), 0, st, c, s, a, sp);
     else
-        hipLaunchKernelGGL((decode_kernel<HD, NT, false>), grid, block, 0, st, c, s, a, sp);
-    if (sp.ranges > 1)
-        hipLaunchKernelGGL(merge_kernel<HD>, dim3((unsigned)(((int64_t)c.n_seq * c.Hkv * sp.tile_rows + 3) / 4)), block, 0, st, c, s, a, sp);
+        hipLaunchKernelGGL((decode_kernel<HD, NT, false>), grid, dim3(256), 0, st, c, s, a, sp);
 }
 
 template <int HD>
 void launch_hd(hipStream_t st, const Cache& c, const Step& s, const Attend& a, const Plan& p) {
-    if (p.tiles == 1) launch_decode<HD, 1>(st, c, s, a, p.sp);
-    if (p.tiles == 2) launch_decode<HD, 2>(st, c, s, a, p.sp);
+    const int64_t pairs = (int64_t)c.n_seq * c.Hkv;
+    const dim3 block(256);
+    if (s.n_rows > 0) {
+        const dim3 grid((unsigned)(pairs * p.sp.ranges * (p.tiles > 0 ? 1 : p.row_tiles)));
+        if (p.tiles == 1) launch_decode<HD, 1>(st, grid, c, s, a, p.sp);
+        else if (p.tiles == 2) launch_decode<HD, 2>(st, grid, c, s, a, p.sp);
+        else hipLaunchKernelGGL(prompt_kernel<HD>, grid, block, 0, st, c, s, a, p.sp, p.row_tiles);
+        if (p.sp.ranges > 1)
+            hipLaunchKernelGGL(merge_kernel<HD>, dim3((unsigned)((pairs * p.sp.tile_rows + 3) / 4)), block, 0, st, c, s, a, p.sp, p.tiles > 0);
+    }
+    if (a.weight_out == nullptr) return;
+    const int chunks = (p.sp.score_stride + 255) / 256;
+    if (chunks == 0) return;
+    if (p.tiles > 0)
+        hipLaunchKernelGGL(weights_kernel, dim3((unsigned)(pairs * chunks)), block, 0, st, c, s, a, p.sp, chunks);
+    else
+        hipLaunchKernelGGL(prompt_weights_kernel<HD>, dim3((unsigned)(pairs * chunks)), block, 0, st, c, s, a, p.sp, chunks);
 }
 
 }  // namespace
@@ -526,29 +782,13 @@ int64_t attend_workspace(const Cache& c, const Step& s, int Hq, bool weights) { 
 
 void launch_attend(hipStream_t st, const Cache& c, const Step& s, const Attend& a) {
     Plan p = plan(c, s, a.Hq, a.weight_out != nullptr);
-    if (p.tiles > 0) {
-        p.sp.acc = (float*)a.ws;
-        p.sp.ml = (float2*)(a.ws + p.o_ml);
-        p.sp.scores = (float*)(a.ws + p.o_scores);
-        p.sp.final_ml = a.weight_out != nullptr ? (float2*)(a.ws + p.o_final) : nullptr;
-        if (s.n_rows > 0) {
-            if (c.hd == 32) launch_hd<32>(st, c, s, a, p);
-            if (c.hd == 64) launch_hd<64>(st, c, s, a, p);
-            if (c.hd == 128) launch_hd<128>(st, c, s, a, p);
-        }
-        if (a.weight_out != nullptr) {
-            const int chunks = (p.sp.score_stride + 255) / 256;
-            if (chunks > 0)
-                hipLaunchKernelGGL(weights_kernel, dim3((unsigned)((int64_t)c.n_seq * c.Hkv * chunks)), dim3(256), 0, st, c, s, a, p.sp, chunks);
-        }
-        return;
-    }
-    float* lse = a.weight_out != nullptr ? (float*)a.ws : nullptr;
-    if (s.n_rows > 0)
-        hipLaunchKernelGGL(attend_plain_kernel, dim3((unsigned)((int64_t)s.n_rows * a.Hq)), dim3(256), 0, st, c, s, a, lse);
-    if (a.weight_out != nullptr)
-        hipLaunchKernelGGL(weights_plain_kernel, dim3((unsigned)((int64_t)c.n_seq * c.Hkv * ((c.max_len + 255) / 256))),
-                           dim3(256), 0, st, c, s, a, (const float*)lse);
+    p.sp.acc = (float*)a.ws;
+    p.sp.ml = (float2*)(a.ws + p.o_ml);
+    p.sp.scores = (float*)(a.ws + p.o_scores);
+    p.sp.final_ml = a.weight_out != nullptr ? (float2*)(a.ws + p.o_final) : nullptr;
+    if (c.hd == 32) launch_hd<32>(st, c, s, a, p);
+    if (c.hd == 64) launch_hd<64>(st, c, s, a, p);
+    if (c.hd == 128) launch_hd<128>(st, c, s, a, p);
 }
 
 }  // namespace kkv8
