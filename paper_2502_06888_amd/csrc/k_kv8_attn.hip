@@ -3,6 +3,8 @@
 // o = softmax(q K^T) V with K and V dequantised on the way into the matrix instructions: a scale is a power of two, so
 // code * scale is exact in bf16 and the conversion instruction applies it for nothing.  Products are bf16, sums and
 // softmax statistics fp32, base-2 exponentials with log2(e) folded into the factor of the scores.
+#include <type_traits>
+
 #include "kv8_kernels.h"
 
 namespace kkv8 {
@@ -55,10 +57,13 @@ struct Split {
     float2* ml;
     float* scores;      // [pair, row, slot] products q . K
     float2* final_ml;   // [pair, row] of the whole sequence: reference, 1 / sum of weights
+    u32x4* packed;      // [pair, tile of kSlots] dequantised (see Tile), or null
+    int32_t* odd;       // [pair, tile]
+    int packed_tiles;   // tiles per pair
 };
 
 template <int HD, int NT, bool SCORES>
-__global__ __launch_bounds__(256, NT == 1 ? 4 : HD < 128 ? 3 : 2) void decode_kernel(Cache c, Step s, Attend a, Split sp) {
+__global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) void decode_kernel(Cache c, Step s, Attend a, Split sp) {
     constexpr int KW = HD / 16;             // words of a K row that a lane holds: HD/4 bytes
     constexpr int VT = HD / 16;             // tiles of 16 elements of the sums
     constexpr int VW = VT >= 4 ? VT / 4 : 1;  // words of a V row that a lane holds: VT bytes
@@ -143,7 +148,8 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : HD < 128 ? 3 : 2) void decode_ke
         load_k(p0);
         load_v(p0);
     }
-    for (; p0 < end; p0 += 128) {
+    auto chunk = [&](auto whole_) {
+        constexpr bool whole = decltype(whole_)::value;  // every row sees all 32 slots
         f32x4 z[NT][2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -158,7 +164,6 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : HD < 128 ? 3 : 2) void decode_ke
             }
         }
         if (p0 + 128 < end) load_k(p0 + 128);
-        const bool whole = p0 + 32 <= q.cached + 1 && p0 + 32 <= end;  // every row sees all 32 slots
         bool odd = false;
         if (!whole) {  // weight 0 times a NaN code would be NaN: such codes are taken out, and put back where they are seen
             uint32_t nan = 0;
@@ -183,7 +188,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : HD < 128 ? 3 : 2) void decode_ke
             }
             float x[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = z[n][j >> 2][j & 3] * a.qscale;
+            for (int j = 0; j < 8; ++j) x[j] = z[n][j >> 2][j & 3];
             if (!whole) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -194,6 +199,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : HD < 128 ? 3 : 2) void decode_ke
             float top = x[0];
 #pragma unroll
             for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
+            top *= a.qscale;
             if (__any(top > m[n] - kNear)) {
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -211,7 +217,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : HD < 128 ? 3 : 2) void decode_ke
             float pr[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                pr[j] = __builtin_amdgcn_exp2f(x[j] - m[n]);
+                pr[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], a.qscale, -m[n]));
                 l[n] += pr[j];
             }
 #pragma unroll
@@ -249,7 +255,10 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : HD < 128 ? 3 : 2) void decode_ke
                             if (j <= q.cached + (n * 8 + ((grp * 4 + r) & 7)) / G) acc[n][v][r] = __builtin_nanf("");
                 }
         }
-    }
+    };
+    const int sure = min(end, q.cached + 1);
+    for (; p0 + 32 <= sure; p0 += 128) chunk(std::true_type{});
+    for (; p0 < end; p0 += 128) chunk(std::false_type{});
     // the lane groups of a column, the two halves of the weights, then the wavefronts
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -361,38 +370,38 @@ __global__ __launch_bounds__(256) void weights_kernel(Cache c, Step s, Attend a,
 // ---- many new tokens: bound by the matrix cores ---------------------------------------------------------------
 //
 // One workgroup of four wavefronts per (sequence, key-value head, 128 rows, range of slots); a row is a (token, query
-// head of the group), so the heads that share K and V share a tile of them.  64 slots at a time are dequantised once
-// per workgroup into LDS as bf16, V transposed on the way by bytes, while the codes of the next 64 are on their way.
-// A wavefront has 32 rows: S^T[slot][row] = K Q^T and O^T[element][row] = V^T P^T, 32x32x16.  Lane l holds row l%32
-// throughout, so softmax statistics and rescaling stay in the lane, and the weights of a lane are its operand of the
-// second product as they are: slots 4*(l/32)..+3 and 8 + 4*(l/32)..+3 of each 16, the order in which V^T is laid out.
+// head of the group), so the heads that share K and V share a tile of them: 64 slots as bf16 in LDS, the next 64 on
+// their way.  A wavefront has 32 rows: S^T[slot][row] = K Q^T and O^T[element][row] = V^T P^T, 32x32x16.  Lane l
+// holds row l%32 throughout, so softmax statistics and rescaling stay in the lane, and the weights of a lane are its
+// operand of the second product as they are: slots 4*(l/32)..+3 and 8 + 4*(l/32)..+3 of each 16.
+//
+// A tile lies in LDS in the order in which the matrix instructions take it: units of 64 lanes x 16 bytes, read
+// and written without bank conflicts; unit (t, f) of K: lane l holds slot 32t + l%32, elements 16f + 8*(l/32)..+7; unit
+// (u, m) of V: lane l holds element 32m + l%32, the eight slots of 16u.. in the order above.
+//
+// Where a tile serves many row tiles it is dequantised once, by pack_kernel, into the workspace in this order, and
+// comes from there into LDS without passing through registers; else the workgroup dequantises it on the way.
 template <int HD>
-struct TileLds {
-    static constexpr int KS = HD + 8, VS = kSlots + 8;  // 16 bytes of padding: reads of 16 bytes free of bank conflicts
-    uint16_t k[2][kSlots * KS];
-    uint16_t v[2][HD * VS];
-    int nan[2];
-};
+struct Tile {
+    static constexpr int kUnits = HD / 8;            // of K, and of V
+    static constexpr int kBytes = 2 * kUnits * 1024;  // K, then V
+    static constexpr int kPieces = kBytes / 4096;     // of 16 bytes per thread
+    __device__ __forceinline__ static int v_slot(int group, int j) { return (group >> 1) * 16 + (group & 1) * 4 + (j & 3) + (j >> 2) * 8; }
 
-// Codes of a tile on their way into LDS.  Items of 32 bytes: HD*2 of K (a slot's 32 elements), then HD*2 of V (four
-// elements of eight slots in the order of a lane's weights), shared out over the threads.
-template <int HD>
-struct TileLoad {
-    static constexpr int kItems = HD * 2, kBoth = kItems == 256;
+    // Codes on their way.  Items of 32 bytes: HD*2 of K (a slot's 32 elements), HD*2 of V (four elements of eight slots).
+    static constexpr int kItems = HD * 2;
+    static constexpr bool kBoth = kItems == 256;
     uint32_t kr[8], vr[8];
-    float ksc, vsc[1];
-
-    __device__ __forceinline__ static int k_item() { return threadIdx.x; }
+    float ksc, vsc;
     __device__ __forceinline__ static int v_item() { return kBoth ? (int)threadIdx.x : (int)threadIdx.x - kItems; }
     __device__ __forceinline__ static bool has_k() { return kBoth || (int)threadIdx.x < kItems; }
     __device__ __forceinline__ static bool has_v() { return kBoth || ((int)threadIdx.x >= kItems && (int)threadIdx.x < 2 * kItems); }
-    __device__ __forceinline__ static int v_slot(int group, int j) { return (group >> 1) * 16 + (group & 1) * 4 + (j & 3) + (j >> 2) * 8; }
 
     // slots past `total` re-read the last one
     __device__ __forceinline__ void load(const Cache& c, const uint8_t* K, const uint8_t* V, const float* ks, const float* vs, int j0, int total) {
         if (has_k()) {
-            const int i = k_item(), slot = min(j0 + i / (HD / 32), total - 1);
-            const u32x4* p = (const u32x4*)(K + (int64_t)slot * HD + i % (HD / 32) * 32);
+            const int slot = min(j0 + ((int)threadIdx.x & 63), total - 1);
+            const u32x4* p = (const u32x4*)(K + (int64_t)slot * HD + (threadIdx.x >> 6) * 32);
             const u32x4 a = p[0], b = p[1];
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
@@ -402,26 +411,27 @@ struct TileLoad {
             ksc = ks[slot >> c.logb];
         }
         if (has_v()) {
-            const int i = v_item(), quad = i % (HD / 4), group = i / (HD / 4);
+            const int quad = v_item() % (HD / 4), group = v_item() / (HD / 4);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 vr[j] = *(const uint32_t*)(V + (int64_t)min(j0 + v_slot(group, j), total - 1) * HD + quad * 4);
-            vsc[0] = vs[min(j0 + (group >> 1) * 16, total - 1) >> c.logb];
+            vsc = vs[min(j0 + (group >> 1) * 16, total - 1) >> c.logb];
         }
     }
-    // part: some row does not see all 64 slots.  Codes past `total` and NaN codes of V then count as 0 (weight 0 times NaN
-    // would reach rows that do not see the slot); that there were NaN is noted.
-    __device__ __forceinline__ void store(TileLds<HD>& t, int buf, int j0, int total, bool part) {
+    // Into a tile at `to`.  Codes of V past `total` count as 0, and so do NaN ones where `part` is set (weight 0 times NaN
+    // would reach rows that do not see the slot); returns whether there were such.
+    template <class P>
+    __device__ __forceinline__ bool store(P to, int j0, int total, bool part) {
+        uint32_t nan = 0;
         if (has_k()) {
-            const int i = k_item();
-            u32x4* to = (u32x4*)(t.k[buf] + i / (HD / 32) * TileLds<HD>::KS + i % (HD / 32) * 32);
+            const int slot = threadIdx.x & 63, p = threadIdx.x >> 6;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) to[w] = widen8(kr[2 * w], kr[2 * w + 1], ksc);
+            for (int w = 0; w < 4; ++w)
+                to[((slot >> 5) * (HD / 16) + 2 * p + (w >> 1)) * 64 + (slot & 31) + 32 * (w & 1)] = widen8(kr[2 * w], kr[2 * w + 1], ksc);
         }
         if (has_v()) {
-            const int i = v_item(), quad = i % (HD / 4), group = i / (HD / 4);
+            const int quad = v_item() % (HD / 4), group = v_item() / (HD / 4);
             if (part) {
-                uint32_t nan = 0;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     if (j0 + v_slot(group, j) >= total) vr[j] = 0u;
@@ -429,7 +439,6 @@ struct TileLoad {
                     vr[j] &= ~((n >> 7) * 0xffu);
                     nan |= n;
                 }
-                if (nan != 0) t.nan[buf] = j0 + 1;
             }
             uint32_t in[2][4], tr[2][4];
 #pragma unroll
@@ -438,10 +447,36 @@ struct TileLoad {
             transpose4(in[1], tr[1]);
 #pragma unroll
             for (int b = 0; b < 4; ++b)
-                *(u32x4*)(t.v[buf] + (quad * 4 + b) * TileLds<HD>::VS + group * 8) = widen8(tr[0][b], tr[1][b], vsc[0]);
+                to[(kUnits + (group >> 1) * (HD / 32) + (quad >> 3)) * 64 + (quad & 7) * 4 + b + 32 * (group & 1)] = widen8(tr[0][b], tr[1][b], vsc);
         }
+        return nan != 0;
     }
 };
+
+// The slots that a step's tokens see, dequantised tile by tile; `odd` notes the tiles of V with NaN codes, which are left out.
+template <int HD>
+__global__ __launch_bounds__(256) void pack_kernel(Cache c, Step s, u32x4* packed, int32_t* odd, int tiles) {
+    __shared__ int any;
+    const int pairs = c.n_seq * c.Hkv, pair = blockIdx.x % pairs, tile = blockIdx.x / pairs, j0 = tile * kSlots;
+    const Seq q = sequence(c, s, pair / c.Hkv);
+    const int total = q.cached + q.n_new;
+    if (j0 >= total || q.n_new == 0) return;
+    const int64_t base = (int64_t)pair * c.max_len, sb = (int64_t)pair * (c.max_len >> c.logb);
+    Tile<HD> t;
+    t.load(c, c.codes[0] + base * HD, c.codes[1] + base * HD, c.scale[0] + sb, c.scale[1] + sb, j0, total);
+    if (threadIdx.x == 0) any = 0;
+    __syncthreads();
+    if (t.store(packed + ((int64_t)pair * tiles + tile) * (Tile<HD>::kBytes / 16), j0, total, true)) any = 1;
+    __syncthreads();
+    if (threadIdx.x == 0) odd[(int64_t)pair * tiles + tile] = any;
+}
+
+// 16 bytes per lane from `from` (the lane's own address) to LDS at `to` + 16 * lane, without registers; the wavefront waits
+// for it with wait_copies().
+__device__ __forceinline__ void copy_to_lds(const void* from, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+}
+__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ f32x16 mfma32(const u32x4 a, const u32x4 b, const f32x16 c) {
@@ -450,9 +485,10 @@ __device__ __forceinline__ f32x16 mfma32(const u32x4 a, const u32x4 b, const f32
 // Row of a 32x32 result that register r of a lane in half g holds.
 __device__ __forceinline__ int row_of(int r, int g) { return 8 * (r >> 2) + 4 * g + (r & 3); }
 
-template <int HD>
+template <int HD, bool PACKED>
 __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend a, Split sp, int tiles) {
-    __shared__ TileLds<HD> lds;
+    __shared__ u32x4 lds[2][Tile<HD>::kBytes / 16];
+    __shared__ int nan[2];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, grp = lane >> 5;
     // last tiles first: they see the most slots; the pairs side by side, so that the tiles of one keep to an XCD
     const int pairs = c.n_seq * c.Hkv;
@@ -470,6 +506,8 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
     const int64_t base = (int64_t)seq * c.Hkv + hk;
     const uint8_t *K = c.codes[0] + base * c.max_len * HD, *V = c.codes[1] + base * c.max_len * HD;
     const float *ks = c.scale[0] + base * (c.max_len >> c.logb), *vs = c.scale[1] + base * (c.max_len >> c.logb);
+    const u32x4* packed = sp.packed + ((int64_t)pair * sp.packed_tiles + first / kSlots) * (Tile<HD>::kBytes / 16) + threadIdx.x;
+    const int32_t* odd = sp.odd + (int64_t)pair * sp.packed_tiles;
 
     const int r = row0 + wave * 32 + col;
     const int token = min(r, rows - 1) / G, head = hk * G + min(r, rows - 1) % G;
@@ -487,87 +525,96 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[m][i] = 0.f;
     float ref = kEmpty, sum = 0.f;
-    if (threadIdx.x < 2) lds.nan[threadIdx.x] = 0;
-    __syncthreads();
-    TileLoad<HD> next;
-    next.load(c, K, V, ks, vs, first, total);
-    next.store(lds, 0, first, total, first + kSlots > least);
-    if (first + kSlots < end) next.load(c, K, V, ks, vs, first + kSlots, total);
-    __syncthreads();
+    Tile<HD> next;
+    const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4*)&lds[0][0];
+    auto copy = [&](int buf) {  // the next tile, a sixteenth of 4 KB per thread and piece
+#pragma unroll
+        for (int i = 0; i < Tile<HD>::kPieces; ++i)
+            copy_to_lds(packed + i * 256, __builtin_amdgcn_readfirstlane(lds_at + buf * Tile<HD>::kBytes + i * 4096 + wave * 1024));
+        packed += Tile<HD>::kBytes / 16;
+    };
+    if (PACKED) {
+        copy(0);
+    } else {
+        if (threadIdx.x < 2) nan[threadIdx.x] = 0;
+        __syncthreads();
+        next.load(c, K, V, ks, vs, first, total);
+        if (next.store(lds[0], first, total, first + kSlots > least)) nan[0] = first + 1;
+        if (first + kSlots < end) next.load(c, K, V, ks, vs, first + kSlots, total);
+    }
     int buf = 0;
     for (int j0 = first; j0 < end; j0 += kSlots, buf ^= 1) {
+        if (PACKED) wait_copies();
+        __syncthreads();  // the tile is there, and nobody reads the other buffer any more
         if (j0 + kSlots < end) {
-            next.store(lds, buf ^ 1, j0 + kSlots, total, j0 + 2 * kSlots > least);
-            if (j0 + 2 * kSlots < end) next.load(c, K, V, ks, vs, j0 + 2 * kSlots, total);
+            if (PACKED) {
+                copy(buf ^ 1);
+            } else {
+                if (next.store(lds[buf ^ 1], j0 + kSlots, total, j0 + 2 * kSlots > least)) nan[buf ^ 1] = j0 + kSlots + 1;
+                if (j0 + 2 * kSlots < end) next.load(c, K, V, ks, vs, j0 + 2 * kSlots, total);
+            }
         }
-        if (active && j0 < wave_most) {
-            f32x16 z[2];
+        if (!active || j0 >= wave_most) continue;
+        const bool holes = PACKED ? odd[j0 / kSlots] != 0 : nan[buf] == j0 + 1;
+        f32x16 z[2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < 2; ++t) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) z[t][i] = 0.f;
-                const uint16_t* kp = lds.k[buf] + (t * 32 + col) * TileLds<HD>::KS + grp * 8;
+            for (int i = 0; i < 16; ++i) z[t][i] = 0.f;
 #pragma unroll
-                for (int f = 0; f < HD / 16; ++f) z[t] = mfma32(*(const u32x4*)(kp + f * 16), qf[f], z[t]);
-            }
-            const bool whole = j0 + kSlots <= wave_least && j0 + kSlots <= end;
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) z[t][i] *= a.qscale;
-            if (!whole) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int slot = j0 + t * 32 + row_of(i, grp);
-                        if (slot >= limit || slot >= end) z[t][i] = -__builtin_inff();
-                    }
-            }
-            float top = z[0][0];
+            for (int f = 0; f < HD / 16; ++f) z[t] = mfma32(lds[buf][(t * (HD / 16) + f) * 64 + lane], qf[f], z[t]);
+        }
+        const bool whole = j0 + kSlots <= wave_least && j0 + kSlots <= end;
+        if (!whole) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, z[t][i]);
-            if (__any(top > ref - kNear)) {
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float now = top > ref - kNear ? fmaxf(ref, top + kAbove) : ref;
-                const float f = __builtin_amdgcn_exp2f(ref - now);
-                ref = now;
-                sum *= f;
+                for (int i = 0; i < 16; ++i) {
+                    const int slot = j0 + t * 32 + row_of(i, grp);
+                    if (slot >= limit || slot >= end) z[t][i] = -__builtin_inff();
+                }
+        }
+        float top = z[0][0];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, z[t][i]);
+        top *= a.qscale;
+        if (__any(top > ref - kNear)) {
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float now = top > ref - kNear ? fmaxf(ref, top + kAbove) : ref;
+            const float f = __builtin_amdgcn_exp2f(ref - now);
+            ref = now;
+            sum *= f;
+#pragma unroll
+            for (int m = 0; m < HD / 32; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[m][i] *= f;
+        }
+        u32x4 pf[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            float p[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u >> 1][(u & 1) * 8 + i], a.qscale, -ref));
+                sum += p[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pf[u][i] = pack_bf16(p[2 * i], p[2 * i + 1]);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int m = 0; m < HD / 32; ++m) acc[m] = mfma32(lds[buf][(Tile<HD>::kUnits + u * (HD / 32) + m) * 64 + lane], pf[u], acc[m]);
+        if (holes) {  // NaN codes that were left out: back in for the rows that see them
+            for (int j = j0; j < min(j0 + kSlots, end); ++j)
 #pragma unroll
                 for (int m = 0; m < HD / 32; ++m)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[m][i] *= f;
-            }
-            u32x4 pf[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                float p[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    p[i] = __builtin_amdgcn_exp2f(z[u >> 1][(u & 1) * 8 + i] - ref);
-                    sum += p[i];
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) pf[u][i] = pack_bf16(p[2 * i], p[2 * i + 1]);
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const uint16_t* vp = lds.v[buf] + col * TileLds<HD>::VS + u * 16 + grp * 8;
-#pragma unroll
-                for (int m = 0; m < HD / 32; ++m) acc[m] = mfma32(*(const u32x4*)(vp + m * 32 * TileLds<HD>::VS), pf[u], acc[m]);
-            }
-            if (lds.nan[buf] == j0 + 1) {  // NaN codes that were taken out: back in for the rows that see them
-                for (int j = j0; j < min(j0 + kSlots, end); ++j)
-#pragma unroll
-                    for (int m = 0; m < HD / 32; ++m)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (j < limit && (V[(int64_t)j * HD + m * 32 + row_of(i, grp)] & 0x7f) == 0x7f) acc[m][i] = __builtin_nanf("");
-            }
+                    for (int i = 0; i < 16; ++i)
+                        if (j < limit && (V[(int64_t)j * HD + m * 32 + row_of(i, grp)] & 0x7f) == 0x7f) acc[m][i] = __builtin_nanf("");
         }
-        __syncthreads();
     }
     sum += __shfl_xor(sum, 32, 64);
     if (r >= rows) return;
@@ -710,7 +757,7 @@ struct Plan {
     int tiles;  // row tiles of decode_kernel; 0: many new tokens, in `row_tiles` tiles of kRows
     int row_tiles;
     Split sp;
-    int64_t o_ml, o_scores, o_final, bytes;
+    int64_t o_ml, o_scores, o_final, o_packed, o_odd, bytes;
 };
 
 Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
@@ -743,6 +790,15 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
     if (weights && p.tiles > 0) o += up256(pairs * p.sp.tile_rows * p.sp.score_stride * 4);
     p.o_final = o;
     if (weights) o += up256(pairs * p.sp.tile_rows * 8);
+    p.o_packed = o;
+    // dequantised once where several row tiles use a tile, and the copy stays under 4 GiB
+    const int64_t tiles = (most + kSlots - 1) / kSlots, copy = pairs * tiles * kSlots * c.hd * 4;
+    if (p.tiles == 0 && p.row_tiles >= 4 && copy <= (int64_t)4 << 30) {
+        p.sp.packed_tiles = (int)tiles;
+        o += up256(copy);
+        p.o_odd = o;
+        o += up256(pairs * tiles * 4);
+    }
     p.bytes = o;
     return p;
 }
@@ -763,7 +819,11 @@ void launch_hd(hipStream_t st, const Cache& c, const Step& s, const Attend& a, c
         const dim3 grid((unsigned)(pairs * p.sp.ranges * (p.tiles > 0 ? 1 : p.row_tiles)));
         if (p.tiles == 1) launch_decode<HD, 1>(st, grid, c, s, a, p.sp);
         else if (p.tiles == 2) launch_decode<HD, 2>(st, grid, c, s, a, p.sp);
-        else hipLaunchKernelGGL(prompt_kernel<HD>, grid, block, 0, st, c, s, a, p.sp, p.row_tiles);
+        else if (p.sp.packed_tiles > 0) {
+            hipLaunchKernelGGL(pack_kernel<HD>, dim3((unsigned)(pairs * p.sp.packed_tiles)), block, 0, st, c, s, p.sp.packed, p.sp.odd, p.sp.packed_tiles);
+            hipLaunchKernelGGL((prompt_kernel<HD, true>), grid, block, 0, st, c, s, a, p.sp, p.row_tiles);
+        } else
+            hipLaunchKernelGGL((prompt_kernel<HD, false>), grid, block, 0, st, c, s, a, p.sp, p.row_tiles);
         if (p.sp.ranges > 1)
             hipLaunchKernelGGL(merge_kernel<HD>, dim3((unsigned)((pairs * p.sp.tile_rows + 3) / 4)), block, 0, st, c, s, a, p.sp, p.tiles > 0);
     }
@@ -785,6 +845,8 @@ void launch_attend(hipStream_t st, const Cache& c, const Step& s, const Attend& 
     p.sp.acc = (float*)a.ws;
     p.sp.ml = (float2*)(a.ws + p.o_ml);
     p.sp.scores = (float*)(a.ws + p.o_scores);
+    p.sp.packed = (u32x4*)(a.ws + p.o_packed);
+    p.sp.odd = (int32_t*)(a.ws + p.o_odd);
     p.sp.final_ml = a.weight_out != nullptr ? (float2*)(a.ws + p.o_final) : nullptr;
     if (c.hd == 32) launch_hd<32>(st, c, s, a, p);
     if (c.hd == 64) launch_hd<64>(st, c, s, a, p);

@@ -91,7 +91,8 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {  // to nearest even
-    return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)lo) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)hi) << 16;
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
 }
 // Four codes rounded again to another scale: `by` = old scale / new scale, a power of two of at most 1.
 __device__ __forceinline__ uint32_t rescale4(uint32_t w, float by) {
