@@ -377,7 +377,7 @@ __global__ __launch_bounds__(256) void weights_kernel(Cache c, Step s, Attend a,
 //
 // A tile lies in LDS in the order in which the matrix instructions take it: units of 64 lanes x 16 bytes, read
 // and written without bank conflicts; unit (t, f) of K: lane l holds slot 32t + l%32, elements 16f + 8*(l/32)..+7; unit
-// (u, m) of V: lane l holds element 32m + l%32, the eight slots of 16u.. in the order above.
+// (u, m) of V: element 32m + l%32, the eight slots of 16u.. in the order above, at place v_place.
 //
 // Where a tile serves many row tiles it is dequantised once, by pack_kernel, into the workspace in this order, and
 // comes from there into LDS without passing through registers; else the workgroup dequantises it on the way.
@@ -387,6 +387,12 @@ struct Tile {
     static constexpr int kBytes = 2 * kUnits * 1024;  // K, then V
     static constexpr int kPieces = kBytes / 4096;     // of 16 bytes per thread
     __device__ __forceinline__ static int v_slot(int group, int j) { return (group >> 1) * 16 + (group & 1) * 4 + (j & 3) + (j >> 2) * 8; }
+
+    // Place of (element % 32, half of the slots) in a unit of V with elements 32m..: spread so that both the threads that
+    // write four neighbouring elements and the lanes that read 32 touch every bank once.
+    __device__ __forceinline__ static int v_place(int e, int half, int m) {
+        return ((e >> 2) ^ ((e >> 1) & 1)) | ((e & 1) << 3 ^ (m >> 1) << 3) | ((e >> 1) & 1) << 4 | half << 5;
+    }
 
     // Codes on their way.  Items of 32 bytes: HD*2 of K (a slot's 32 elements), HD*2 of V (four elements of eight slots).
     static constexpr int kItems = HD * 2;
@@ -447,7 +453,7 @@ struct Tile {
             transpose4(in[1], tr[1]);
 #pragma unroll
             for (int b = 0; b < 4; ++b)
-                to[(kUnits + (group >> 1) * (HD / 32) + (quad >> 3)) * 64 + (quad & 7) * 4 + b + 32 * (group & 1)] = widen8(tr[0][b], tr[1][b], vsc);
+                to[(kUnits + (group >> 1) * (HD / 32) + (quad >> 3)) * 64 + v_place((quad & 7) * 4 + b, group & 1, quad >> 3)] = widen8(tr[0][b], tr[1][b], vsc);
         }
         return nan != 0;
     }
@@ -514,6 +520,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
     const int limit = q.cached + token + 1;
     const int wave_least = q.cached + min(row0 + wave * 32, rows - 1) / G + 1;
     const int wave_most = q.cached + min(row0 + wave * 32 + 31, rows - 1) / G + 1;
+    const int within = min(limit, end) - 4 * grp;  // slots of this range that the row sees, less the lane's own offset
     const bool active = row0 + wave * 32 < rows;
     u32x4 qf[HD / 16];
     const uint16_t* qp = a.q.p + (int64_t)(q.row0 + token) * a.q.row + (int64_t)head * a.q.head + grp * 8;
@@ -542,6 +549,10 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
         if (next.store(lds[0], first, total, first + kSlots > least)) nan[0] = first + 1;
         if (first + kSlots < end) next.load(c, K, V, ks, vs, first + kSlots, total);
     }
+    const int v_at = Tile<HD>::v_place(col, grp, 0);
+    // q is waited for here: a wait in the loop would be one for the copies of the next tile, too
+#pragma unroll
+    for (int f = 0; f < HD / 16; ++f) asm volatile("" : "+v"(qf[f]));
     int buf = 0;
     for (int j0 = first; j0 < end; j0 += kSlots, buf ^= 1) {
         if (PACKED) wait_copies();
@@ -570,8 +581,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int slot = j0 + t * 32 + row_of(i, grp);
-                    if (slot >= limit || slot >= end) z[t][i] = -__builtin_inff();
+                    if (t * 32 + row_of(i, 0) >= within - j0) z[t][i] = -__builtin_inff();
                 }
         }
         float top = z[0][0];
@@ -606,7 +616,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int m = 0; m < HD / 32; ++m) acc[m] = mfma32(lds[buf][(Tile<HD>::kUnits + u * (HD / 32) + m) * 64 + lane], pf[u], acc[m]);
+            for (int m = 0; m < HD / 32; ++m) acc[m] = mfma32(lds[buf][(Tile<HD>::kUnits + u * (HD / 32) + m) * 64 + (v_at ^ (m >> 1) << 3)], pf[u], acc[m]);
         if (holes) {  // NaN codes that were left out: back in for the rows that see them
             for (int j = j0; j < min(j0 + kSlots, end); ++j)
 #pragma unroll
@@ -617,9 +627,9 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
         }
     }
     sum += __shfl_xor(sum, 32, 64);
-    if (r >= rows) return;
     const int many = (sees + sp.per - 1) / sp.per;  // ranges of this tile of rows
     if (many > 1) {
+        if (r >= rows) return;
         const int64_t at = ((int64_t)pair * sp.ranges + range) * sp.tile_rows + r;
 #pragma unroll
         for (int m = 0; m < HD / 32; ++m)
@@ -630,7 +640,11 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
         return;
     }
     const float inv = 1.f / sum;
-    uint16_t* o = a.out.p + (int64_t)(q.row0 + token) * a.out.row + (int64_t)head * a.out.head;
+    if (sp.final_ml != nullptr && grp == 0 && r < rows) sp.final_ml[(int64_t)pair * sp.tile_rows + r] = make_float2(ref, inv);
+    // rows through LDS (16 bytes of padding), so that a row leaves in one piece
+    constexpr int RS = HD / 8 + 1;
+    __syncthreads();
+    u32x4* mine = &lds[0][0] + wave * 32 * RS;
 #pragma unroll
     for (int m = 0; m < HD / 32; ++m)
 #pragma unroll
@@ -638,9 +652,15 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
             u32x2 w;
             w.x = pack_bf16(acc[m][4 * i] * inv, acc[m][4 * i + 1] * inv);
             w.y = pack_bf16(acc[m][4 * i + 2] * inv, acc[m][4 * i + 3] * inv);
-            *(u32x2*)(o + m * 32 + row_of(i * 4, grp)) = w;
+            ((u32x2*)(mine + col * RS))[(m * 32 + row_of(i * 4, grp)) / 4] = w;
         }
-    if (sp.final_ml != nullptr && grp == 0) sp.final_ml[(int64_t)pair * sp.tile_rows + r] = make_float2(ref, inv);
+    constexpr int LPR = HD / 8;  // lanes per row
+#pragma unroll
+    for (int i = 0; i < 32 / (64 / LPR); ++i) {
+        const int in = i * (64 / LPR) + lane / LPR, at = row0 + wave * 32 + in;
+        if (at < rows)
+            *(u32x4*)(a.out.p + (int64_t)(q.row0 + at / G) * a.out.row + (int64_t)(hk * G + at % G) * a.out.head + lane % LPR * 8) = mine[in * RS + lane % LPR];
+    }
 }
 
 // The weights of 256 slots (64 per wavefront, K in registers) from all rows that see them: S^T again, then
