@@ -11,7 +11,7 @@ namespace {
 // scale rose.  A lane takes 16-byte pieces of the rows (8 elements) and writes 8 codes.
 template <int WAVES>
 __global__ __launch_bounds__(256) void append_kernel(Cache c, Step s, Rows k, Rows v, int blocks) {
-    constexpr int UNITS = 4 / WAVES, N = 64 * WAVES;
+    constexpr int UNITS = 4 / WAVES, N = 64 * WAVES, PER = WAVES == 1 ? 1 : 8;
     __shared__ uint32_t most[4];
     const int wave = threadIdx.x >> 6;
     const int tid = (int)threadIdx.x % N;
@@ -25,14 +25,22 @@ __global__ __launch_bounds__(256) void append_kernel(Cache c, Step s, Rows k, Ro
     const int lo = max(q.cached, block << c.logb), hi = min(q.cached + q.n_new, (block + 1) << c.logb);
     const int n = exists ? max(hi - lo, 0) : 0;  // new slots of this block
     const Rows r = kv ? v : k;
-    const int pieces = c.hd / 8, total = n * pieces;
+    const int logp = c.hd == 128 ? 4 : c.hd == 64 ? 3 : 2, total = n << logp;  // pieces of 8 elements
     const uint16_t* src = r.p + (int64_t)(q.row0 + (lo - q.cached)) * r.row + (int64_t)head * r.head;
+    // at most PER pieces per thread: a block of 128 slots of 128 elements, or four tokens for a wavefront
+    u32x4 x[PER];
     uint32_t top = 0;
-    for (int i = tid; i < total; i += N) {
-        const u32x4 x = *(const u32x4*)(src + (int64_t)(i / pieces) * r.row + i % pieces * 8);
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+        const int i = tid + u * N;
+        if (i < total) x[u] = __builtin_nontemporal_load((const u32x4*)(src + (int64_t)(i >> logp) * r.row + (i & ((1 << logp) - 1)) * 8));
+    }
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+        if (tid + u * N >= total) break;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t a = x[j] & 0x7fffu, b = (x[j] >> 16) & 0x7fffu;  // magnitudes order as integers
+            const uint32_t a = x[u][j] & 0x7fffu, b = (x[u][j] >> 16) & 0x7fffu;  // magnitudes order as integers
             if (a < 0x7f80u) top = max(top, a);
             if (b < 0x7f80u) top = max(top, b);
         }
@@ -60,11 +68,13 @@ __global__ __launch_bounds__(256) void append_kernel(Cache c, Step s, Rows k, Ro
     }
     const float inv = 1.f / now;  // a power of two
     u32x2* dst = (u32x2*)(codes + (int64_t)lo * c.hd);
-    for (int i = tid; i < total; i += N) {
-        const u32x4 x = *(const u32x4*)(src + (int64_t)(i / pieces) * r.row + i % pieces * 8);
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+        const int i = tid + u * N;
+        if (i >= total) break;
         u32x2 o;
-        o.x = codes4(bf_lo(x.x) * inv, bf_hi(x.x) * inv, bf_lo(x.y) * inv, bf_hi(x.y) * inv);
-        o.y = codes4(bf_lo(x.z) * inv, bf_hi(x.z) * inv, bf_lo(x.w) * inv, bf_hi(x.w) * inv);
+        o.x = codes4(bf_lo(x[u].x) * inv, bf_hi(x[u].x) * inv, bf_lo(x[u].y) * inv, bf_hi(x[u].y) * inv);
+        o.y = codes4(bf_lo(x[u].z) * inv, bf_hi(x[u].z) * inv, bf_lo(x[u].w) * inv, bf_hi(x[u].w) * inv);
         dst[i] = o;
     }
     if (kv == 0 && c.position != nullptr) {
@@ -101,22 +111,167 @@ __device__ __forceinline__ uint32_t scan256(uint32_t v, uint32_t* total, uint32_
     return before + inc - v;
 }
 
-// One workgroup per (sequence, head): the key of the keep-th largest weight digit by digit (four passes over 8 bits),
-// then the chosen slots in order, the list of those that have to move, and what every slot below `keep` takes over.
-__global__ __launch_bounds__(256) void select_kernel(Cache c, const int32_t* held, int max_held, int keep, int recent,
-                                                     const int32_t* next_position, const float* weight_in,
-                                                     float* weight_out, const int32_t* position_in,
-                                                     int32_t* position_out, int32_t* sources, int32_t* kept) {
+// What a (sequence, head) pair selects from and writes to.
+struct Select {
+    const int32_t* held;
+    int32_t max_held, keep, recent;
+    const int32_t* next_position;
+    const float* weight_in;
+    float* weight_out;
+    const int32_t* position_in;
+    int32_t* position_out;
+    int32_t* sources;  // [pair, keep] chosen slots from `keep` on, in order
+    int32_t* kept;     // [pair, keep] slot that each slot was before
+};
+
+// One group of WAVES wavefronts per (sequence, head), KPT keys per lane in registers (slot = step * lanes + lane).  The key
+// of the keep-th largest weight is found by halving the range of keys, 32 times: the compares of a step leave a count in
+// scalar registers, groups of several wavefronts add theirs up through LDS.  Then the ranks of the chosen slots,
+// by ballots and one scan over the (step, wavefront) counts.  Reads weights and positions once: 4096 pairs of 576 slots
+// take one wavefront each; a few pairs of thousands of slots would leave the chip idle, so 16 wavefronts share one.
+// The halving ends as soon as a bound parts off just `keep` keys, after 20 steps or so where weights differ.
+template <int WAVES, int KPT>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_kernel(Cache c, Select a) {
+    constexpr int GROUPS = WAVES == 1 ? 4 : 1, LANES = WAVES * 64, CELLS = KPT * WAVES;
+    __shared__ int counts[2][WAVES];
+    __shared__ uint32_t cells[GROUPS][CELLS];
+    const int group = WAVES == 1 ? threadIdx.x >> 6 : 0, wave = WAVES == 1 ? 0 : threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int tid = wave * 64 + lane;
+    const int64_t pair = (int64_t)blockIdx.x * GROUPS + group;
+    const bool exists = pair < (int64_t)c.n_seq * c.Hkv;
+    const int64_t at = exists ? pair : 0;
+    const int seq = (int)(at / c.Hkv), keep = a.keep;
+    const int n = exists ? clampi(a.held[seq], 0, a.max_held) : 0;
+    const bool cut = n > keep;
+    const float* win = a.weight_in + at * c.max_len;
+    const int32_t* pin = a.position_in + at * c.max_len;
+    float* wout = a.weight_out + at * c.max_len;
+    int32_t* pout = a.position_out + at * c.max_len;
+    int32_t *list = a.sources + at * keep, *to = a.kept + at * keep;
+    // positions from here on are recent; in 64 bits, since next - recent may pass the least int
+    const int64_t young = (int64_t)(a.next_position != nullptr ? a.next_position[seq] : n) - a.recent;
+    uint32_t key[KPT];
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) {
+        const int i = j * LANES + tid;
+        key[j] = 0;
+        if (cut && i < n) key[j] = key_of(win[i], a.recent > 0 && pin[i] >= young);
+    }
+    // keys past n count as 0, the least there is: they are told apart by their slot
+    int phase = 0;
+    auto count_over = [&](uint32_t v) {  // keys >= v, v > 0
+        int sum = 0;
+#pragma unroll
+        for (int j = 0; j < KPT; ++j) sum += __popcll(__ballot(key[j] >= v));
+        if (WAVES > 1) {
+            if (lane == 0) counts[phase][wave] = sum;
+            __syncthreads();
+            sum = 0;
+            for (int w = 0; w < WAVES; ++w) sum += counts[phase][w];
+            phase ^= 1;  // the next counts go elsewhere, so that one barrier is enough
+        }
+        return sum;
+    };
+    uint32_t best = 0;  // largest key that at least `keep` keys reach
+    int want = -1;      // how many of the slots at it are chosen
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t v = best | 1u << bit;
+        const int reach = count_over(v);
+        if (reach >= keep) best = v;
+        if (reach == keep) {  // just these: all that lie over v - 1
+            best = v - 1;
+            want = 0;
+            break;
+        }
+    }
+    if (want < 0) want = keep - (best == 0xffffffffu ? 0 : count_over(best + 1));
+    // exclusive sums over the cells (step, wavefront) in order; a wavefront scans them, CELLS / 64 per lane
+    auto scan = [&] {
+        __syncthreads();
+        if (wave == 0) {
+            constexpr int PER = (CELLS + 63) / 64;
+            uint32_t v[PER], mine = 0;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                v[e] = lane * PER + e < CELLS ? cells[group][lane * PER + e] : 0u;
+                mine += v[e];
+            }
+            uint32_t inc = mine;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const uint32_t o = (uint32_t)__shfl_up((int)inc, d, 64);
+                if (lane >= d) inc += o;
+            }
+            uint32_t run = inc - mine;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                if (lane * PER + e < CELLS) cells[group][lane * PER + e] = run;
+                run += v[e];
+            }
+        }
+        __syncthreads();
+    };
+    const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) {
+        const uint64_t ties = __ballot(j * LANES + tid < n && key[j] == best);
+        if (lane == 0) cells[group][j * WAVES + wave] = (uint32_t)__popcll(ties);
+    }
+    scan();
+    uint64_t chosen[KPT];
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) {
+        const int i = j * LANES + tid;
+        const bool tie = i < n && key[j] == best;
+        const uint64_t ties = __ballot(tie);
+        const int rank = (int)cells[group][j * WAVES + wave] + __popcll(ties & below);
+        chosen[j] = __ballot(i < n && (key[j] > best || (tie && rank < want)));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) {
+        const int i = j * LANES + tid;
+        const bool in = chosen[j] >> lane & 1;
+        const uint64_t holes = __ballot(cut && i < keep && !in), sources = __ballot(cut && i >= keep && in);
+        if (lane == 0) cells[group][j * WAVES + wave] = (uint32_t)__popcll(holes) | (uint32_t)__popcll(sources) << 16;
+    }
+    scan();
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) {
+        const int i = j * LANES + tid;
+        const bool in = chosen[j] >> lane & 1;
+        const uint64_t sources = __ballot(cut && i >= keep && in);
+        if (cut && i >= keep && in) list[(cells[group][j * WAVES + wave] >> 16) + __popcll(sources & below)] = i;
+    }
+    __syncthreads();  // the list is there (of this workgroup's own pairs)
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) {
+        const int i = j * LANES + tid;
+        const bool in = chosen[j] >> lane & 1;
+        const uint64_t holes = __ballot(cut && i < keep && !in);
+        if (!exists || i >= keep) continue;
+        int from = i < n ? i : -1;
+        if (cut && !in) from = list[(cells[group][j * WAVES + wave] & 0xffffu) + __popcll(holes & below)];
+        to[i] = from;
+        if (from < 0) continue;
+        if (from != i || wout != win) wout[i] = win[from];
+        if (from != i || pout != pin) pout[i] = pin[from];
+    }
+}
+
+// The same for sequences of any length, 256 slots at a time: the key digit by digit (four passes over 8 bits), then the
+// chosen slots in order.
+__global__ __launch_bounds__(256) void select_long_kernel(Cache c, Select a) {
     __shared__ uint32_t hist[256], part[4], found[2];
     const int64_t pair = blockIdx.x;
-    const int seq = (int)(pair / c.Hkv), tid = threadIdx.x;
-    const int n = clampi(held[seq], 0, max_held);
-    const float* win = weight_in + pair * c.max_len;
-    float* wout = weight_out + pair * c.max_len;
-    const int32_t* pin = position_in + pair * c.max_len;
-    int32_t* pout = position_out + pair * c.max_len;
-    int32_t* list = sources + pair * keep;
-    int32_t* to = kept + pair * keep;
+    const int seq = (int)(pair / c.Hkv), tid = threadIdx.x, keep = a.keep;
+    const int n = clampi(a.held[seq], 0, a.max_held);
+    const float* win = a.weight_in + pair * c.max_len;
+    float* wout = a.weight_out + pair * c.max_len;
+    const int32_t* pin = a.position_in + pair * c.max_len;
+    int32_t* pout = a.position_out + pair * c.max_len;
+    int32_t* list = a.sources + pair * keep;
+    int32_t* to = a.kept + pair * keep;
     if (n <= keep) {
         for (int i = tid; i < keep; i += 256) {
             to[i] = i < n ? i : -1;
@@ -127,9 +282,8 @@ __global__ __launch_bounds__(256) void select_kernel(Cache c, const int32_t* hel
         }
         return;
     }
-    // positions from here on are recent; in 64 bits, since next - recent may pass the least int
-    const int64_t young = (int64_t)(next_position != nullptr ? next_position[seq] : n) - recent;
-    auto key = [&](int i) { return key_of(win[i], recent > 0 && pin[i] >= young); };
+    const int64_t young = (int64_t)(a.next_position != nullptr ? a.next_position[seq] : n) - a.recent;
+    auto key = [&](int i) { return key_of(win[i], a.recent > 0 && pin[i] >= young); };
     uint32_t prefix = 0;
     int want = keep;  // how many of the slots that share the prefix are chosen
     for (int shift = 24; shift >= 0; shift -= 8) {
@@ -179,39 +333,50 @@ __global__ __launch_bounds__(256) void select_kernel(Cache c, const int32_t* hel
     }
 }
 
-// One workgroup per (sequence, head, block below `keep`): the codes that moved into it.
+// One wavefront per (sequence, head, block below `keep`, K or V): the codes that move into it, 16 bytes per lane.
+template <int HD>
 __global__ __launch_bounds__(256) void move_kernel(Cache c, int keep, const int32_t* kept) {
-    const int blocks = keep >> c.logb, B = 1 << c.logb;
-    const int64_t pair = blockIdx.x / blocks;
-    const int block = blockIdx.x % blocks;
-    const int32_t* from = kept + pair * keep + (block << c.logb);
-    __shared__ int src[128];
-    __shared__ int any;
-    if (threadIdx.x == 0) any = 0;
-    __syncthreads();
-    if (threadIdx.x < (unsigned)B) {
-        const int f = from[threadIdx.x];
-        src[threadIdx.x] = f;
-        if (f >= keep) any = 1;
-    }
-    __syncthreads();
-    if (any == 0) return;
-    const int words = c.hd / 4;
-    for (int kv = 0; kv < 2; ++kv) {
-        float* scale = c.scale[kv] + pair * (c.max_len >> c.logb);
-        uint32_t* codes = (uint32_t*)(c.codes[kv] + pair * c.max_len * c.hd);
-        const float before = scale[block];
-        float now = before;
-        for (int i = 0; i < B; ++i)
-            if (src[i] >= keep) now = fmaxf(now, scale[src[i] >> c.logb]);
-        __syncthreads();
-        if (threadIdx.x == 0) scale[block] = now;
-        for (int i = threadIdx.x; i < B * words; i += 256) {
-            const int slot = i / words, f = src[slot];
-            if (f < keep && (now == before || f < 0)) continue;
-            const float by = (f >= keep ? scale[f >> c.logb] : before) / now;
-            const uint32_t w = codes[(int64_t)f * words + i % words];
-            codes[((int64_t)(block << c.logb) + slot) * words + i % words] = by == 1.f ? w : rescale4(w, by);
+    constexpr int LPS = HD / 16, SIDE = 64 / LPS;  // lanes per slot, slots side by side
+    const int blocks = keep >> c.logb, B = 1 << c.logb, lane = threadIdx.x & 63;
+    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), of = item >> 1;
+    const int64_t pair = of / blocks;
+    if (pair >= (int64_t)c.n_seq * c.Hkv) return;
+    const int block = (int)(of % blocks), kv = (int)(item & 1);
+    const int32_t* list = kept + pair * keep + (block << c.logb);
+    const int f0 = lane < B ? list[lane] : -1, f1 = lane + 64 < B ? list[lane + 64] : -1;
+    if (!__any(f0 >= keep || f1 >= keep)) return;
+    float* scale = c.scale[kv] + pair * (c.max_len >> c.logb);
+    u32x4* codes = (u32x4*)(c.codes[kv] + pair * c.max_len * HD);
+    const float before = scale[block];
+    const float s0 = f0 >= keep ? scale[f0 >> c.logb] : before, s1 = f1 >= keep ? scale[f1 >> c.logb] : before;
+    float now = fmaxf(s0, s1);
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) now = fmaxf(now, __shfl_xor(now, m, 64));
+    now = fmaxf(now, before);
+    if (lane == 0) scale[block] = now;
+    const float b0 = s0 / now, b1 = s1 / now;  // powers of two
+    constexpr int AHEAD = 4;  // pieces on their way per lane
+    for (int i = 0; i < B; i += AHEAD * SIDE) {
+        u32x4 x[AHEAD];
+        float by[AHEAD];
+        bool moves[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int slot = i + u * SIDE + lane / LPS;
+            const int fa = __shfl(f0, slot & 63, 64), fb = __shfl(f1, slot & 63, 64);
+            const float ba = __shfl(b0, slot & 63, 64), bb = __shfl(b1, slot & 63, 64);
+            const int from = slot < 64 ? fa : fb;
+            by[u] = slot < 64 ? ba : bb;
+            moves[u] = slot < B && from >= 0 && (from >= keep || by[u] != 1.f);
+            if (moves[u]) x[u] = codes[(int64_t)from * LPS + lane % LPS];
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (!moves[u]) continue;
+            if (by[u] != 1.f)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) x[u][w] = rescale4(x[u][w], by[u]);
+            codes[((int64_t)(block << c.logb) + i + u * SIDE + lane / LPS) * LPS + lane % LPS] = x[u];
         }
     }
 }
@@ -236,12 +401,21 @@ void launch_evict(hipStream_t st, const Cache& c, const int32_t* held, int max_h
                   const int32_t* next_position, const float* weight_in, float* weight_out, int32_t* position_out,
                   int32_t* kept, uint8_t* ws) {
     const int64_t pairs = (int64_t)c.n_seq * c.Hkv;
-    int32_t* list = (int32_t*)ws;
     if (kept == nullptr) kept = (int32_t*)(ws + up256(pairs * keep * 4));
-    hipLaunchKernelGGL(select_kernel, dim3((unsigned)pairs), dim3(256), 0, st, c, held, max_held, keep, recent,
-                       next_position, weight_in, weight_out, c.position, position_out, list, kept);
-    if (max_held > keep)
-        hipLaunchKernelGGL(move_kernel, dim3((unsigned)(pairs * (keep >> c.logb))), dim3(256), 0, st, c, keep, kept);
+    const Select a{held, max_held, keep, recent, next_position, weight_in, weight_out, c.position, position_out, (int32_t*)ws, kept};
+    const int most = max_held > keep ? max_held : keep;  // slots that the lanes have to cover
+    const unsigned p = (unsigned)pairs, p4 = (unsigned)((pairs + 3) / 4);
+    if (most <= 512) hipLaunchKernelGGL((select_kernel<1, 8>), dim3(p4), dim3(256), 0, st, c, a);
+    else if (most <= 768) hipLaunchKernelGGL((select_kernel<1, 12>), dim3(p4), dim3(256), 0, st, c, a);
+    else if (most <= 1024) hipLaunchKernelGGL((select_kernel<1, 16>), dim3(p4), dim3(256), 0, st, c, a);
+    else if (most <= 4096) hipLaunchKernelGGL((select_kernel<16, 4>), dim3(p), dim3(1024), 0, st, c, a);
+    else if (most <= 16384) hipLaunchKernelGGL((select_kernel<16, 16>), dim3(p), dim3(1024), 0, st, c, a);
+    else hipLaunchKernelGGL(select_long_kernel, dim3(p), dim3(256), 0, st, c, a);
+    if (max_held <= keep) return;
+    const dim3 grid((unsigned)((pairs * (keep >> c.logb) * 2 + 3) / 4)), block(256);
+    if (c.hd == 32) hipLaunchKernelGGL(move_kernel<32>, grid, block, 0, st, c, keep, kept);
+    if (c.hd == 64) hipLaunchKernelGGL(move_kernel<64>, grid, block, 0, st, c, keep, kept);
+    if (c.hd == 128) hipLaunchKernelGGL(move_kernel<128>, grid, block, 0, st, c, keep, kept);
 }
 
 }  // namespace kkv8

@@ -51,9 +51,8 @@ def _check(status: int):
         raise B.MoeError(status, load_library().moe_kv8_last_error().decode())
 
 
-def _want(ok: bool, what: str):
-    if not ok:
-        raise B.MoeError(B.MOE_ERR_INVALID_ARG, what)
+def _refuse(what: str):
+    raise B.MoeError(B.MOE_ERR_INVALID_ARG, what)
 
 
 def _ptr(t):
@@ -62,8 +61,8 @@ def _ptr(t):
 
 def _whole(t, name: str, dtype, shape):
     """`t` is a contiguous tensor of this type and shape."""
-    _want(t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
-          f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
     return t
 
 
@@ -72,7 +71,8 @@ class Kv8Cache:
 
     def __init__(self, k, v, k_scale, v_scale, block: int, position=None):
         import torch
-        _want(k.dim() == 4, "k must have four dimensions [n_seq, n_kv_heads, max_len, head_dim]")
+        if k.dim() != 4:
+            _refuse("k must have four dimensions [n_seq, n_kv_heads, max_len, head_dim]")
         n_seq, kv, max_len, hd = k.shape
         _whole(k, "k", torch.uint8, k.shape)
         _whole(v, "v", torch.uint8, k.shape)
@@ -82,7 +82,7 @@ class Kv8Cache:
             _whole(position, "position", torch.int32, (n_seq, kv, max_len))
         self.k, self.v, self.k_scale, self.v_scale, self.position, self.block = k, v, k_scale, v_scale, position, block
         self.n_seq, self.n_kv_heads, self.max_len, self.head_dim = n_seq, kv, max_len, hd
-        self.device = k.device
+        self.device, self.slots = k.device, k.shape[:3]
         self.c = MoeKv8Cache(n_seq, kv, hd, max_len, block, 0, _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(position))
         self.ref = C.byref(self.c)
 
@@ -115,17 +115,22 @@ class Kv8Step:
 
 
 def _stream(cache: Kv8Cache, stream):
+    if stream is not None:
+        return stream.cuda_stream
     import torch
-    return (torch.cuda.current_stream(cache.device) if stream is None else stream).cuda_stream
+    # the raw handle: a step has several calls of a few microseconds, and a Stream object costs two
+    return torch._C._cuda_getCurrentRawStream(cache.device.index or 0)
 
 
-def _rows(t, name: str, n_rows: int, heads, hd: int):
-    """`t` holds bf16 rows [n_rows or more, heads, hd], elements of a head side by side."""
+def _rows(t, name: str, step: Kv8Step, cache: Kv8Cache, heads):
+    """Strides of bf16 rows [n_rows or more, heads, head_dim], elements of a head side by side."""
     import torch
-    _want(t.dtype == torch.bfloat16 and t.dim() == 3 and t.shape[0] >= n_rows and t.shape[2] == hd
-          and (heads is None or t.shape[1] == heads) and t.stride(2) == 1,
-          f"{name} must be a bf16 tensor [{n_rows} or more, {'heads' if heads is None else heads}, {hd}] with the last dimension contiguous")
-    return t
+    shape, stride = t.shape, t.stride()
+    if (t.dtype != torch.bfloat16 or len(shape) != 3 or shape[0] < step.n_rows or shape[2] != cache.head_dim
+            or (heads is not None and shape[1] != heads) or stride[2] != 1):
+        _refuse(f"{name} must be a bf16 tensor [{step.n_rows} or more, {'heads' if heads is None else heads}, {cache.head_dim}] "
+                "with the last dimension contiguous")
+    return stride
 
 
 def _own(workspace, stream):
@@ -135,14 +140,19 @@ def _own(workspace, stream):
     return workspace
 
 
+def _same_sequences(cache: Kv8Cache, step: Kv8Step):
+    if step.n_seq != cache.n_seq:
+        _refuse("the step is for another number of sequences")
+
+
 def append(cache: Kv8Cache, step: Kv8Step, k_new, v_new, stream=None):
     """Quantises k_new and v_new [n_rows, n_kv_heads, head_dim] (bf16, the same strides) into the cache."""
-    _want(step.n_seq == cache.n_seq, "the step is for another number of sequences")
-    for t, name in ((k_new, "k_new"), (v_new, "v_new")):
-        _rows(t, name, step.n_rows, cache.n_kv_heads, cache.head_dim)
-    _want(k_new.stride() == v_new.stride(), "k_new and v_new must have the same strides")
+    _same_sequences(cache, step)
+    stride = _rows(k_new, "k_new", step, cache, cache.n_kv_heads)
+    if _rows(v_new, "v_new", step, cache, cache.n_kv_heads) != stride:
+        _refuse("k_new and v_new must have the same strides")
     _check(load_library().moe_kv8_append(_stream(cache, stream), cache.ref, step.ref, k_new.data_ptr(), v_new.data_ptr(),
-                                         k_new.stride(0), k_new.stride(1)))
+                                         stride[0], stride[1]))
 
 
 def attend_workspace_bytes(cache: Kv8Cache, step: Kv8Step, n_q_heads: int, with_weights: bool) -> int:
@@ -160,17 +170,17 @@ def attend(cache: Kv8Cache, step: Kv8Step, q, out, weight_in=None, weight_out=No
            stream=None):
     """Attention of q [n_rows, n_q_heads, head_dim] over the cache into `out`, after the append of the same step."""
     import torch
-    _want(step.n_seq == cache.n_seq, "the step is for another number of sequences")
-    _rows(q, "q", step.n_rows, None, cache.head_dim)
-    _rows(out, "out", step.n_rows, q.shape[1], cache.head_dim)
+    _same_sequences(cache, step)
+    heads = q.shape[1] if q.dim() == 3 else None
+    qs, os = _rows(q, "q", step, cache, None), _rows(out, "out", step, cache, heads)
     for t, name in ((weight_in, "weight_in"), (weight_out, "weight_out")):
         if t is not None:
-            _whole(t, name, torch.float32, cache.k.shape[:3])
+            _whole(t, name, torch.float32, cache.slots)
     if workspace is None:
-        workspace = _own(attend_workspace(cache, step, q.shape[1], weight_out is not None), stream)
+        workspace = _own(attend_workspace(cache, step, heads, weight_out is not None), stream)
     _check(load_library().moe_kv8_attend(
-        _stream(cache, stream), cache.ref, step.ref, q.shape[1], q.data_ptr(), q.stride(0), q.stride(1), softmax_scale,
-        out.data_ptr(), out.stride(0), out.stride(1), _ptr(weight_in), _ptr(weight_out), workspace.data_ptr(), workspace.numel()))
+        _stream(cache, stream), cache.ref, step.ref, heads, q.data_ptr(), qs[0], qs[1], softmax_scale,
+        out.data_ptr(), os[0], os[1], _ptr(weight_in), _ptr(weight_out), workspace.data_ptr(), workspace.numel()))
     return out
 
 
@@ -191,11 +201,11 @@ def evict(cache: Kv8Cache, held, max_held: int, keep: int, recent: int, next_pos
     if next_position is not None:
         _whole(next_position, "next_position", torch.int32, (cache.n_seq,))
     for t, name in ((weight_in, "weight_in"), (weight_out, "weight_out")):
-        _whole(t, name, torch.float32, cache.k.shape[:3])
+        _whole(t, name, torch.float32, cache.slots)
     if position_out is not None:
-        _whole(position_out, "position_out", torch.int32, cache.k.shape[:3])
+        _whole(position_out, "position_out", torch.int32, cache.slots)
     if kept is not None:
-        _whole(kept, "kept", torch.int32, cache.k.shape[:2] + (keep,))
+        _whole(kept, "kept", torch.int32, cache.slots[:2] + (keep,))
     if workspace is None:
         workspace = _own(evict_workspace(cache, keep), stream)
     _check(load_library().moe_kv8_evict(

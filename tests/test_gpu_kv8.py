@@ -350,6 +350,11 @@ EVICTS = [
     (32, 64, 1, [257], 32, 7, "nan"),
     (16, 64, 2, [70], 64, 3, "zeros"),
     (64, 128, 1, [5000], 2048, 256, "random"),
+    (16, 32, 1, [1024, 1, 1025], 1008, 1, "random"),              # around what a wavefront takes
+    (128, 32, 2, [4097, 4095], 3968, 100, "ties"),
+    (128, 32, 1, [16384, 9000], 16256, 8000, "random"),
+    (128, 32, 1, [20000, 70], 128, 0, "ties"),                    # longer than the lanes hold
+    (128, 32, 2, [17000], 16896, 3, "random"),
 ]
 
 
