@@ -27,6 +27,7 @@
 #define KLOTSKI_MOE_ATTN_H
 
 #include "moe.h"
+#include "moe_kv8.h"
 
 #ifdef __cplusplus
 extern "C" {
@@ -128,6 +129,22 @@ moe_status moe_attn_forward_group(moe_attn_ctx* ctx, int32_t layer, int32_t n_ba
  * device-resident caches.  Errors as for a batch of moe_attn_forward_group.
  */
 moe_status moe_attn_prefetch(moe_attn_ctx* ctx, const moe_attn_batch* first);
+
+/*
+ * moe_attn_forward_kv8 -- the layer over a cache held in 8 bits (moe_kv8.h), for the new tokens of `step`: one or many per
+ * sequence, sequences of different lengths, prompts and decoding alike.  Normalisation, projections and rotation (by
+ * step->next_position, null: cached, plus the token's place) as above; the new k and v (rounded to bf16) go through
+ * moe_kv8_append, q (rounded to bf16) through moe_kv8_attend, then the output projection and the residual.
+ *   cache: n_kv_heads and head_dim of the context; step->n_rows at most max(max_seqs, max_group_seqs).
+ *   h_in, h_out: device, bf16 [n_rows, d_model]; h_out may be h_in.  Rows of no sequence are left as they were.
+ *   weight_in, weight_out, workspace: as for moe_kv8_attend (moe_kv8_attend_workspace_bytes with the context's n_q_heads).
+ * Runs on the compute stream, whose order it follows; everything is on the device, so the call is a plain run of kernels
+ * that can be captured.  Not profiled.  Errors: as moe_kv8_append and moe_kv8_attend, found before anything is
+ * launched; MOE_ERR_STATE (the layer has no weights).
+ */
+moe_status moe_attn_forward_kv8(moe_attn_ctx* ctx, int32_t layer, const moe_kv8_cache* cache, const moe_kv8_step* step,
+                                const void* h_in, void* h_out, const float* weight_in, float* weight_out,
+                                void* workspace, int64_t workspace_bytes);
 
 /* Profiling: when on (1..64), every forward_group call times its streams with events and
  * synchronises.  With on = n > 1 each kernel but the last (the residual, which may work in place)

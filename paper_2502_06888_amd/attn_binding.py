@@ -10,10 +10,11 @@ from dataclasses import dataclass
 from typing import Sequence
 
 from . import binding as B
+from . import kv8_binding as Q
 
 ATTN_EXPORTS = ["moe_attn_workspace_bytes", "moe_attn_create", "moe_attn_destroy",
                 "moe_attn_set_weights", "moe_attn_forward_group", "moe_attn_set_profiling",
-                "moe_attn_get_profile", "moe_attn_last_error", "moe_attn_prefetch"]
+                "moe_attn_get_profile", "moe_attn_last_error", "moe_attn_prefetch", "moe_attn_forward_kv8"]
 
 
 class MoeAttnConfig(C.Structure):
@@ -52,6 +53,7 @@ def load_library():
         lib.moe_attn_set_weights.argtypes = [vp, i32] + [vp] * 5 + [i32]
         lib.moe_attn_forward_group.argtypes = [vp, i32, i32, P(MoeAttnBatch)]
         lib.moe_attn_prefetch.argtypes = [vp, P(MoeAttnBatch)]
+        lib.moe_attn_forward_kv8.argtypes = [vp, i32, P(Q.MoeKv8Cache), P(Q.MoeKv8Step)] + [vp] * 5 + [i64]
         lib.moe_attn_set_profiling.argtypes = [vp, i32]
         lib.moe_attn_get_profile.argtypes = [vp, P(MoeAttnProfile)]
         lib.moe_attn_last_error.argtypes = [vp]
@@ -123,6 +125,23 @@ class AttnContext:
         for i, b in enumerate(batches):
             arr[i] = self._marshal(b)
         _check(self.lib.moe_attn_forward_group(self.h, layer, len(batches), arr), self.h)
+
+    def kv8_workspace(self, cache: Q.Kv8Cache, step: Q.Kv8Step, with_weights: bool):
+        """Workspace of forward_kv8 for steps of these bounds."""
+        return Q.attend_workspace(cache, step, self.cfg.n_q_heads, with_weights)
+
+    def forward_kv8(self, cache: Q.Kv8Cache, step: Q.Kv8Step, h_in, h_out, workspace, layer: int = 0, weight_in=None,
+                    weight_out=None):
+        """The layer over an 8-bit cache for the new tokens of `step`, on the compute stream."""
+        import torch
+        Q._same_sequences(cache, step)
+        for t, name in ((h_in, "h_in"), (h_out, "h_out")):
+            Q._whole(t, name, torch.bfloat16, (step.n_rows, self.cfg.d_model))
+        for t, name in ((weight_in, "weight_in"), (weight_out, "weight_out")):
+            if t is not None:
+                Q._whole(t, name, torch.float32, cache.slots)
+        _check(self.lib.moe_attn_forward_kv8(self.h, layer, cache.ref, step.ref, h_in.data_ptr(), h_out.data_ptr(),
+                                             Q._ptr(weight_in), Q._ptr(weight_out), workspace.data_ptr(), workspace.numel()), self.h)
 
     def set_profiling(self, level: int):
         """0 off; n >= 1 on, kernels repeated n times between their events."""

@@ -518,4 +518,67 @@ moe_status moe_attn_forward_group(moe_attn_ctx* ctx, int32_t layer, int32_t n_ba
     return MOE_OK;
 }
 
+moe_status moe_attn_forward_kv8(moe_attn_ctx* ctx, int32_t layer, const moe_kv8_cache* cache, const moe_kv8_step* step,
+                                const void* h_in, void* h_out, const float* weight_in, float* weight_out,
+                                void* workspace, int64_t workspace_bytes) {
+    if (!ctx) return fail(nullptr, MOE_ERR_INVALID_ARG, "ctx is null");
+    if (!cache || !step) return fail(ctx, MOE_ERR_INVALID_ARG, "null argument");
+    const moe_attn_config& c = ctx->cfg;
+    if (layer < 0 || layer >= c.n_layers) return fail(ctx, MOE_ERR_INVALID_ARG, "layer %d outside 0..%d", layer, c.n_layers - 1);
+    if (!ctx->has_weights[layer]) return fail(ctx, MOE_ERR_STATE, "moe_attn_set_weights has not been called for layer %d", layer);
+    if (cache->n_kv_heads != c.n_kv_heads || cache->head_dim != c.head_dim)
+        return fail(ctx, MOE_ERR_SHAPE, "cache of %d heads of %d, context of %d heads of %d", cache->n_kv_heads, cache->head_dim, c.n_kv_heads, c.head_dim);
+    const int cap = c.max_group_seqs > c.max_seqs ? c.max_group_seqs : c.max_seqs;
+    if (step->n_rows > cap) return fail(ctx, MOE_ERR_SHAPE, "%d rows, the context has room for %d", step->n_rows, cap);
+    uint8_t* w = ctx->ws;
+    moe_status cs = kkv8::check_layer_call(cache, step, c.n_q_heads, w + ctx->o_q, weight_in, weight_out, workspace, workspace_bytes);
+    if (cs != MOE_OK) return fail(ctx, cs, "%s", moe_kv8_last_error());
+    const size_t d = c.d_model, hd = c.head_dim, dkv = (size_t)c.n_kv_heads * hd, dq = (size_t)c.n_q_heads * hd;
+    const int rows = step->n_rows;
+    // q, k and the attention's output share the buffer of the fp32 queries (two halves), v the one of the attention output
+    uint16_t* q = (uint16_t*)(w + ctx->o_q);
+    uint16_t* k = q + (size_t)ctx->rows_alloc * dq;
+    uint16_t* v = (uint16_t*)(w + ctx->o_ao);
+    uint16_t* o = k;  // the new keys are in the cache by then
+    if (rows == 0) {
+        cs = moe_kv8_attend(ctx->compute, cache, step, c.n_q_heads, q, dq, hd, 0.f, o, dq, hd, weight_in, weight_out, workspace, workspace_bytes);
+        return cs == MOE_OK ? MOE_OK : fail(ctx, cs, "%s", moe_kv8_last_error());
+    }
+    if (!h_in || !h_out) return fail(ctx, MOE_ERR_INVALID_ARG, "null pointer");
+    if (((uintptr_t)h_in & 15u) != 0 || ((uintptr_t)h_out & 15u) != 0 || pointer_kind(h_in) != 2 || pointer_kind(h_out) != 2)
+        return fail(ctx, MOE_ERR_INVALID_ARG, "hidden-state pointers are not 16-byte aligned device memory");
+    hipStream_t st = ctx->compute;
+    const kkv8::Cache kc = kkv8::cache_of_call(cache);
+    const kkv8::Step ks = kkv8::step_of_call(step);
+    const size_t lo = (size_t)layer * ctx->layer_stride;
+    const int nrb = (rows + kRowBlk - 1) / kRowBlk, rows_pad = ((rows + 127) / 128) * 128, n_qkv = (int)(dq + 2 * dkv);
+    auto splits_for = [&](int K, int n_out) {
+        int sp = pick_splits(nrb, K, n_out);
+        while (sp > 1 && sp * rows_pad > ctx->part_rows) sp /= 2;
+        return sp;
+    };
+    const int64_t stride = (int64_t)rows_pad * (int64_t)ctx->widest;
+    float* part = (float*)(w + ctx->o_part);
+    GroupTab tab{};
+    tab.n = 1;
+    tab.row0[1] = rows;
+    tab.h_in[0] = h_in;
+    tab.h_out[0] = h_out;
+    launch_rmsnorm(st, tab, w + lo + ctx->o_g, (int)d, c.rms_eps, w + ctx->o_ax);
+    const int sp1 = splits_for((int)d, n_qkv);
+    launch_proj(st, w + ctx->o_ax, w + lo + ctx->o_wqkv, nrb, (int)d, n_qkv, sp1, part, stride);
+    launch_qkv_rows(st, part, sp1, stride, ctx->dm, kc, ks, (const double*)(w + ctx->o_freq), q, k, v);
+    HIP_TRY(ctx, hipGetLastError());
+    cs = moe_kv8_append(st, cache, step, k, v, (int64_t)dkv, (int64_t)hd);
+    if (cs == MOE_OK)
+        cs = moe_kv8_attend(st, cache, step, c.n_q_heads, q, (int64_t)dq, (int64_t)hd, 0.f, o, (int64_t)dq, (int64_t)hd, weight_in, weight_out, workspace, workspace_bytes);
+    if (cs != MOE_OK) return fail(ctx, cs, "%s", moe_kv8_last_error());
+    launch_pack_weight(st, o, nrb * kRowBlk, (int)dq, w + ctx->o_ao);
+    const int sp2 = splits_for((int)dq, (int)d);
+    launch_proj(st, w + ctx->o_ao, w + lo + ctx->o_wo, nrb, (int)dq, (int)d, sp2, part, stride);
+    launch_out_rows(st, part, sp2, stride, (int)d, kc, ks, h_in, h_out);
+    HIP_TRY(ctx, hipGetLastError());
+    return MOE_OK;
+}
+
 }  // extern "C"

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "kv8_kernels.h"
+
 namespace kattn {
 
 constexpr int kRowBlk = 32;   // rows (sequences) per MFMA block
@@ -68,5 +70,12 @@ int launch_attention(hipStream_t st, const float* q, const Dims& dm, const Group
 // y = x + sum of the split-K partials of the output projection, one rounding to bf16.
 void launch_out_finish(hipStream_t st, const float* part, int splits, int64_t split_stride,
                        const GroupTab& tab, int d);
+
+// The same two ends of the layer for the rows of a step over an 8-bit cache.  q, k and v: bf16 [rows, heads * hd], rotated to
+// the tokens' positions; rows of no sequence are not written, there as in h_out.
+void launch_qkv_rows(hipStream_t st, const float* part, int splits, int64_t split_stride, const Dims& dm, const kkv8::Cache& c,
+                     const kkv8::Step& s, const double* inv_freq, uint16_t* q, uint16_t* k, uint16_t* v);
+void launch_out_rows(hipStream_t st, const float* part, int splits, int64_t split_stride, int d, const kkv8::Cache& c,
+                     const kkv8::Step& s, const void* h_in, void* h_out);
 
 }  // namespace kattn

@@ -578,6 +578,64 @@ __global__ __launch_bounds__(256) void out_finish_kernel(const float* __restrict
     ((u32x4*)tab.h_out[bt])[at] = o;
 }
 
+// One thread per rotated pair of a head of q or k, or per two elements of v, of one row of a step.
+__global__ __launch_bounds__(256) void qkv_rows_kernel(const float* __restrict__ part, int splits, int64_t split_stride,
+                                                       Dims dm, kkv8::Cache c, kkv8::Step s,
+                                                       const double* __restrict__ inv_freq, uint16_t* __restrict__ q,
+                                                       uint16_t* __restrict__ k, uint16_t* __restrict__ v) {
+    const int row = blockIdx.x, hd = dm.hd, half = hd / 2;
+    const int dq = dm.Hq * hd, dkv = dm.Hkv * hd, n_out = dq + 2 * dkv;
+    const int i = blockIdx.y * 256 + threadIdx.x;
+    if (i >= n_out / 2) return;
+    int token;
+    kkv8::Seq of;
+    const int seq = kkv8::seq_of_row(c, s, row, &token, &of);
+    if (seq < 0) return;
+    const int h = i / half, j = i % half;  // heads of q, then k, then v
+    const float* p = part + (size_t)row * n_out + (size_t)h * hd + j;
+    float a = 0.f, b = 0.f;
+    for (int sp = 0; sp < splits; ++sp) {
+        a += p[(size_t)sp * split_stride];
+        b += p[(size_t)sp * split_stride + half];
+    }
+    if (h < dm.Hq + dm.Hkv) {
+        // angle reduced to [-pi, pi] in double, sine and cosine of the remainder in single
+        const double pos = (double)(s.next_position != nullptr ? s.next_position[seq] : of.cached) + token;
+        const double ang = pos * inv_freq[j];
+        const double turns = rint(ang * 0.15915494309189535);
+        float sn, cs;
+        sincosf((float)(ang - turns * 6.283185307179586), &sn, &cs);
+        const float r0 = a * cs - b * sn, r1 = b * cs + a * sn;
+        a = r0;
+        b = r1;
+    }
+    uint16_t* to = h < dm.Hq ? q + (size_t)row * dq + (size_t)h * hd
+                 : h < dm.Hq + dm.Hkv ? k + (size_t)row * dkv + (size_t)(h - dm.Hq) * hd
+                                      : v + (size_t)row * dkv + (size_t)(h - dm.Hq - dm.Hkv) * hd;
+    to[j] = (uint16_t)bf_bits(a);
+    to[j + half] = (uint16_t)bf_bits(b);
+}
+
+// y = x + sum of the partials, 8 elements per thread, for the rows of a step that belong to a sequence.
+__global__ __launch_bounds__(256) void out_rows_kernel(const float* __restrict__ part, int splits, int64_t split_stride, int d,
+                                                       kkv8::Cache c, kkv8::Step s, const u32x4* h_in, u32x4* h_out) {
+    const int i = blockIdx.y * 256 + threadIdx.x, row = blockIdx.x;
+    if (i >= d / 8) return;
+    int token;
+    kkv8::Seq of;
+    if (kkv8::seq_of_row(c, s, row, &token, &of) < 0) return;
+    const size_t at = (size_t)row * (d / 8) + i;
+    float f[8];
+    widen8(h_in[at], f);
+    for (int sp = 0; sp < splits; ++sp) {
+        const float4* p = reinterpret_cast<const float4*>(part + (size_t)sp * split_stride + at * 8);
+        const float4 a = p[0], b = p[1];
+        f[0] += a.x; f[1] += a.y; f[2] += a.z; f[3] += a.w;
+        f[4] += b.x; f[5] += b.y; f[6] += b.z; f[7] += b.w;
+    }
+    h_out[at] = u32x4{pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])};
+}
+
 }  // namespace
 
 void launch_pack_weight(hipStream_t st, const void* w, int rows, int K, void* out) {
@@ -683,6 +741,18 @@ int launch_attention(hipStream_t st, const float* q, const Dims& dm, const Group
         case 128: return launch_attention_hd<128>(st, q, dm, tab, scratch, max_ranges, o_frag);
     }
     return -1;
+}
+
+void launch_qkv_rows(hipStream_t st, const float* part, int splits, int64_t split_stride, const Dims& dm, const kkv8::Cache& c,
+                     const kkv8::Step& s, const double* inv_freq, uint16_t* q, uint16_t* k, uint16_t* v) {
+    const int pairs = (dm.Hq + 2 * dm.Hkv) * dm.hd / 2;
+    hipLaunchKernelGGL(qkv_rows_kernel, dim3(s.n_rows, (pairs + 255) / 256), dim3(256), 0, st, part, splits, split_stride, dm, c, s, inv_freq, q, k, v);
+}
+
+void launch_out_rows(hipStream_t st, const float* part, int splits, int64_t split_stride, int d, const kkv8::Cache& c,
+                     const kkv8::Step& s, const void* h_in, void* h_out) {
+    hipLaunchKernelGGL(out_rows_kernel, dim3(s.n_rows, (d / 8 + 255) / 256), dim3(256), 0, st, part, splits, split_stride, d, c, s,
+                       (const u32x4*)h_in, (u32x4*)h_out);
 }
 
 void launch_out_finish(hipStream_t st, const float* part, int splits, int64_t split_stride,

@@ -858,6 +858,13 @@ void launch_hd(hipStream_t st, const Cache& c, const Step& s, const Attend& a, c
 
 }  // namespace
 
+bool attend_fits(const Cache& c, const Step& s, int Hq) {
+    const Plan p = plan(c, s, Hq, true);
+    const int64_t pairs = (int64_t)c.n_seq * c.Hkv;
+    const int64_t most = pairs * p.sp.ranges * (p.tiles > 0 ? 1 : p.row_tiles);
+    return most <= 0x7fffffff && pairs * p.sp.tile_rows <= (int64_t)0x7fffffff * 4;
+}
+
 int64_t attend_workspace(const Cache& c, const Step& s, int Hq, bool weights) { return plan(c, s, Hq, weights).bytes; }
 
 void launch_attend(hipStream_t st, const Cache& c, const Step& s, const Attend& a) {

@@ -137,50 +137,27 @@ Cache cache_of(const moe_kv8_cache* c) {
 
 Step step_of(const moe_kv8_step* s) { return Step{s->n_rows, s->max_new, s->max_cached, s->row_offsets, s->cached, s->next_position}; }
 
-moe_status launched() {
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? MOE_OK : fail(MOE_ERR_HIP, "launch failed: %s", hipGetErrorString(e));
-}
-
-}  // namespace
-
-extern "C" {
-
-const char* moe_kv8_last_error(void) { return g_error; }
-
-moe_status moe_kv8_append(void* stream, const moe_kv8_cache* cache, const moe_kv8_step* step, const void* k_new,
-                          const void* v_new, int64_t row_stride, int64_t head_stride) {
+// Everything that moe_kv8_append refuses; *device: where the tensors are.
+moe_status check_append(const moe_kv8_cache* cache, const moe_kv8_step* step, const void* k_new, const void* v_new,
+                        int64_t row_stride, int64_t head_stride, int* device) {
     TRY(check_sizes(cache));
     TRY(check_step_sizes(cache, step));
     Where w;
     TRY(check_cache(cache, &w));
     TRY(check_step(step, &w));
+    *device = w.device;
     if (step->n_rows == 0) return MOE_OK;
     TRY(check_rows(k_new, "k_new", row_stride, head_stride, &w));
     TRY(check_rows(v_new, "v_new", row_stride, head_stride, &w));
     const int64_t blocks = (step->max_new + cache->block - 2) / cache->block + 1;
     if ((int64_t)cache->n_seq * cache->n_kv_heads * 2 * blocks > 0x7fffffff) return fail(MOE_ERR_SHAPE, "too many blocks: bring fewer sequences or tokens at once");
-    OnDevice on(w.device);
-    if (on.failed()) return fail(MOE_ERR_HIP, "device %d cannot be made current", w.device);
-    launch_append((hipStream_t)stream, cache_of(cache), step_of(step), Rows{(const uint16_t*)k_new, row_stride, head_stride},
-                  Rows{(const uint16_t*)v_new, row_stride, head_stride});
-    return launched();
-}
-
-moe_status moe_kv8_attend_workspace_bytes(const moe_kv8_cache* cache, const moe_kv8_step* step, int32_t n_q_heads,
-                                          int32_t with_weights, int64_t* bytes_out) {
-    if (!bytes_out) return fail(MOE_ERR_INVALID_ARG, "bytes_out is null");
-    TRY(check_sizes(cache));
-    TRY(check_step_sizes(cache, step));
-    TRY(check_heads(cache, n_q_heads));
-    *bytes_out = attend_workspace(cache_of(cache), step_of(step), n_q_heads, with_weights != 0);
     return MOE_OK;
 }
 
-moe_status moe_kv8_attend(void* stream, const moe_kv8_cache* cache, const moe_kv8_step* step, int32_t n_q_heads,
-                          const void* q, int64_t q_row_stride, int64_t q_head_stride, float softmax_scale, void* out,
-                          int64_t out_row_stride, int64_t out_head_stride, const float* weight_in,
-                          float* weight_out, void* workspace, int64_t workspace_bytes) {
+moe_status check_attend(const moe_kv8_cache* cache, const moe_kv8_step* step, int32_t n_q_heads, const void* q,
+                        int64_t q_row_stride, int64_t q_head_stride, float softmax_scale, const void* out,
+                        int64_t out_row_stride, int64_t out_head_stride, const float* weight_in, const float* weight_out,
+                        const void* workspace, int64_t workspace_bytes, int* device) {
     TRY(check_sizes(cache));
     TRY(check_step_sizes(cache, step));
     TRY(check_heads(cache, n_q_heads));
@@ -188,6 +165,7 @@ moe_status moe_kv8_attend(void* stream, const moe_kv8_cache* cache, const moe_kv
     Where w;
     TRY(check_cache(cache, &w));
     TRY(check_step(step, &w));
+    *device = w.device;
     if (step->n_rows > 0) {
         TRY(check_rows(q, "q", q_row_stride, q_head_stride, &w));
         TRY(check_rows(out, "out", out_row_stride, out_head_stride, &w));
@@ -199,10 +177,71 @@ moe_status moe_kv8_attend(void* stream, const moe_kv8_cache* cache, const moe_kv
     if (weight_in && weight_in != weight_out) TRY(w.on(weight_in, "weight_in", 4));
     const Cache c = cache_of(cache);
     const Step s = step_of(step);
-    TRY(check_workspace(workspace, workspace_bytes, attend_workspace(c, s, n_q_heads, weight_out != nullptr), &w));
+    if (!attend_fits(c, s, n_q_heads)) return fail(MOE_ERR_SHAPE, "too many workgroups: bring fewer sequences or tokens at once");
+    return check_workspace(workspace, workspace_bytes, attend_workspace(c, s, n_q_heads, weight_out != nullptr), &w);
+}
+
+moe_status launched() {
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? MOE_OK : fail(MOE_ERR_HIP, "launch failed: %s", hipGetErrorString(e));
+}
+
+}  // namespace
+
+namespace kkv8 {
+
+moe_status check_layer_call(const moe_kv8_cache* cache, const moe_kv8_step* step, int n_q_heads, const void* rows,
+                            const float* weight_in, const float* weight_out, const void* workspace, int64_t workspace_bytes) {
+    int device = 0;
+    TRY(check_append(cache, step, rows, rows, 8, 8, &device));
+    return check_attend(cache, step, n_q_heads, rows, 8, 8, 0.f, (const uint8_t*)rows + 16, 8, 8, weight_in, weight_out, workspace,
+                        workspace_bytes, &device);
+}
+
+Cache cache_of_call(const moe_kv8_cache* c) { return cache_of(c); }
+Step step_of_call(const moe_kv8_step* s) { return step_of(s); }
+
+}  // namespace kkv8
+
+extern "C" {
+
+const char* moe_kv8_last_error(void) { return g_error; }
+
+moe_status moe_kv8_append(void* stream, const moe_kv8_cache* cache, const moe_kv8_step* step, const void* k_new,
+                          const void* v_new, int64_t row_stride, int64_t head_stride) {
+    int device = 0;
+    TRY(check_append(cache, step, k_new, v_new, row_stride, head_stride, &device));
+    if (step->n_rows == 0) return MOE_OK;
+    OnDevice on(device);
+    if (on.failed()) return fail(MOE_ERR_HIP, "device %d cannot be made current", device);
+    launch_append((hipStream_t)stream, cache_of(cache), step_of(step), Rows{(const uint16_t*)k_new, row_stride, head_stride},
+                  Rows{(const uint16_t*)v_new, row_stride, head_stride});
+    return launched();
+}
+
+moe_status moe_kv8_attend_workspace_bytes(const moe_kv8_cache* cache, const moe_kv8_step* step, int32_t n_q_heads,
+                                          int32_t with_weights, int64_t* bytes_out) {
+    if (!bytes_out) return fail(MOE_ERR_INVALID_ARG, "bytes_out is null");
+    TRY(check_sizes(cache));
+    TRY(check_step_sizes(cache, step));
+    TRY(check_heads(cache, n_q_heads));
+    if (!attend_fits(cache_of(cache), step_of(step), n_q_heads)) return fail(MOE_ERR_SHAPE, "too many workgroups: bring fewer sequences or tokens at once");
+    *bytes_out = attend_workspace(cache_of(cache), step_of(step), n_q_heads, with_weights != 0);
+    return MOE_OK;
+}
+
+moe_status moe_kv8_attend(void* stream, const moe_kv8_cache* cache, const moe_kv8_step* step, int32_t n_q_heads,
+                          const void* q, int64_t q_row_stride, int64_t q_head_stride, float softmax_scale, void* out,
+                          int64_t out_row_stride, int64_t out_head_stride, const float* weight_in,
+                          float* weight_out, void* workspace, int64_t workspace_bytes) {
+    int device = 0;
+    TRY(check_attend(cache, step, n_q_heads, q, q_row_stride, q_head_stride, softmax_scale, out, out_row_stride,
+                     out_head_stride, weight_in, weight_out, workspace, workspace_bytes, &device));
     if (step->n_rows == 0 && !weight_out) return MOE_OK;
-    OnDevice on(w.device);
-    if (on.failed()) return fail(MOE_ERR_HIP, "device %d cannot be made current", w.device);
+    OnDevice on(device);
+    if (on.failed()) return fail(MOE_ERR_HIP, "device %d cannot be made current", device);
+    const Cache c = cache_of(cache);
+    const Step s = step_of(step);
     Attend a{};
     a.Hq = n_q_heads;
     a.qscale = (float)(1.4426950408889634 * (softmax_scale == 0.f ? 1.0 / std::sqrt((double)c.hd) : (double)softmax_scale));

@@ -43,12 +43,21 @@ struct Attend {
 };
 
 void launch_append(hipStream_t st, const Cache& c, const Step& s, const Rows& k, const Rows& v);
+// Whether the grids of launch_attend stay within what a launch can have.
+bool attend_fits(const Cache& c, const Step& s, int Hq);
 int64_t attend_workspace(const Cache& c, const Step& s, int Hq, bool weights);
 void launch_attend(hipStream_t st, const Cache& c, const Step& s, const Attend& a);
 int64_t evict_workspace(const Cache& c, int keep);
 void launch_evict(hipStream_t st, const Cache& c, const int32_t* held, int max_held, int keep, int recent,
                   const int32_t* next_position, const float* weight_in, float* weight_out, int32_t* position_out,
                   int32_t* kept, uint8_t* ws);
+
+// For the attention layer, whose rows lie in its own workspace: what moe_kv8_append and moe_kv8_attend would refuse (with
+// the text in moe_kv8_last_error), and the kernels' views of the caller's structs.
+moe_status check_layer_call(const moe_kv8_cache* cache, const moe_kv8_step* step, int n_q_heads, const void* rows,
+                            const float* weight_in, const float* weight_out, const void* workspace, int64_t workspace_bytes);
+Cache cache_of_call(const moe_kv8_cache* c);
+Step step_of_call(const moe_kv8_step* s);
 
 // ---- device helpers shared by the kernels -------------------------------------------------------
 
@@ -75,6 +84,24 @@ __device__ __forceinline__ Seq sequence(const Cache& c, const Step& s, int seq) 
     q.cached = clampi(s.cached[seq], 0, s.max_cached);
     q.n_new = min(q.n_new, c.max_len - q.cached);
     return q;
+}
+
+// Sequence whose rows include `row`, and the token's place in it; -1 where there is none.
+__device__ __forceinline__ int seq_of_row(const Cache& c, const Step& s, int row, int* token, Seq* q) {
+    int lo = 0;
+    if (s.row_offsets == nullptr) {
+        lo = row / s.max_new;
+    } else {
+        int hi = c.n_seq - 1;  // last sequence whose rows begin at or before `row`
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (s.row_offsets[mid] <= row) lo = mid;
+            else hi = mid - 1;
+        }
+    }
+    *q = sequence(c, s, lo);
+    *token = row - q->row0;
+    return *token >= 0 && *token < q->n_new ? lo : -1;
 }
 
 // Two codes (bytes 0, 1 or 2, 3 of w) as bf16 times a power of two: exact.
