@@ -482,7 +482,14 @@ __global__ __launch_bounds__(256) void pack_kernel(Cache c, Step s, u32x4* packe
 __device__ __forceinline__ void copy_to_lds(const void* from, uint32_t to) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
 }
-__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void copy_word_to_lds(const void* from, uint32_t to) {  // 4 bytes per lane, to `to` + 4 * lane
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
+}
+// Until at most N of the wavefront's copies (and other accesses) are on their way.
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
+}
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ f32x16 mfma32(const u32x4 a, const u32x4 b, const f32x16 c) {
@@ -555,7 +562,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
     for (int f = 0; f < HD / 16; ++f) asm volatile("" : "+v"(qf[f]));
     int buf = 0;
     for (int j0 = first; j0 < end; j0 += kSlots, buf ^= 1) {
-        if (PACKED) wait_copies();
+        if (PACKED) wait_copies<0>();
         __syncthreads();  // the tile is there, and nobody reads the other buffer any more
         if (j0 + kSlots < end) {
             if (PACKED) {
@@ -663,111 +670,113 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
     }
 }
 
-// The weights of 256 slots (64 per wavefront, K in registers) from all rows that see them: S^T again, then
+// The weights of 128 slots (32 per wavefront, K in registers) from all rows that see them: S^T again, then
 // exp2(score - reference) / sum with the row's statistics, which are the lane's; added up over the rows in the lane, over
-// the lanes at the end.  32 rows of q at a time go through LDS, shared by the wavefronts.
+// the lanes at the end.  32 rows of q at a time come into LDS in the order of the matrix instructions, shared by the
+// wavefronts.  Bound by the exponentials and, next to them, the matrix cores.
+constexpr int kWeightSlots = 128;
 template <int HD>
-__global__ __launch_bounds__(256, 2) void prompt_weights_kernel(Cache c, Step s, Attend a, Split sp, int chunks) {
-    constexpr int QS = HD + 8, QI = 32 * HD / 8;  // pieces of 16 bytes of a tile of q
-    __shared__ uint16_t qt[2][32 * QS];
-    __shared__ float2 ml[2][32];
+__global__ __launch_bounds__(256, 4) void prompt_weights_kernel(Cache c, Step s, Attend a, Split sp, int chunks) {
+    constexpr int F = HD / 16, U = F < 4 ? 1 : F / 4;  // units of 32 rows; units that a wavefront copies
+    constexpr int RING = 4;                            // tiles of 32 rows in LDS, RING - 1 of them on their way
+    __shared__ u32x4 qt[RING][F * 64];
+    __shared__ float2 ml[RING][32];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, grp = lane >> 5;
     const int pairs = c.n_seq * c.Hkv;
     const int pair = blockIdx.x % pairs, chunk = blockIdx.x / pairs;
     const int seq = pair / c.Hkv, hk = pair % c.Hkv, G = a.Hq / c.Hkv;
     const Seq q = sequence(c, s, seq);
     const int total = q.cached + q.n_new, rows = q.n_new * G;
-    const int w0 = chunk * 256, j0 = w0 + wave * 64;
+    const int w0 = chunk * kWeightSlots, j0 = w0 + wave * 32;
     if (w0 >= total) return;
-    const int64_t base = (int64_t)seq * c.Hkv + hk;
-    const uint8_t* K = c.codes[0] + base * c.max_len * HD;
-    const float* ks = c.scale[0] + base * (c.max_len >> c.logb);
-    u32x4 kf[2][HD / 16];
+    const int64_t base = (int64_t)pair * c.max_len;
+    u32x4 kf[F];
+    {
+        const int slot = min(j0 + col, total - 1);
+        const float sc = c.scale[0][(int64_t)pair * (c.max_len >> c.logb) + (slot >> c.logb)];
+        const uint8_t* K = c.codes[0] + (base + slot) * HD + grp * 8;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const int slot = min(j0 + t * 32 + col, total - 1);
-        const float sc = ks[slot >> c.logb];
-#pragma unroll
-        for (int f = 0; f < HD / 16; ++f) {
-            const u32x2 x = *(const u32x2*)(K + (int64_t)slot * HD + f * 16 + grp * 8);
-            kf[t][f] = widen8(x.x, x.y, sc);
+        for (int f = 0; f < F; ++f) {
+            const u32x2 x = *(const u32x2*)(K + f * 16);
+            kf[f] = widen8(x.x, x.y, sc);
         }
+#pragma unroll
+        for (int f = 0; f < F; ++f) asm volatile("" : "+v"(kf[f]));  // waited for here, not in the loop
     }
-    float w[2][16];
+    float w[16];
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) w[t][i] = 0.f;
+    for (int i = 0; i < 16; ++i) w[i] = 0.f;
     const int r_first = max(0, w0 - q.cached) * G / 32 * 32;
-    u32x4 piece[QI / 256 > 0 ? QI / 256 : 1];
-    float2 piece_ml;
-    auto load = [&](int r0) {
+    const uint32_t qt_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4*)&qt[0][0];
+    const uint32_t ml_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float2*)&ml[0][0];
+    const float* stats = (const float*)(sp.final_ml + (int64_t)pair * sp.tile_rows);
+    // U + 1 copies of every wavefront, so that it can count them (rows past the end: the last one again; where there
+    // are more wavefronts than units some copy the same, and so do all the statistics)
+    // The lane's row of q in the next tile to copy, stepped on by 32 rows; past the end the last row again.
+    const uint16_t* heads = a.q.p + (int64_t)hk * G * a.q.head + grp * 8;
+    const uint16_t* last = heads + (int64_t)(q.row0 + q.n_new - 1) * a.q.row + (int64_t)(G - 1) * a.q.head;
+    int row = r_first + col, g = row % G;
+    const uint16_t* from = heads + (int64_t)(q.row0 + row / G) * a.q.row + (int64_t)g * a.q.head;
+    const int step_g = 32 % G;
+    const int64_t step = (int64_t)(32 / G) * a.q.row + (int64_t)step_g * a.q.head, wrap = a.q.row - (int64_t)G * a.q.head;
+    // U + 1 copies of every wavefront, so that it can count them (where there are more wavefronts than units some copy
+    // the same, and so do all the statistics)
+    auto copy = [&](int at, int r0) {
+        const uint16_t* p = row < rows ? from : last;
 #pragma unroll
-        for (int i = 0; i < (QI + 255) / 256; ++i) {
-            const int at = threadIdx.x + i * 256, row = min(r0 + at / (HD / 8), rows - 1);
-            if (QI >= 256 || at < QI)
-                piece[i] = *(const u32x4*)(a.q.p + (int64_t)(q.row0 + row / G) * a.q.row + (int64_t)(hk * G + row % G) * a.q.head + at % (HD / 8) * 8);
+        for (int i = 0; i < U; ++i) {
+            const int f = (wave * U + i) % F;
+            copy_to_lds(p + f * 16, __builtin_amdgcn_readfirstlane(qt_at + (at * F + f) * 1024));
         }
-        if (threadIdx.x < 32) {
-            piece_ml = sp.final_ml[(int64_t)pair * sp.tile_rows + min(r0 + (int)threadIdx.x, rows - 1)];
-            if (r0 + (int)threadIdx.x >= rows) piece_ml.y = 0.f;
+        copy_word_to_lds(stats + min(r0 + (lane >> 1), rows - 1) * 2 + (lane & 1), __builtin_amdgcn_readfirstlane(ml_at + at * 256));
+        row += 32;
+        from += step;
+        g += step_g;
+        if (g >= G) {
+            g -= G;
+            from += wrap;
         }
     };
-    auto store = [&](int buf) {
 #pragma unroll
-        for (int i = 0; i < (QI + 255) / 256; ++i) {
-            const int at = threadIdx.x + i * 256;
-            if (QI >= 256 || at < QI) *(u32x4*)(qt[buf] + at / (HD / 8) * QS + at % (HD / 8) * 8) = piece[i];
-        }
-        if (threadIdx.x < 32) ml[buf][threadIdx.x] = piece_ml;
-    };
-    if (r_first < rows) {
-        load(r_first);
-        store(0);
-        if (r_first + 32 < rows) load(r_first + 32);
-    }
-    __syncthreads();
-    int buf = 0;
-    for (int r0 = r_first; r0 < rows; r0 += 32, buf ^= 1) {
-        if (r0 + 32 < rows) {
-            store(buf ^ 1);
-            if (r0 + 64 < rows) load(r0 + 64);
-        }
-        const int limit = q.cached + min(r0 + col, rows - 1) / G + 1;
-        const float2 e = ml[buf][col];
-        if (q.cached + min(r0 + 31, rows - 1) / G + 1 > j0) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                f32x16 z;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) z[i] = 0.f;
-                const uint16_t* p = qt[buf] + col * QS + grp * 8;
-#pragma unroll
-                for (int f = 0; f < HD / 16; ++f) z = mfma32(kf[t][f], *(const u32x4*)(p + f * 16), z);
-                const bool whole = r0 + 32 <= rows && j0 + t * 32 + 32 <= q.cached + r0 / G + 1;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], a.qscale, -e.x));
-                    if (whole) w[t][i] = __builtin_fmaf(x, e.y, w[t][i]);
-                    else w[t][i] += j0 + t * 32 + row_of(i, grp) < limit && r0 + col < rows ? x * e.y : 0.f;
-                }
-            }
-        }
+    for (int i = 0; i < RING - 1; ++i) copy(i, r_first + i * 32);
+    const int r_see = (j0 - q.cached) * G, r_whole = (j0 + 31 - q.cached) * G;  // first rows that see a slot of the wavefront, and all
+    int at = 0;
+    for (int r0 = r_first; r0 < rows; r0 += 32, at = (at + 1) % RING) {
+        wait_copies<(RING - 2) * (U + 1)>();  // all but the two youngest tiles
         __syncthreads();
-    }
+        copy((at + RING - 1) % RING, r0 + (RING - 1) * 32);  // past the end: again, so that the count stays
+        if (r0 + 31 < r_see) continue;
+        const float2 e = ml[at][col];
+        f32x16 z;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+        for (int i = 0; i < 16; ++i) z[i] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float x = w[t][i];
+        for (int f = 0; f < F; ++f) z = mfma32(kf[f], qt[at][f * 64 + lane], z);
+        if (r0 + 32 <= rows && r0 >= r_whole) {
 #pragma unroll
-            for (int m = 1; m < 32; m <<= 1) x += __shfl_xor(x, m, 64);
-            const int slot = j0 + t * 32 + row_of(i, grp);
-            if (col == i && slot < total) {
-                if (a.weight_in != nullptr && slot < q.cached) x += a.weight_in[base * c.max_len + slot];
-                a.weight_out[base * c.max_len + slot] = x;
+            for (int i = 0; i < 16; ++i)
+                w[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(z[i], a.qscale, -e.x)), e.y, w[i]);
+        } else {
+            const int within = r0 + col < rows ? q.cached + (r0 + col) / G + 1 - j0 - 4 * grp : 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], a.qscale, -e.x)) * e.y;
+                w[i] += row_of(i, 0) < within ? x : 0.f;
             }
         }
+    }
+    wait_copies<0>();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float x = w[i];
+#pragma unroll
+        for (int m = 1; m < 32; m <<= 1) x += __shfl_xor(x, m, 64);
+        const int slot = j0 + row_of(i, grp);
+        if (col == i && slot < total) {
+            if (a.weight_in != nullptr && slot < q.cached) x += a.weight_in[base + slot];
+            a.weight_out[base + slot] = x;
+        }
+    }
 }
 
 int64_t up256(int64_t v) { return (v + 255) & ~(int64_t)255; }
@@ -792,10 +801,8 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
         per = ((int64_t)most * pairs / 2048 + 127) / 128 * 128;  // 2048 workgroups
         per = per < 256 ? 256 : per;
     } else {
-        int64_t want = 512 / (pairs * p.row_tiles);  // two workgroups for each compute unit
-        want = want < 1 ? 1 : want;
-        per = (most + want * kSlots - 1) / (want * kSlots) * kSlots;
-        per = per < 512 ? 512 : per;
+        per = ((int64_t)most * pairs * p.row_tiles / 1536 + kSlots - 1) / kSlots * kSlots;  // 1536 workgroups
+        per = per < 1024 ? 1024 : per;
     }
     const int64_t ranges = most > per ? (most + per - 1) / per : 1;
     p.sp.per = (int)per;
@@ -848,7 +855,7 @@ void launch_hd(hipStream_t st, const Cache& c, const Step& s, const Attend& a, c
             hipLaunchKernelGGL(merge_kernel<HD>, dim3((unsigned)((pairs * p.sp.tile_rows + 3) / 4)), block, 0, st, c, s, a, p.sp, p.tiles > 0);
     }
     if (a.weight_out == nullptr) return;
-    const int chunks = (p.sp.score_stride + 255) / 256;
+    const int chunk = p.tiles > 0 ? 256 : kWeightSlots, chunks = (p.sp.score_stride + chunk - 1) / chunk;
     if (chunks == 0) return;
     if (p.tiles > 0)
         hipLaunchKernelGGL(weights_kernel, dim3((unsigned)(pairs * chunks)), block, 0, st, c, s, a, p.sp, chunks);
