@@ -482,6 +482,10 @@ __global__ __launch_bounds__(256) void pack_kernel(Cache c, Step s, u32x4* packe
 __device__ __forceinline__ void copy_to_lds(const void* from, uint32_t to) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
 }
+// The same from `base` (uniform) + `offset` bytes (the lane's): the addresses then cost no vector instructions.
+__device__ __forceinline__ void copy_to_lds(const void* base, uint32_t offset, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to) : "memory");
+}
 __device__ __forceinline__ void copy_word_to_lds(const void* from, uint32_t to) {  // 4 bytes per lane, to `to` + 4 * lane
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
 }
@@ -519,7 +523,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
     const int64_t base = (int64_t)seq * c.Hkv + hk;
     const uint8_t *K = c.codes[0] + base * c.max_len * HD, *V = c.codes[1] + base * c.max_len * HD;
     const float *ks = c.scale[0] + base * (c.max_len >> c.logb), *vs = c.scale[1] + base * (c.max_len >> c.logb);
-    const u32x4* packed = sp.packed + ((int64_t)pair * sp.packed_tiles + first / kSlots) * (Tile<HD>::kBytes / 16) + threadIdx.x;
+    const uint8_t* packed = (const uint8_t*)sp.packed + ((int64_t)pair * sp.packed_tiles + first / kSlots) * Tile<HD>::kBytes;
     const int32_t* odd = sp.odd + (int64_t)pair * sp.packed_tiles;
 
     const int r = row0 + wave * 32 + col;
@@ -541,11 +545,12 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
     float ref = kEmpty, sum = 0.f;
     Tile<HD> next;
     const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4*)&lds[0][0];
-    auto copy = [&](int buf) {  // the next tile, a sixteenth of 4 KB per thread and piece
+    const uint32_t wave_at = __builtin_amdgcn_readfirstlane(lds_at + wave * 1024);
+    auto copy = [&](int buf) {  // the next tile, 16 bytes per thread and piece
 #pragma unroll
         for (int i = 0; i < Tile<HD>::kPieces; ++i)
-            copy_to_lds(packed + i * 256, __builtin_amdgcn_readfirstlane(lds_at + buf * Tile<HD>::kBytes + i * 4096 + wave * 1024));
-        packed += Tile<HD>::kBytes / 16;
+            copy_to_lds(packed + i * 4096, threadIdx.x * 16, wave_at + buf * Tile<HD>::kBytes + i * 4096);
+        packed += Tile<HD>::kBytes;
     };
     if (PACKED) {
         copy(0);
