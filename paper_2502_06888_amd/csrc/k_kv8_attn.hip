@@ -18,6 +18,8 @@ constexpr float kEmpty = -1.0e30f;  // finite stand-in for "no slot seen yet"
 // the sums of 2^20 slots of any finite values stay finite.
 constexpr float kAbove = 28.f, kNear = 20.f;
 
+// The wavefront's number in its workgroup, in a scalar register.
+__device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 __device__ __forceinline__ bf16x8 as_bf16x8(const u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
 __device__ __forceinline__ f32x4 mfma16(const u32x4 a, const u32x4 b, const f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
@@ -69,7 +71,7 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
     constexpr int VW = VT >= 4 ? VT / 4 : 1;  // words of a V row that a lane holds: VT bytes
     __shared__ float sm_o[4][NT * 8][HD];
     __shared__ float2 sm_ml[4][NT * 8];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 15, grp = lane >> 4;
     const int range = blockIdx.x % sp.ranges, pair = blockIdx.x / sp.ranges;
     const int seq = pair / c.Hkv, hk = pair % c.Hkv, G = a.Hq / c.Hkv;
     const Seq q = sequence(c, s, seq);
@@ -405,23 +407,30 @@ struct Tile {
 
     // slots past `total` re-read the last one
     __device__ __forceinline__ void load(const Cache& c, const uint8_t* K, const uint8_t* V, const float* ks, const float* vs, int j0, int total) {
+        // 32-bit offsets from the uniform pointers: a cache row has at most 2^27 bytes
         if (has_k()) {
             const int slot = min(j0 + ((int)threadIdx.x & 63), total - 1);
-            const u32x4* p = (const u32x4*)(K + (int64_t)slot * HD + (threadIdx.x >> 6) * 32);
+            const u32x4* p = (const u32x4*)(K + (uint32_t)(slot * HD + ((int)threadIdx.x >> 6) * 32));
             const u32x4 a = p[0], b = p[1];
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 kr[w] = a[w];
                 kr[4 + w] = b[w];
             }
-            ksc = ks[slot >> c.logb];
+            ksc = ks[(uint32_t)(slot >> c.logb)];
         }
         if (has_v()) {
             const int quad = v_item() % (HD / 4), group = v_item() / (HD / 4);
+            if (j0 + kSlots <= total) {  // one address for the eight slots
+                const uint8_t* p = V + (uint32_t)((j0 + v_slot(group, 0)) * HD + quad * 4);
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                vr[j] = *(const uint32_t*)(V + (int64_t)min(j0 + v_slot(group, j), total - 1) * HD + quad * 4);
-            vsc = vs[min(j0 + (group >> 1) * 16, total - 1) >> c.logb];
+                for (int j = 0; j < 8; ++j) vr[j] = *(const uint32_t*)(p + (j & 3) * HD + (j >> 2) * 8 * HD);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    vr[j] = *(const uint32_t*)(V + (uint32_t)(min(j0 + v_slot(group, j), total - 1) * HD + quad * 4));
+            }
+            vsc = vs[(uint32_t)(min(j0 + (group >> 1) * 16, total - 1) >> c.logb)];
         }
     }
     // Into a tile at `to`.  Codes of V past `total` count as 0, and so do NaN ones where `part` is set (weight 0 times NaN
@@ -502,176 +511,210 @@ __device__ __forceinline__ f32x16 mfma32(const u32x4 a, const u32x4 b, const f32
 // Row of a 32x32 result that register r of a lane in half g holds.
 __device__ __forceinline__ int row_of(int r, int g) { return 8 * (r >> 2) + 4 * g + (r & 3); }
 
+// A workgroup takes `each` row tiles of its pair, one after the other (with one range): the first slots and the rows of q of
+// the next one come while the last one ends.  Tiles see the more slots the later they are, so those of a workgroup are
+// taken from both ends.
 template <int HD, bool PACKED>
-__global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend a, Split sp, int tiles) {
+__global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend a, Split sp, int groups, int each) {
     __shared__ u32x4 lds[2][Tile<HD>::kBytes / 16];
     __shared__ int nan[2];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, grp = lane >> 5;
-    // last tiles first: they see the most slots; the pairs side by side, so that the tiles of one keep to an XCD
+    const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, grp = lane >> 5;
+    // the pairs side by side, so that the tiles of one keep to an XCD
     const int pairs = c.n_seq * c.Hkv;
     const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-    const int range = rest % sp.ranges, tile = tiles - 1 - rest / sp.ranges;
+    const int range = rest % sp.ranges, group = rest / sp.ranges;
     const int seq = pair / c.Hkv, hk = pair % c.Hkv, G = a.Hq / c.Hkv;
     const Seq q = sequence(c, s, seq);
-    const int rows = q.n_new * G, row0 = tile * kRows;
-    if (row0 >= rows) return;
-    const int total = q.cached + q.n_new;
-    const int least = q.cached + row0 / G + 1;                                 // slots that the first row sees
-    const int sees = q.cached + min(row0 + kRows - 1, rows - 1) / G + 1;       // and the last one
-    const int first = range * sp.per, end = min(first + sp.per, sees);
-    if (first >= end) return;
+    const int rows = q.n_new * G, total = q.cached + q.n_new, first = range * sp.per;
+    const int row_tiles = (rows + kRows - 1) / kRows;
+    // k-th row tile of the workgroup, -1 where there is none (later ones then do not exist, either)
+    auto tile_of = [&](int k) {
+        const int i = k * groups + (k & 1 ? groups - 1 - group : group);
+        return k < each && i < row_tiles ? row_tiles - 1 - i : -1;
+    };
+    auto sees_of = [&](int tile) { return q.cached + min(tile * kRows + kRows - 1, rows - 1) / G + 1; };  // slots its last row sees
+    int tile = tile_of(0);
+    if (tile < 0 || first >= sees_of(tile)) return;
     const int64_t base = (int64_t)seq * c.Hkv + hk;
     const uint8_t *K = c.codes[0] + base * c.max_len * HD, *V = c.codes[1] + base * c.max_len * HD;
     const float *ks = c.scale[0] + base * (c.max_len >> c.logb), *vs = c.scale[1] + base * (c.max_len >> c.logb);
-    const uint8_t* packed = (const uint8_t*)sp.packed + ((int64_t)pair * sp.packed_tiles + first / kSlots) * Tile<HD>::kBytes;
+    const uint8_t* packed = (const uint8_t*)sp.packed + (int64_t)pair * sp.packed_tiles * Tile<HD>::kBytes;
     const int32_t* odd = sp.odd + (int64_t)pair * sp.packed_tiles;
 
-    const int r = row0 + wave * 32 + col;
-    const int token = min(r, rows - 1) / G, head = hk * G + min(r, rows - 1) % G;
-    const int limit = q.cached + token + 1;
-    const int wave_least = q.cached + min(row0 + wave * 32, rows - 1) / G + 1;
-    const int wave_most = q.cached + min(row0 + wave * 32 + 31, rows - 1) / G + 1;
-    const int within = min(limit, end) - 4 * grp;  // slots of this range that the row sees, less the lane's own offset
-    const bool active = row0 + wave * 32 < rows;
     u32x4 qf[HD / 16];
-    const uint16_t* qp = a.q.p + (int64_t)(q.row0 + token) * a.q.row + (int64_t)head * a.q.head + grp * 8;
+    auto load_q = [&](int tile) {
+        const int r = min(tile * kRows + wave * 32 + col, rows - 1);
+        const uint16_t* p = a.q.p + (int64_t)(q.row0 + r / G) * a.q.row + (int64_t)(hk * G + r % G) * a.q.head + grp * 8;
 #pragma unroll
-    for (int f = 0; f < HD / 16; ++f) qf[f] = *(const u32x4*)(qp + f * 16);
-    f32x16 acc[HD / 32];
-#pragma unroll
-    for (int m = 0; m < HD / 32; ++m)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[m][i] = 0.f;
-    float ref = kEmpty, sum = 0.f;
+        for (int f = 0; f < HD / 16; ++f) qf[f] = *(const u32x4*)(p + f * 16);
+    };
     Tile<HD> next;
     const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4*)&lds[0][0];
     const uint32_t wave_at = __builtin_amdgcn_readfirstlane(lds_at + wave * 1024);
-    auto copy = [&](int buf) {  // the next tile, 16 bytes per thread and piece
+    auto copy = [&](int buf, int j0) {  // 64 slots, 16 bytes per thread and piece
+        const uint8_t* from = packed + (int64_t)(j0 / kSlots) * Tile<HD>::kBytes;
 #pragma unroll
         for (int i = 0; i < Tile<HD>::kPieces; ++i)
-            copy_to_lds(packed + i * 4096, threadIdx.x * 16, wave_at + buf * Tile<HD>::kBytes + i * 4096);
-        packed += Tile<HD>::kBytes;
+            copy_to_lds(from + i * 4096, threadIdx.x * 16, wave_at + buf * Tile<HD>::kBytes + i * 4096);
+    };
+    // `least`: slots that the first row of the tile that uses them sees
+    auto store = [&](int buf, int j0, int least) {
+        if (next.store(lds[buf], j0, total, j0 + kSlots > least)) nan[buf] = j0 + 1;
     };
     if (PACKED) {
-        copy(0);
+        copy(0, first);
     } else {
         if (threadIdx.x < 2) nan[threadIdx.x] = 0;
         __syncthreads();
         next.load(c, K, V, ks, vs, first, total);
-        if (next.store(lds[0], first, total, first + kSlots > least)) nan[0] = first + 1;
-        if (first + kSlots < end) next.load(c, K, V, ks, vs, first + kSlots, total);
+        store(0, first, q.cached + tile * kRows / G + 1);
+        next.load(c, K, V, ks, vs, first + kSlots < sees_of(tile) ? first + kSlots : first, total);  // the one after it
     }
+    load_q(tile);
     const int v_at = Tile<HD>::v_place(col, grp, 0);
-    // q is waited for here: a wait in the loop would be one for the copies of the next tile, too
-#pragma unroll
-    for (int f = 0; f < HD / 16; ++f) asm volatile("" : "+v"(qf[f]));
     int buf = 0;
-    for (int j0 = first; j0 < end; j0 += kSlots, buf ^= 1) {
-        if (PACKED) wait_copies<0>();
-        __syncthreads();  // the tile is there, and nobody reads the other buffer any more
-        if (j0 + kSlots < end) {
-            if (PACKED) {
-                copy(buf ^ 1);
-            } else {
-                if (next.store(lds[buf ^ 1], j0 + kSlots, total, j0 + 2 * kSlots > least)) nan[buf ^ 1] = j0 + kSlots + 1;
-                if (j0 + 2 * kSlots < end) next.load(c, K, V, ks, vs, j0 + 2 * kSlots, total);
-            }
-        }
-        if (!active || j0 >= wave_most) continue;
-        const bool holes = PACKED ? odd[j0 / kSlots] != 0 : nan[buf] == j0 + 1;
-        f32x16 z[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) z[t][i] = 0.f;
-#pragma unroll
-            for (int f = 0; f < HD / 16; ++f) z[t] = mfma32(lds[buf][(t * (HD / 16) + f) * 64 + lane], qf[f], z[t]);
-        }
-        const bool whole = j0 + kSlots <= wave_least && j0 + kSlots <= end;
-        if (!whole) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    if (t * 32 + row_of(i, 0) >= within - j0) z[t][i] = -__builtin_inff();
-                }
-        }
-        float top = z[0][0];
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, z[t][i]);
-        top *= a.qscale;
-        if (__any(top > ref - kNear)) {
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float now = top > ref - kNear ? fmaxf(ref, top + kAbove) : ref;
-            const float f = __builtin_amdgcn_exp2f(ref - now);
-            ref = now;
-            sum *= f;
-#pragma unroll
-            for (int m = 0; m < HD / 32; ++m)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[m][i] *= f;
-        }
-        u32x4 pf[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            float p[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u >> 1][(u & 1) * 8 + i], a.qscale, -ref));
-                sum += p[i];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) pf[u][i] = pack_bf16(p[2 * i], p[2 * i + 1]);
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int m = 0; m < HD / 32; ++m) acc[m] = mfma32(lds[buf][(Tile<HD>::kUnits + u * (HD / 32) + m) * 64 + (v_at ^ (m >> 1) << 3)], pf[u], acc[m]);
-        if (holes) {  // NaN codes that were left out: back in for the rows that see them
-            for (int j = j0; j < min(j0 + kSlots, end); ++j)
-#pragma unroll
-                for (int m = 0; m < HD / 32; ++m)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (j < limit && (V[(int64_t)j * HD + m * 32 + row_of(i, grp)] & 0x7f) == 0x7f) acc[m][i] = __builtin_nanf("");
-        }
-    }
-    sum += __shfl_xor(sum, 32, 64);
-    const int many = (sees + sp.per - 1) / sp.per;  // ranges of this tile of rows
-    if (many > 1) {
-        if (r >= rows) return;
-        const int64_t at = ((int64_t)pair * sp.ranges + range) * sp.tile_rows + r;
+    for (int k = 0; tile >= 0; ++k) {
+        const int row0 = tile * kRows, sees = sees_of(tile), end = min(first + sp.per, sees);
+        const int least = q.cached + row0 / G + 1;  // slots that the first row sees
+        const int r = row0 + wave * 32 + col;
+        const int limit = q.cached + min(r, rows - 1) / G + 1;
+        const int wave_least = q.cached + min(row0 + wave * 32, rows - 1) / G + 1;
+        const int wave_most = q.cached + min(row0 + wave * 32 + 31, rows - 1) / G + 1;
+        const int within = min(limit, end) - 4 * grp;  // slots of this range that the row sees, less the lane's own offset
+        const bool active = row0 + wave * 32 < rows;
+        const int tile_next = tile_of(k + 1);
+        f32x16 acc[HD / 32];
 #pragma unroll
         for (int m = 0; m < HD / 32; ++m)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *(f32x4*)(sp.acc + at * HD + m * 32 + row_of(i * 4, grp)) = f32x4{acc[m][4 * i], acc[m][4 * i + 1], acc[m][4 * i + 2], acc[m][4 * i + 3]};
-        if (grp == 0) sp.ml[at] = make_float2(ref, sum);
-        return;
-    }
-    const float inv = 1.f / sum;
-    if (sp.final_ml != nullptr && grp == 0 && r < rows) sp.final_ml[(int64_t)pair * sp.tile_rows + r] = make_float2(ref, inv);
-    // rows through LDS (16 bytes of padding), so that a row leaves in one piece
-    constexpr int RS = HD / 8 + 1;
-    __syncthreads();
-    u32x4* mine = &lds[0][0] + wave * 32 * RS;
+            for (int i = 0; i < 16; ++i) acc[m][i] = 0.f;
+        float ref = kEmpty, sum = 0.f;
+        // q is waited for here: a wait in the loop would be one for the copies of the next slots, too
 #pragma unroll
-    for (int m = 0; m < HD / 32; ++m)
+        for (int f = 0; f < HD / 16; ++f) asm volatile("" : "+v"(qf[f]));
+        for (int j0 = first; j0 < end; j0 += kSlots, buf ^= 1) {
+            if (PACKED) wait_copies<0>();
+            __syncthreads();  // the slots are there, and nobody reads the other buffer any more
+            const bool more = j0 + kSlots < end;
+            if (more || tile_next >= 0) {  // the next slots, or the first ones again for the next rows
+                if (PACKED) {
+                    copy(buf ^ 1, more ? j0 + kSlots : first);
+                } else {
+                    store(buf ^ 1, more ? j0 + kSlots : first, more ? least : q.cached + tile_next * kRows / G + 1);
+                    const int then = (more ? j0 + kSlots : first) + kSlots;  // and the ones after that
+                    next.load(c, K, V, ks, vs, then < (more ? end : sees_of(tile_next)) ? then : first, total);
+                }
+            }
+            if (!active || j0 >= wave_most) continue;
+            const bool holes = PACKED ? odd[j0 / kSlots] != 0 : nan[buf] == j0 + 1;
+            f32x16 z[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            u32x2 w;
-            w.x = pack_bf16(acc[m][4 * i] * inv, acc[m][4 * i + 1] * inv);
-            w.y = pack_bf16(acc[m][4 * i + 2] * inv, acc[m][4 * i + 3] * inv);
-            ((u32x2*)(mine + col * RS))[(m * 32 + row_of(i * 4, grp)) / 4] = w;
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[t][i] = 0.f;
+#pragma unroll
+                for (int f = 0; f < HD / 16; ++f) z[t] = mfma32(lds[buf][(t * (HD / 16) + f) * 64 + lane], qf[f], z[t]);
+            }
+            const bool whole = j0 + kSlots <= wave_least && j0 + kSlots <= end;
+            if (!whole) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        if (t * 32 + row_of(i, 0) >= within - j0) z[t][i] = -__builtin_inff();
+                    }
+            }
+            float top = z[0][0];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, z[t][i]);
+            top *= a.qscale;
+            if (__any(top > ref - kNear)) {
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                const float now = top > ref - kNear ? fmaxf(ref, top + kAbove) : ref;
+                const float f = __builtin_amdgcn_exp2f(ref - now);
+                ref = now;
+                sum *= f;
+#pragma unroll
+                for (int m = 0; m < HD / 32; ++m)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[m][i] *= f;
+            }
+            u32x4 pf[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                float p[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u >> 1][(u & 1) * 8 + i], a.qscale, -ref));
+                    sum += p[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pf[u][i] = pack_bf16(p[2 * i], p[2 * i + 1]);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int m = 0; m < HD / 32; ++m) acc[m] = mfma32(lds[buf][(Tile<HD>::kUnits + u * (HD / 32) + m) * 64 + (v_at ^ (m >> 1) << 3)], pf[u], acc[m]);
+            if (holes) {  // NaN codes that were left out: back in for the rows that see them
+                for (int j = j0; j < min(j0 + kSlots, end); ++j)
+#pragma unroll
+                    for (int m = 0; m < HD / 32; ++m)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (j < limit && (V[(int64_t)j * HD + m * 32 + row_of(i, grp)] & 0x7f) == 0x7f) acc[m][i] = __builtin_nanf("");
+            }
         }
-    constexpr int LPR = HD / 8;  // lanes per row
+        if (tile_next >= 0) load_q(tile_next);
+        sum += __shfl_xor(sum, 32, 64);
+        if ((sees + sp.per - 1) / sp.per > 1) {  // several ranges: merged later
+            if (r < rows) {
+                const int64_t at = ((int64_t)pair * sp.ranges + range) * sp.tile_rows + r;
 #pragma unroll
-    for (int i = 0; i < 32 / (64 / LPR); ++i) {
-        const int in = i * (64 / LPR) + lane / LPR, at = row0 + wave * 32 + in;
-        if (at < rows)
-            *(u32x4*)(a.out.p + (int64_t)(q.row0 + at / G) * a.out.row + (int64_t)(hk * G + at % G) * a.out.head + lane % LPR * 8) = mine[in * RS + lane % LPR];
+                for (int m = 0; m < HD / 32; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        *(f32x4*)(sp.acc + at * HD + m * 32 + row_of(i * 4, grp)) = f32x4{acc[m][4 * i], acc[m][4 * i + 1], acc[m][4 * i + 2], acc[m][4 * i + 3]};
+                if (grp == 0) sp.ml[at] = make_float2(ref, sum);
+            }
+        } else {
+            const float inv = 1.f / sum;
+            if (sp.final_ml != nullptr && grp == 0 && r < rows) sp.final_ml[(int64_t)pair * sp.tile_rows + r] = make_float2(ref, inv);
+            // The rows go through the buffer that is done with, so that each leaves in one piece; its 16-byte pieces lie
+            // at an xor of the row, which spreads them over the banks.
+            constexpr int PPR = HD / 8;  // pieces of a row
+            __syncthreads();
+            u32x4* mine = &lds[buf ^ 1][0] + wave * 32 * PPR;
+#pragma unroll
+            for (int m = 0; m < HD / 32; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    u32x2 w;
+                    w.x = pack_bf16(acc[m][4 * i] * inv, acc[m][4 * i + 1] * inv);
+                    w.y = pack_bf16(acc[m][4 * i + 2] * inv, acc[m][4 * i + 3] * inv);
+                    ((u32x2*)(mine + col * PPR + ((m * 4 + i) ^ (col % PPR))))[grp] = w;
+                }
+            // the lane's rows, 64 / PPR apart
+            constexpr int APART = 64 / PPR;
+            int at = row0 + wave * 32 + lane / PPR, g = at % G;
+            uint16_t* o = a.out.p + (int64_t)(q.row0 + at / G) * a.out.row + (int64_t)(hk * G + g) * a.out.head + lane % PPR * 8;
+            const int step_g = APART % G;
+            const int64_t step = (int64_t)(APART / G) * a.out.row + (int64_t)step_g * a.out.head, wrap = a.out.row - (int64_t)G * a.out.head;
+#pragma unroll
+            for (int i = 0; i < PPR / 2; ++i) {
+                const int in = i * APART + lane / PPR;
+                if (at < rows) *(u32x4*)o = mine[in * PPR + (lane % PPR ^ in % PPR)];
+                at += APART;
+                o += step;
+                g += step_g;
+                if (g >= G) {
+                    g -= G;
+                    o += wrap;
+                }
+            }
+        }
+        tile = tile_next;
     }
 }
 
@@ -686,7 +729,7 @@ __global__ __launch_bounds__(256, 4) void prompt_weights_kernel(Cache c, Step s,
     constexpr int RING = 4;                            // tiles of 32 rows in LDS, RING - 1 of them on their way
     __shared__ u32x4 qt[RING][F * 64];
     __shared__ float2 ml[RING][32];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, grp = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, grp = lane >> 5;
     const int pairs = c.n_seq * c.Hkv;
     const int pair = blockIdx.x % pairs, chunk = blockIdx.x / pairs;
     const int seq = pair / c.Hkv, hk = pair % c.Hkv, G = a.Hq / c.Hkv;
@@ -789,7 +832,7 @@ int64_t up256(int64_t v) { return (v + 255) & ~(int64_t)255; }
 // How a step is run, from its sizes and bounds.
 struct Plan {
     int tiles;  // row tiles of decode_kernel; 0: many new tokens, in `row_tiles` tiles of kRows
-    int row_tiles;
+    int row_tiles, each;  // `each`: row tiles of a workgroup
     Split sp;
     int64_t o_ml, o_scores, o_final, o_packed, o_odd, bytes;
 };
@@ -813,6 +856,10 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
     p.sp.per = (int)per;
     p.sp.ranges = (int)ranges;
     p.sp.score_stride = (most + 31) / 32 * 32;
+    // Short prompts: two row tiles and more per workgroup while 1024 workgroups remain (32 prompts of 512 tokens 150 us
+    // with one, 145 with two, 144 with four); long ones keep the order of the heaviest first (two prompts of 4096: 277, 281, 284).
+    p.each = 1;
+    while (ranges == 1 && most <= 1024 && p.each < 4 && pairs * p.row_tiles >= 1024 * p.each) p.each *= 2;
     int64_t o = 0;
     const int64_t items = ranges > 1 ? pairs * ranges * p.sp.tile_rows : 0;
     o += up256(items * c.hd * 4);
@@ -825,7 +872,7 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
     p.o_packed = o;
     // dequantised once where several row tiles use a tile, and the copy stays under 4 GiB
     const int64_t tiles = (most + kSlots - 1) / kSlots, copy = pairs * tiles * kSlots * c.hd * 4;
-    if (p.tiles == 0 && p.row_tiles >= 4 && copy <= (int64_t)4 << 30) {
+    if (p.tiles == 0 && p.row_tiles >= 32 && copy <= (int64_t)4 << 30) {
         p.sp.packed_tiles = (int)tiles;
         o += up256(copy);
         p.o_odd = o;
@@ -848,14 +895,15 @@ void launch_hd(hipStream_t st, const Cache& c, const Step& s, const Attend& a, c
     const int64_t pairs = (int64_t)c.n_seq * c.Hkv;
     const dim3 block(256);
     if (s.n_rows > 0) {
-        const dim3 grid((unsigned)(pairs * p.sp.ranges * (p.tiles > 0 ? 1 : p.row_tiles)));
+        const int groups = p.tiles > 0 ? 1 : (p.row_tiles + p.each - 1) / p.each;
+        const dim3 grid((unsigned)(pairs * p.sp.ranges * groups));
         if (p.tiles == 1) launch_decode<HD, 1>(st, grid, c, s, a, p.sp);
         else if (p.tiles == 2) launch_decode<HD, 2>(st, grid, c, s, a, p.sp);
         else if (p.sp.packed_tiles > 0) {
             hipLaunchKernelGGL(pack_kernel<HD>, dim3((unsigned)(pairs * p.sp.packed_tiles)), block, 0, st, c, s, p.sp.packed, p.sp.odd, p.sp.packed_tiles);
-            hipLaunchKernelGGL((prompt_kernel<HD, true>), grid, block, 0, st, c, s, a, p.sp, p.row_tiles);
+            hipLaunchKernelGGL((prompt_kernel<HD, true>), grid, block, 0, st, c, s, a, p.sp, groups, p.each);
         } else
-            hipLaunchKernelGGL((prompt_kernel<HD, false>), grid, block, 0, st, c, s, a, p.sp, p.row_tiles);
+            hipLaunchKernelGGL((prompt_kernel<HD, false>), grid, block, 0, st, c, s, a, p.sp, groups, p.each);
         if (p.sp.ranges > 1)
             hipLaunchKernelGGL(merge_kernel<HD>, dim3((unsigned)((pairs * p.sp.tile_rows + 3) / 4)), block, 0, st, c, s, a, p.sp, p.tiles > 0);
     }

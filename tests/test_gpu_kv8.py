@@ -209,6 +209,10 @@ ATTENDS = [
     (16, 64, 16, 8, [1000, 0, 3], [17, 0, 300]),
     (64, 128, 12, 2, [2100], [40]),
     (128, 32, 4, 1, [600, 1], [70, 700]),
+    (16, 32, 64, 64, [0] * 9, [530, 512, 31, 500, 64, 65, 1, 0, 400]),      # many row tiles: two and more per workgroup
+    (64, 64, 64, 32, [3, 0, 100], [600, 580, 33]),
+    (64, 128, 48, 16, [0, 5], [350, 400]),
+    (32, 64, 128, 128, [0, 70, 64, 1], [250, 200, 129, 128]),               # two row tiles per pair, not dequantised ahead
 ]
 
 
@@ -249,7 +253,7 @@ def test_attention_of_infinite_and_nan_values_stays_with_those_who_see_them():
     cache, codes, scale = filled(g, 1, kv, 64, hd, block, [40])
     cache.v[0, 0, 39, 7] = 0x7f
     codes[1][0, 0, 39, 7] = 0x7f
-    for cached, new in ([0, 40], [38, 2], [36, 4], [32, 8], [39, 1]):
+    for cached, new in ([0, 40], [38, 2], [36, 4], [32, 8], [10, 30], [39, 1]):
         q = rand(g, (new, heads, hd))
         out = torch.zeros((new, heads, hd), dtype=torch.bfloat16, device=DEV)
         Q.attend(cache, Q.Kv8Step(ints([cached]), new, new, cached), q.to(DEV), out)
@@ -257,6 +261,23 @@ def test_attention_of_infinite_and_nan_values_stays_with_those_who_see_them():
         nan = torch.zeros_like(got, dtype=torch.bool)
         nan[-1, :heads // kv, 7] = True
         assert torch.equal(got.isnan(), nan)
+
+
+def test_nan_codes_in_prompts_stay_with_those_who_see_them():
+    """Four row tiles and more, dequantised ahead: NaN codes at slots 70 and 300 of a prompt of 400 tokens."""
+    block, hd, heads, kv, new = 32, 64, 8, 2, 400
+    g = torch.Generator().manual_seed(19)
+    for cached in (0, 75):
+        cache, codes, scale = filled(g, 1, kv, 480, hd, block, [cached + new])
+        for slot, e in ((70, 3), (300, 60)):
+            cache.v[0, 1, slot, e] = 0xff
+        q = rand(g, (new, heads, hd))
+        out = torch.zeros((new, heads, hd), dtype=torch.bfloat16, device=DEV)
+        Q.attend(cache, Q.Kv8Step(ints([cached]), new, new, cached), q.to(DEV), out)
+        nan = torch.zeros((new, heads, hd), dtype=torch.bool)
+        nan[max(0, 70 - cached):, heads // kv:, 3] = True
+        nan[300 - cached:, heads // kv:, 60] = True
+        assert torch.equal(out.cpu().isnan(), nan)
 
 
 @pytest.mark.parametrize("cached,new", [(700, 1), (0, 150), (300, 5)])
