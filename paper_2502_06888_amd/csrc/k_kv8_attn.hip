@@ -849,7 +849,13 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
         per = ((int64_t)most * pairs / 2048 + 127) / 128 * 128;  // 2048 workgroups
         per = per < 256 ? 256 : per;
     } else {
-        per = ((int64_t)most * pairs * p.row_tiles / 1536 + kSlots - 1) / kSlots * kSlots;  // 1536 workgroups
+        // Ranges only where the row tiles do not fill the chip (two workgroups per compute unit; half of that where most
+        // slots are the new tokens' own, so that many tiles see few): their fp32 sums, written and read, cost more than
+        // what they even out.  One prompt of 2048 tokens, 512 tiles: 54 us whole, 79-84 in ranges; one of 4096: 156 and 234.
+        // Two of 512 behind 16000 slots, 256 tiles: in 2 ranges 382, 3 331, 4 327, 5 334 us.
+        const int64_t tiles = pairs * p.row_tiles;
+        const bool fills = tiles >= 512 || (tiles >= 256 && s.max_cached <= s.max_new);
+        per = fills ? (most + kSlots) / kSlots * kSlots : (most * tiles / 1024 + kSlots - 1) / kSlots * kSlots;
         per = per < 1024 ? 1024 : per;
     }
     const int64_t ranges = most > per ? (most + per - 1) / per : 1;
