@@ -58,27 +58,36 @@ struct Split {
     float* acc;         // [pair, range, row, hd] unnormalised sums; with float2 `ml` (reference, sum of weights)
     float2* ml;
     float* scores;      // [pair, row, slot] products q . K
-    float2* final_ml;   // [pair, row] of the whole sequence: reference, 1 / sum of weights
+    float2* final_ml;   // [pair, row] with many new tokens: reference of all ranges, 1 / sum of weights
     u32x4* packed;      // [pair, tile of kSlots] dequantised (see Tile), or null
     int32_t* odd;       // [pair, tile]
     int packed_tiles;   // tiles per pair
 };
 
-template <int HD, int NT, bool SCORES>
+template <bool STREAM, class T>
+__device__ __forceinline__ T fetch(const T* p) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+
+template <int HD, int NT, bool SCORES, bool STREAM>
 __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) void decode_kernel(Cache c, Step s, Attend a, Split sp) {
     constexpr int KW = HD / 16;             // words of a K row that a lane holds: HD/4 bytes
     constexpr int VT = HD / 16;             // tiles of 16 elements of the sums
     constexpr int VW = VT >= 4 ? VT / 4 : 1;  // words of a V row that a lane holds: VT bytes
     __shared__ float sm_o[4][NT * 8][HD];
-    __shared__ float2 sm_ml[4][NT * 8];
+    __shared__ float2 sm_ml[4][NT * 8], done[NT * 8];
     const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 15, grp = lane >> 4;
     const int range = blockIdx.x % sp.ranges, pair = blockIdx.x / sp.ranges;
     const int seq = pair / c.Hkv, hk = pair % c.Hkv, G = a.Hq / c.Hkv;
     const Seq q = sequence(c, s, seq);
     const int len = q.cached + q.n_new, rows = q.n_new * G;
     const int first = range * sp.per, end = min(first + sp.per, len);
-    if (rows == 0 || first >= end) return;
     const int64_t base = (int64_t)seq * c.Hkv + hk;
+    const int many = (len + sp.per - 1) / sp.per;  // ranges of this sequence
+    if (SCORES && rows == 0 && many <= 1 && range == 0)  // no new tokens: the weights stay
+        for (int j = threadIdx.x; j < len; j += 256) a.weight_out[base * c.max_len + j] = a.weight_in != nullptr ? a.weight_in[base * c.max_len + j] : 0.f;
+    if (rows == 0 || first >= end) return;
     const uint8_t *K = c.codes[0] + base * c.max_len * HD, *V = c.codes[1] + base * c.max_len * HD;
     const float *ks = c.scale[0] + base * (c.max_len >> c.logb), *vs = c.scale[1] + base * (c.max_len >> c.logb);
 
@@ -115,13 +124,13 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
             const uint8_t* p = K + (int64_t)min(p0 + t * 16 + col, end - 1) * HD;
             ksc[t] = ks[min(p0 + t * 16, end - 1) >> c.logb];
             if constexpr (HD == 32) {
-                const u32x2 x = *(const u32x2*)(p + grp * 8);
+                const u32x2 x = fetch<STREAM>((const u32x2*)(p + grp * 8));
                 kr[t][0] = x.x;
                 kr[t][1] = x.y;
             } else {
 #pragma unroll
                 for (int h = 0; h < HD / 64; ++h) {
-                    const u32x4 x = *(const u32x4*)(p + h * 64 + grp * 16);
+                    const u32x4 x = fetch<STREAM>((const u32x4*)(p + h * 64 + grp * 16));
 #pragma unroll
                     for (int i = 0; i < 4; ++i) kr[t][h * 4 + i] = x[i];
                 }
@@ -133,13 +142,13 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
         for (int j = 0; j < 8; ++j) {
             const uint8_t* p = V + (int64_t)min(p0 + (j >> 2) * 16 + grp * 4 + (j & 3), end - 1) * HD + col * VT;
             if constexpr (HD == 128) {
-                const u32x2 x = *(const u32x2*)p;
+                const u32x2 x = fetch<STREAM>((const u32x2*)p);
                 vr[j][0] = x.x;
                 vr[j][1] = x.y;
             } else if constexpr (HD == 64) {
-                vr[j][0] = *(const uint32_t*)p;
+                vr[j][0] = fetch<STREAM>((const uint32_t*)p);
             } else {
-                vr[j][0] = *(const uint16_t*)p;
+                vr[j][0] = fetch<STREAM>((const uint16_t*)p);
             }
         }
 #pragma unroll
@@ -276,7 +285,6 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
             }
     }
     __syncthreads();
-    const int many = (len + sp.per - 1) / sp.per;  // ranges of this sequence
     const int total = min(rows, NT * 8) * HD;
     for (int i = threadIdx.x * 4; i < total; i += 1024) {
         const int r = i / HD, d = i % HD;
@@ -302,71 +310,145 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
             w.x = pack_bf16(o[0] * inv, o[1] * inv);
             w.y = pack_bf16(o[2] * inv, o[3] * inv);
             *(u32x2*)(a.out.p + (int64_t)(q.row0 + r / G) * a.out.row + (int64_t)(hk * G + r % G) * a.out.head + d) = w;
-            if (SCORES && d == 0) sp.final_ml[(int64_t)pair * sp.tile_rows + r] = make_float2(mm, inv);
+            if (SCORES && d == 0) done[r] = make_float2(mm, inv);
         }
+    }
+    if (!SCORES || many > 1) return;
+    __syncthreads();  // statistics and scores are there, those of this workgroup
+    for (int j = threadIdx.x; j < len; j += 256) {
+        float w = a.weight_in != nullptr && j < q.cached ? a.weight_in[base * c.max_len + j] : 0.f;
+        for (int r = max(0, j - q.cached) * G; r < rows; ++r) {
+            const float z = sp.scores[((int64_t)pair * sp.tile_rows + r) * sp.score_stride + j];
+            w += __builtin_amdgcn_exp2f(__builtin_fmaf(z, a.qscale, -done[r].x)) * done[r].y;
+        }
+        a.weight_out[base * c.max_len + j] = w;
     }
 }
 
-// Adds up the ranges of one (pair, row): one wavefront, HD/4 lanes per range.
-template <int HD>
-__global__ __launch_bounds__(256) void merge_kernel(Cache c, Step s, Attend a, Split sp, bool few) {
-    constexpr int LPR = HD / 4, SIDE = 64 / LPR;
-    const int lane = threadIdx.x & 63, sub = lane % LPR;
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int pair = (int)(item / sp.tile_rows), r = (int)(item % sp.tile_rows);
-    if (pair >= c.n_seq * c.Hkv) return;
-    const int seq = pair / c.Hkv, hk = pair % c.Hkv, G = a.Hq / c.Hkv;
-    const Seq q = sequence(c, s, seq);
-    if (r >= q.n_new * G) return;
-    // few tokens: the ranges of the sequence; else those of the slots that the row's tile sees
-    const int sees = few ? q.cached + q.n_new : q.cached + min(r / kRows * kRows + kRows - 1, q.n_new * G - 1) / G + 1;
-    const int many = (sees + sp.per - 1) / sp.per;
-    if (many <= 1) return;
-    const int64_t at = (int64_t)pair * sp.ranges * sp.tile_rows + r;
+struct Partial {  // running softmax over ranges: reference, sum of weights, four elements of the sums
     float m = kEmpty, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    auto add = [&](float m2, float l2, const f32x4& o2) {
+    __device__ __forceinline__ void add(float m2, float l2, const f32x4& o2) {
         const float mn = fmaxf(m, m2), fa = __builtin_amdgcn_exp2f(m - mn), fb = __builtin_amdgcn_exp2f(m2 - mn);
         l = l * fa + l2 * fb;
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] = o[j] * fa + o2[j] * fb;
         m = mn;
-    };
-    for (int i = lane / LPR; i < many; i += SIDE) {
-        const float2 e = sp.ml[at + (int64_t)i * sp.tile_rows];
-        add(e.x, e.y, *(const f32x4*)(sp.acc + (at + (int64_t)i * sp.tile_rows) * HD + sub * 4));
     }
+    // ranges i, i + by, .. of the row whose first partial sums are at `at`, four requested before the first is used
+    template <int HD>
+    __device__ __forceinline__ void add_ranges(const Split& sp, int64_t at, int i, int by, int many, int element) {
+        constexpr int AHEAD = 4;
+        for (; i < many; i += AHEAD * by) {
+            float2 e[AHEAD];
+            f32x4 x[AHEAD];
 #pragma unroll
-    for (int off = LPR; off < 64; off <<= 1) {
-        const float m2 = __shfl_xor(m, off, 64), l2 = __shfl_xor(l, off, 64);
-        f32x4 o2;
+            for (int u = 0; u < AHEAD; ++u) {  // past the end: the last one again, unused
+                const int64_t from = at + (int64_t)min(i + u * by, many - 1) * sp.tile_rows;
+                e[u] = sp.ml[from];
+                x[u] = *(const f32x4*)(sp.acc + from * HD + element);
+            }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o2[j] = __shfl_xor(o[j], off, 64);
-        add(m2, l2, o2);
+            for (int u = 0; u < AHEAD; ++u)
+                if (i + u * by < many) add(e[u].x, e[u].y, x[u]);
+        }
     }
-    if (lane < LPR) {
+    __device__ __forceinline__ void add_lanes(int from) {  // lanes `from`, 2 * from, .. apart
+        for (int off = from; off < 64; off <<= 1) {
+            const float m2 = __shfl_xor(m, off, 64), l2 = __shfl_xor(l, off, 64);
+            f32x4 o2;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o2[j] = __shfl_xor(o[j], off, 64);
+            add(m2, l2, o2);
+        }
+    }
+    __device__ __forceinline__ void write(uint16_t* to) const {
         const float inv = 1.f / l;
         u32x2 w;
         w.x = pack_bf16(o[0] * inv, o[1] * inv);
         w.y = pack_bf16(o[2] * inv, o[3] * inv);
-        *(u32x2*)(a.out.p + (int64_t)(q.row0 + r / G) * a.out.row + (int64_t)(hk * G + r % G) * a.out.head + sub * 4) = w;
-        if (sp.final_ml != nullptr && sub == 0) sp.final_ml[(int64_t)pair * sp.tile_rows + r] = make_float2(m, inv);
+        *(u32x2*)to = w;
     }
+};
+
+// Few new tokens, sequences of several ranges.  The first workgroups take a (pair, row) each and add up its ranges, four
+// wavefronts of 64 / (HD/4) ranges side by side; the others take 256 slots of a pair each: what its rows gave
+// them, from the products kept by decode_kernel and the statistics of all ranges.
+template <int HD>
+__global__ __launch_bounds__(256) void finish_kernel(Cache c, Step s, Attend a, Split sp, int merges, int chunks) {
+    constexpr int LPR = HD / 4, SIDE = 64 / LPR;
+    __shared__ float4 sums[4][LPR];
+    __shared__ float2 stat[16];
+    const int lane = threadIdx.x & 63, wave = wave_number(), G = a.Hq / c.Hkv;
+    const bool merging = (int)blockIdx.x < merges;
+    const int item = merging ? blockIdx.x : blockIdx.x - merges;
+    const int pair = item / (merging ? sp.tile_rows : chunks), seq = pair / c.Hkv;
+    const Seq q = sequence(c, s, seq);
+    const int len = q.cached + q.n_new, rows = q.n_new * G, many = (len + sp.per - 1) / sp.per;
+    if (merging) {
+        const int r = item % sp.tile_rows;
+        if (r >= rows || many <= 1) return;
+        const int64_t at = (int64_t)pair * sp.ranges * sp.tile_rows + r;
+        Partial t;
+        t.add_ranges<HD>(sp, at, wave * SIDE + lane / LPR, 4 * SIDE, many, lane % LPR * 4);
+        t.add_lanes(LPR);
+        if (lane < LPR) sums[wave][lane] = make_float4(t.o[0], t.o[1], t.o[2], t.o[3]);
+        if (lane == 0) stat[wave] = make_float2(t.m, t.l);
+        __syncthreads();
+        if (wave != 0 || lane >= LPR) return;
+        for (int w = 1; w < 4; ++w) t.add(stat[w].x, stat[w].y, f32x4{sums[w][lane].x, sums[w][lane].y, sums[w][lane].z, sums[w][lane].w});
+        t.write(a.out.p + (int64_t)(q.row0 + r / G) * a.out.row + (int64_t)(pair % c.Hkv * G + r % G) * a.out.head + lane * 4);
+        return;
+    }
+    if (many <= 1) return;  // done by decode_kernel
+    const int j0 = item % chunks * 256, j = j0 + threadIdx.x;
+    if (j0 >= len) return;
+    for (int r = wave * 4; r < rows; r += 16)  // 16 lanes per row
+        if (const int row = r + lane / 16; true) {
+            float m = kEmpty, l = 0.f;
+            for (int i = lane % 16; i < many && row < rows; i += 16) {
+                const float2 e = sp.ml[((int64_t)pair * sp.ranges + i) * sp.tile_rows + row];
+                const float mn = fmaxf(m, e.x);
+                l = l * __builtin_amdgcn_exp2f(m - mn) + e.y * __builtin_amdgcn_exp2f(e.x - mn);
+                m = mn;
+            }
+            for (int off = 1; off < 16; off <<= 1) {
+                const float m2 = __shfl_xor(m, off, 64), l2 = __shfl_xor(l, off, 64), mn = fmaxf(m, m2);
+                l = l * __builtin_amdgcn_exp2f(m - mn) + l2 * __builtin_amdgcn_exp2f(m2 - mn);
+                m = mn;
+            }
+            if (lane % 16 == 0 && row < rows) stat[row] = make_float2(m, 1.f / l);
+        }
+    __syncthreads();
+    if (j >= len) return;
+    const int64_t at = (int64_t)pair * c.max_len + j;
+    float w = a.weight_in != nullptr && j < q.cached ? a.weight_in[at] : 0.f;
+    for (int r = max(0, j - q.cached) * G; r < rows; ++r) {
+        const float z = sp.scores[((int64_t)pair * sp.tile_rows + r) * sp.score_stride + j];
+        w += __builtin_amdgcn_exp2f(__builtin_fmaf(z, a.qscale, -stat[r].x)) * stat[r].y;
+    }
+    a.weight_out[at] = w;
 }
 
-// One thread per slot: what the rows of its pair gave it, from the products kept by decode_kernel.
-__global__ __launch_bounds__(256) void weights_kernel(Cache c, Step s, Attend a, Split sp, int chunks) {
-    const int64_t pair = blockIdx.x / chunks;
-    const int j = blockIdx.x % chunks * 256 + threadIdx.x, seq = (int)(pair / c.Hkv), G = a.Hq / c.Hkv;
-    const Seq q = sequence(c, s, seq);
-    if (j >= q.cached + q.n_new) return;
-    float w = a.weight_in != nullptr && j < q.cached ? a.weight_in[pair * c.max_len + j] : 0.f;
-    for (int r = max(0, j - q.cached) * G; r < q.n_new * G; ++r) {
-        const float2 ml = sp.final_ml[pair * sp.tile_rows + r];
-        const float z = sp.scores[(pair * sp.tile_rows + r) * sp.score_stride + j];
-        w += __builtin_amdgcn_exp2f(z * a.qscale - ml.x) * ml.y;
-    }
-    a.weight_out[pair * c.max_len + j] = w;
+// Many new tokens: adds up the ranges of one (pair, row), one wavefront.
+template <int HD>
+__global__ __launch_bounds__(256) void merge_kernel(Cache c, Step s, Attend a, Split sp) {
+    constexpr int LPR = HD / 4, SIDE = 64 / LPR;
+    const int lane = threadIdx.x & 63, G = a.Hq / c.Hkv;
+    const int64_t item = (int64_t)blockIdx.x * 4 + wave_number();
+    const int pair = (int)(item / sp.tile_rows), r = (int)(item % sp.tile_rows);
+    if (pair >= c.n_seq * c.Hkv) return;
+    const Seq q = sequence(c, s, pair / c.Hkv);
+    const int rows = q.n_new * G;
+    if (r >= rows) return;
+    const int many = (q.cached + min(r / kRows * kRows + kRows - 1, rows - 1) / G + sp.per) / sp.per;  // of what the row's tile sees
+    if (many <= 1) return;
+    Partial t;
+    t.add_ranges<HD>(sp, (int64_t)pair * sp.ranges * sp.tile_rows + r, lane / LPR, SIDE, many, lane % LPR * 4);
+    t.add_lanes(LPR);
+    if (lane >= LPR) return;
+    t.write(a.out.p + (int64_t)(q.row0 + r / G) * a.out.row + (int64_t)(pair % c.Hkv * G + r % G) * a.out.head + lane * 4);
+    if (sp.final_ml != nullptr && lane == 0) sp.final_ml[(int64_t)pair * sp.tile_rows + r] = make_float2(t.m, 1.f / t.l);
 }
 
 // ---- many new tokens: bound by the matrix cores ---------------------------------------------------------------
@@ -785,8 +867,10 @@ __global__ __launch_bounds__(256, 4) void prompt_weights_kernel(Cache c, Step s,
             from += wrap;
         }
     };
+    if (rows > 0) {  // a sequence without new tokens has no row of q, and its weights stay
 #pragma unroll
-    for (int i = 0; i < RING - 1; ++i) copy(i, r_first + i * 32);
+        for (int i = 0; i < RING - 1; ++i) copy(i, r_first + i * 32);
+    }
     const int r_see = (j0 - q.cached) * G, r_whole = (j0 + 31 - q.cached) * G;  // first rows that see a slot of the wavefront, and all
     int at = 0;
     for (int r0 = r_first; r0 < rows; r0 += 32, at = (at + 1) % RING) {
@@ -841,7 +925,7 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
     Plan p{};
     const int64_t pairs = (int64_t)c.n_seq * c.Hkv, rows = (int64_t)s.max_new * (Hq / c.Hkv);
     const int most = (int)min((int64_t)s.max_cached + s.max_new, (int64_t)c.max_len);
-    p.tiles = rows <= 8 ? 1 : rows <= 16 ? 2 : 0;
+    p.tiles = rows == 0 ? 0 : rows <= 8 ? 1 : rows <= 16 ? 2 : 0;  // without rows prompt_weights_kernel carries the weights over
     p.row_tiles = (int)((rows + kRows - 1) / kRows);
     p.sp.tile_rows = p.tiles > 0 ? p.tiles * 8 : p.row_tiles * kRows;
     int64_t per;
@@ -874,7 +958,7 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
     p.o_scores = o;
     if (weights && p.tiles > 0) o += up256(pairs * p.sp.tile_rows * p.sp.score_stride * 4);
     p.o_final = o;
-    if (weights) o += up256(pairs * p.sp.tile_rows * 8);
+    if (weights && p.tiles == 0) o += up256(pairs * p.sp.tile_rows * 8);
     p.o_packed = o;
     // dequantised once where several row tiles use a tile, and the copy stays under 4 GiB
     const int64_t tiles = (most + kSlots - 1) / kSlots, copy = pairs * tiles * kSlots * c.hd * 4;
@@ -890,10 +974,16 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
 
 template <int HD, int NT>
 void launch_decode(hipStream_t st, const dim3& grid, const Cache& c, const Step& s, const Attend& a, const Split& sp) {
+    // Caches beyond the last-level cache of 256 MiB are read past it: 512 sequences of 513 slots (538 MB) 98 us with ordinary
+    // loads, 91 without; 4 of 8000 (61 MB), read again before they are evicted, 31 and 32.
+    const bool stream = (int64_t)c.n_seq * c.Hkv * min((int64_t)s.max_cached + s.max_new, (int64_t)c.max_len) * HD * 2 > (256 << 20);
+    auto launch = [&](auto scores, auto streamed) {
+        hipLaunchKernelGGL((decode_kernel<HD, NT, decltype(scores)::value, decltype(streamed)::value>), grid, dim3(256), 0, st, c, s, a, sp);
+    };
     if (a.weight_out != nullptr)
-        hipLaunchKernelGGL((decode_kernel<HD, NT, true>), grid, dim3(256), 0, st, c, s, a, sp);
+        stream ? launch(std::true_type{}, std::true_type{}) : launch(std::true_type{}, std::false_type{});
     else
-        hipLaunchKernelGGL((decode_kernel<HD, NT, false>), grid, dim3(256), 0, st, c, s, a, sp);
+        stream ? launch(std::false_type{}, std::true_type{}) : launch(std::false_type{}, std::false_type{});
 }
 
 template <int HD>
@@ -910,15 +1000,16 @@ void launch_hd(hipStream_t st, const Cache& c, const Step& s, const Attend& a, c
             hipLaunchKernelGGL((prompt_kernel<HD, true>), grid, block, 0, st, c, s, a, p.sp, groups, p.each);
         } else
             hipLaunchKernelGGL((prompt_kernel<HD, false>), grid, block, 0, st, c, s, a, p.sp, groups, p.each);
-        if (p.sp.ranges > 1)
-            hipLaunchKernelGGL(merge_kernel<HD>, dim3((unsigned)((pairs * p.sp.tile_rows + 3) / 4)), block, 0, st, c, s, a, p.sp, p.tiles > 0);
+        if (p.sp.ranges > 1 && p.tiles > 0) {
+            const int64_t merges = pairs * p.sp.tile_rows, chunks = a.weight_out != nullptr ? (p.sp.score_stride + 255) / 256 : 0;
+            hipLaunchKernelGGL(finish_kernel<HD>, dim3((unsigned)(merges + pairs * chunks)), block, 0, st, c, s, a, p.sp, (int)merges, (int)chunks);
+        } else if (p.sp.ranges > 1) {
+            hipLaunchKernelGGL(merge_kernel<HD>, dim3((unsigned)((pairs * p.sp.tile_rows + 3) / 4)), block, 0, st, c, s, a, p.sp);
+        }
     }
-    if (a.weight_out == nullptr) return;
-    const int chunk = p.tiles > 0 ? 256 : kWeightSlots, chunks = (p.sp.score_stride + chunk - 1) / chunk;
-    if (chunks == 0) return;
-    if (p.tiles > 0)
-        hipLaunchKernelGGL(weights_kernel, dim3((unsigned)(pairs * chunks)), block, 0, st, c, s, a, p.sp, chunks);
-    else
+    if (a.weight_out == nullptr || p.tiles > 0) return;
+    const int chunks = (p.sp.score_stride + kWeightSlots - 1) / kWeightSlots;
+    if (chunks > 0)
         hipLaunchKernelGGL(prompt_weights_kernel<HD>, dim3((unsigned)(pairs * chunks)), block, 0, st, c, s, a, p.sp, chunks);
 }
 
@@ -928,7 +1019,7 @@ bool attend_fits(const Cache& c, const Step& s, int Hq) {
     const Plan p = plan(c, s, Hq, true);
     const int64_t pairs = (int64_t)c.n_seq * c.Hkv;
     const int64_t most = pairs * p.sp.ranges * (p.tiles > 0 ? 1 : p.row_tiles);
-    return most <= 0x7fffffff && pairs * p.sp.tile_rows <= (int64_t)0x7fffffff * 4;
+    return most <= 0x7fffffff && pairs * p.sp.tile_rows + pairs * ((p.sp.score_stride + kWeightSlots - 1) / kWeightSlots) <= 0x7fffffff;
 }
 
 int64_t attend_workspace(const Cache& c, const Step& s, int Hq, bool weights) { return plan(c, s, Hq, weights).bytes; }

@@ -212,6 +212,7 @@ ATTENDS = [
     (16, 32, 64, 64, [0] * 9, [530, 512, 31, 500, 64, 65, 1, 0, 400]),      # many row tiles: two and more per workgroup
     (64, 64, 64, 32, [3, 0, 100], [600, 580, 33]),
     (64, 128, 48, 16, [0, 5], [350, 400]),
+    (32, 64, 8, 2, [60, 5, 0, 33], [0, 200, 0, 0]),                          # sequences without tokens before and behind
     (32, 64, 128, 128, [0, 70, 64, 1], [250, 200, 129, 128]),               # two row tiles per pair, not dequantised ahead
 ]
 
