@@ -54,10 +54,11 @@ constexpr int kRows = 128, kSlots = 64;  // rows and slots of a tile where there
 struct Split {
     int per, ranges;    // slots of a range (a multiple of 128, with many new tokens of 64), ranges of a sequence at most
     int tile_rows;      // rows the buffers below hold per pair
-    int score_stride;   // slots a row of `scores` holds, a multiple of 32
+    int score_stride;   // slots a row of `scores` holds, a multiple of 16
     float* acc;         // [pair, range, row, hd] unnormalised sums; with float2 `ml` (reference, sum of weights)
     float2* ml;
     float* scores;      // [pair, row, slot] products q . K
+    int lds_scores;     // bytes of LDS that hold those of a pair instead, 0: they are in `scores`
     float2* final_ml;   // [pair, row] with many new tokens: reference of all ranges, 1 / sum of weights
     u32x4* packed;      // [pair, tile of kSlots] dequantised (see Tile), or null
     int32_t* odd;       // [pair, tile]
@@ -70,13 +71,17 @@ __device__ __forceinline__ T fetch(const T* p) {
     else return *p;
 }
 
-template <int HD, int NT, bool SCORES, bool STREAM>
+// Where the products q . K go: nowhere, to the workspace, or into LDS (where they fit and a sequence is one range).
+enum { kNoScores, kScores, kScoresLds };
+
+template <int HD, int NT, int SCORES, bool STREAM>
 __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) void decode_kernel(Cache c, Step s, Attend a, Split sp) {
     constexpr int KW = HD / 16;             // words of a K row that a lane holds: HD/4 bytes
     constexpr int VT = HD / 16;             // tiles of 16 elements of the sums
     constexpr int VW = VT >= 4 ? VT / 4 : 1;  // words of a V row that a lane holds: VT bytes
     __shared__ float sm_o[4][NT * 8][HD];
     __shared__ float2 sm_ml[4][NT * 8], done[NT * 8];
+    extern __shared__ __attribute__((aligned(16))) float lds_scores[];
     const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 15, grp = lane >> 4;
     const int range = blockIdx.x % sp.ranges, pair = blockIdx.x / sp.ranges;
     const int seq = pair / c.Hkv, hk = pair % c.Hkv, G = a.Hq / c.Hkv;
@@ -85,6 +90,7 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
     const int first = range * sp.per, end = min(first + sp.per, len);
     const int64_t base = (int64_t)seq * c.Hkv + hk;
     const int many = (len + sp.per - 1) / sp.per;  // ranges of this sequence
+    float* scores = SCORES == kScoresLds ? lds_scores : sp.scores + (int64_t)pair * sp.tile_rows * sp.score_stride;
     if (SCORES && rows == 0 && many <= 1 && range == 0)  // no new tokens: the weights stay
         for (int j = threadIdx.x; j < len; j += 256) a.weight_out[base * c.max_len + j] = a.weight_in != nullptr ? a.weight_in[base * c.max_len + j] : 0.f;
     if (rows == 0 || first >= end) return;
@@ -192,8 +198,8 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
         u32x4 pf[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            if (SCORES && col < 8 && n * 8 + col < rows) {
-                float* to = sp.scores + ((int64_t)pair * sp.tile_rows + n * 8 + col) * sp.score_stride + p0 + grp * 4;
+            if (SCORES != kNoScores && col < 8 && n * 8 + col < rows) {
+                float* to = scores + (int64_t)(n * 8 + col) * sp.score_stride + p0 + grp * 4;
                 *(f32x4*)to = z[n][0];
                 *(f32x4*)(to + 16) = z[n][1];
             }
@@ -318,8 +324,7 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
     for (int j = threadIdx.x; j < len; j += 256) {
         float w = a.weight_in != nullptr && j < q.cached ? a.weight_in[base * c.max_len + j] : 0.f;
         for (int r = max(0, j - q.cached) * G; r < rows; ++r) {
-            const float z = sp.scores[((int64_t)pair * sp.tile_rows + r) * sp.score_stride + j];
-            w += __builtin_amdgcn_exp2f(__builtin_fmaf(z, a.qscale, -done[r].x)) * done[r].y;
+            w += __builtin_amdgcn_exp2f(__builtin_fmaf(scores[(int64_t)r * sp.score_stride + j], a.qscale, -done[r].x)) * done[r].y;
         }
         a.weight_out[base * c.max_len + j] = w;
     }
@@ -371,18 +376,19 @@ struct Partial {  // running softmax over ranges: reference, sum of weights, fou
     }
 };
 
-// Few new tokens, sequences of several ranges.  The first workgroups take a (pair, row) each and add up its ranges, four
-// wavefronts of 64 / (HD/4) ranges side by side; the others take 256 slots of a pair each: what its rows gave
-// them, from the products kept by decode_kernel and the statistics of all ranges.
-template <int HD>
+// Few new tokens, sequences of several ranges.  The first workgroups add up the ranges of a (pair, row): WIDE one each, four
+// wavefronts of 64 / (HD/4) ranges side by side, else one in each wavefront; the others take 256 slots of a pair each:
+// what its rows gave them, from the products kept by decode_kernel and the statistics of all ranges.
+template <int HD, bool WIDE>
 __global__ __launch_bounds__(256) void finish_kernel(Cache c, Step s, Attend a, Split sp, int merges, int chunks) {
     constexpr int LPR = HD / 4, SIDE = 64 / LPR;
     __shared__ float4 sums[4][LPR];
     __shared__ float2 stat[16];
     const int lane = threadIdx.x & 63, wave = wave_number(), G = a.Hq / c.Hkv;
     const bool merging = (int)blockIdx.x < merges;
-    const int item = merging ? blockIdx.x : blockIdx.x - merges;
+    const int item = !merging ? blockIdx.x - merges : WIDE ? blockIdx.x : blockIdx.x * 4 + wave;
     const int pair = item / (merging ? sp.tile_rows : chunks), seq = pair / c.Hkv;
+    if (pair >= c.n_seq * c.Hkv) return;
     const Seq q = sequence(c, s, seq);
     const int len = q.cached + q.n_new, rows = q.n_new * G, many = (len + sp.per - 1) / sp.per;
     if (merging) {
@@ -390,8 +396,12 @@ __global__ __launch_bounds__(256) void finish_kernel(Cache c, Step s, Attend a, 
         if (r >= rows || many <= 1) return;
         const int64_t at = (int64_t)pair * sp.ranges * sp.tile_rows + r;
         Partial t;
-        t.add_ranges<HD>(sp, at, wave * SIDE + lane / LPR, 4 * SIDE, many, lane % LPR * 4);
+        t.add_ranges<HD>(sp, at, (WIDE ? wave * SIDE : 0) + lane / LPR, (WIDE ? 4 : 1) * SIDE, many, lane % LPR * 4);
         t.add_lanes(LPR);
+        if (!WIDE) {
+            if (lane < LPR) t.write(a.out.p + (int64_t)(q.row0 + r / G) * a.out.row + (int64_t)(pair % c.Hkv * G + r % G) * a.out.head + lane * 4);
+            return;
+        }
         if (lane < LPR) sums[wave][lane] = make_float4(t.o[0], t.o[1], t.o[2], t.o[3]);
         if (lane == 0) stat[wave] = make_float2(t.m, t.l);
         __syncthreads();
@@ -930,7 +940,10 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
     p.sp.tile_rows = p.tiles > 0 ? p.tiles * 8 : p.row_tiles * kRows;
     int64_t per;
     if (p.tiles > 0) {
-        per = ((int64_t)most * pairs / 2048 + 127) / 128 * 128;  // 2048 workgroups
+        // About 512 workgroups of 256 slots and more: a range costs its start, its end and its sums written and read.  Aiming at
+        // 512, 1024, 4096 workgroups: 1 sequence of 32000 slots 20, 23, 23 us; 4 of 8000 22, 24, 24; 64 of 750 21, 29, 33;
+        // 256 of 100 to 1500 96, 117, 149; 16 of 2000 19, 21, 21.
+        per = ((int64_t)most * pairs / 512 + 127) / 128 * 128;
         per = per < 256 ? 256 : per;
     } else {
         // Ranges only where the row tiles do not fill the chip (two workgroups per compute unit; half of that where most
@@ -956,7 +969,17 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
     p.o_ml = o;
     o += up256(items * 8);
     p.o_scores = o;
-    if (weights && p.tiles > 0) o += up256(pairs * p.sp.tile_rows * p.sp.score_stride * 4);
+    if (weights && p.tiles > 0) {
+        // The products stay in LDS where a sequence is one range and they fit the 64 KiB that a workgroup can have beside the
+        // sums: 512 sequences of 513 slots 114 us instead of 137, 96 of up to 3002 (48 KB, two workgroups per unit) 52, not 63.
+        const int64_t stride = (most + 63) / 64 * 64 + 16, lds = rows * stride * 4;  // rows 16 banks apart
+        if (ranges == 1 && lds <= (64 << 10) - p.tiles * 8 * (16 * c.hd + 40)) {
+            p.sp.score_stride = (int)stride;
+            p.sp.lds_scores = (int)lds;
+        } else {
+            o += up256(pairs * p.sp.tile_rows * p.sp.score_stride * 4);
+        }
+    }
     p.o_final = o;
     if (weights && p.tiles == 0) o += up256(pairs * p.sp.tile_rows * 8);
     p.o_packed = o;
@@ -977,13 +1000,15 @@ void launch_decode(hipStream_t st, const dim3& grid, const Cache& c, const Step&
     // Caches beyond the last-level cache of 256 MiB are read past it: 512 sequences of 513 slots (538 MB) 98 us with ordinary
     // loads, 91 without; 4 of 8000 (61 MB), read again before they are evicted, 31 and 32.
     const bool stream = (int64_t)c.n_seq * c.Hkv * min((int64_t)s.max_cached + s.max_new, (int64_t)c.max_len) * HD * 2 > (256 << 20);
-    auto launch = [&](auto scores, auto streamed) {
-        hipLaunchKernelGGL((decode_kernel<HD, NT, decltype(scores)::value, decltype(streamed)::value>), grid, dim3(256), 0, st, c, s, a, sp);
+    auto launch = [&](auto mode) {
+        constexpr int SCORES = decltype(mode)::value;
+        const unsigned lds = SCORES == kScoresLds ? (unsigned)sp.lds_scores : 0u;
+        if (stream) hipLaunchKernelGGL((decode_kernel<HD, NT, SCORES, true>), grid, dim3(256), lds, st, c, s, a, sp);
+        else hipLaunchKernelGGL((decode_kernel<HD, NT, SCORES, false>), grid, dim3(256), lds, st, c, s, a, sp);
     };
-    if (a.weight_out != nullptr)
-        stream ? launch(std::true_type{}, std::true_type{}) : launch(std::true_type{}, std::false_type{});
-    else
-        stream ? launch(std::false_type{}, std::true_type{}) : launch(std::false_type{}, std::false_type{});
+    if (a.weight_out == nullptr) launch(std::integral_constant<int, kNoScores>{});
+    else if (sp.lds_scores > 0) launch(std::integral_constant<int, kScoresLds>{});
+    else launch(std::integral_constant<int, kScores>{});
 }
 
 template <int HD>
@@ -1001,8 +1026,12 @@ void launch_hd(hipStream_t st, const Cache& c, const Step& s, const Attend& a, c
         } else
             hipLaunchKernelGGL((prompt_kernel<HD, false>), grid, block, 0, st, c, s, a, p.sp, groups, p.each);
         if (p.sp.ranges > 1 && p.tiles > 0) {
-            const int64_t merges = pairs * p.sp.tile_rows, chunks = a.weight_out != nullptr ? (p.sp.score_stride + 255) / 256 : 0;
-            hipLaunchKernelGGL(finish_kernel<HD>, dim3((unsigned)(merges + pairs * chunks)), block, 0, st, c, s, a, p.sp, (int)merges, (int)chunks);
+            const bool wide = p.sp.ranges > 8;
+            const int64_t merges = wide ? pairs * p.sp.tile_rows : (pairs * p.sp.tile_rows + 3) / 4;
+            const int64_t chunks = a.weight_out != nullptr ? (p.sp.score_stride + 255) / 256 : 0;
+            const dim3 all((unsigned)(merges + pairs * chunks));
+            if (wide) hipLaunchKernelGGL((finish_kernel<HD, true>), all, block, 0, st, c, s, a, p.sp, (int)merges, (int)chunks);
+            else hipLaunchKernelGGL((finish_kernel<HD, false>), all, block, 0, st, c, s, a, p.sp, (int)merges, (int)chunks);
         } else if (p.sp.ranges > 1) {
             hipLaunchKernelGGL(merge_kernel<HD>, dim3((unsigned)((pairs * p.sp.tile_rows + 3) / 4)), block, 0, st, c, s, a, p.sp);
         }

@@ -587,7 +587,9 @@ def test_refusals_that_need_device_memory():
     refused(lambda: Q.attend(c, s, q, q.cpu()), B.MOE_ERR_INVALID_ARG, "device memory")
     refused(lambda: Q.attend(c, s, q, q, None, w), B.MOE_ERR_INVALID_ARG, "out may be q")
     refused(lambda: Q.attend(c, s, q, torch.zeros((2, 5, 64), dtype=torch.bfloat16, device=DEV)[:, :4], w, None), B.MOE_ERR_INVALID_ARG, "weight_in")
-    refused(lambda: Q.attend(c, s, q, q.clone(), w, w, torch.empty(16, dtype=torch.uint8, device=DEV)), B.MOE_ERR_OOM, "workspace")
+    long, far = Q.Kv8Cache.empty(2, 2, 64, 4096, 32, DEV), Q.Kv8Step(ints([3, 4]), 2, 1, 4000)
+    assert Q.attend_workspace_bytes(long, far, 4, False) > 16
+    refused(lambda: Q.attend(long, far, q, q.clone(), workspace=torch.empty(16, dtype=torch.uint8, device=DEV)), B.MOE_ERR_OOM, "workspace")
     refused(lambda: Q.evict(c, ints([3, 4]), 4, 32, 0, None, w, workspace=torch.empty(16, dtype=torch.uint8, device=DEV)), B.MOE_ERR_OOM, "workspace")
     assert lib.moe_kv8_append(None, c.ref, s.ref, k.data_ptr(), k.data_ptr(), -256, 64) == B.MOE_ERR_INVALID_ARG
     Q.append(c, s, k, k)                                                     # a refused call leaves everything usable

@@ -208,7 +208,8 @@ def test_refusals():
     refused(B.MOE_ERR_INVALID_ARG, "h_in", cache, step, x[:3], x, space)
     refused(B.MOE_ERR_INVALID_ARG, "device memory", cache, step, x.cpu(), x, space)
     wt = torch.zeros((4, kv, 64), device=DEV)
-    refused(B.MOE_ERR_OOM, "workspace", cache, step, x, x, torch.empty(16, dtype=torch.uint8, device=DEV), weight_out=wt)
+    long, far = Q.Kv8Cache.empty(4, kv, hd, 4096, 16, DEV), Q.Kv8Step(ints([0] * 4), 4, 1, 4000)
+    refused(B.MOE_ERR_OOM, "workspace", long, far, x, x, torch.empty(16, dtype=torch.uint8, device=DEV))
     refused(B.MOE_ERR_INVALID_ARG, "weight_in", cache, step, x, x, space, weight_in=wt)
     torch.cuda.synchronize()
     ctx.forward_kv8(cache, step, x, x, space)                                # a refused call leaves the context usable
