@@ -120,7 +120,7 @@ struct Select {
     float* weight_out;
     const int32_t* position_in;
     int32_t* position_out;
-    int32_t* sources;  // [pair, keep] chosen slots from `keep` on, in order
+    int32_t* sources;  // [pair, keep], of select_long_kernel: chosen slots from `keep` on, in order
     int32_t* kept;     // [pair, keep] slot that each slot was before
 };
 
@@ -135,6 +135,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_kernel(C
     constexpr int GROUPS = WAVES == 1 ? 4 : 1, LANES = WAVES * 64, CELLS = KPT * WAVES;
     __shared__ int counts[2][WAVES];
     __shared__ uint32_t cells[GROUPS][CELLS];
+    __shared__ uint16_t movers[GROUPS][KPT * LANES / 2];  // chosen slots from `keep` on, in order: at most half of all
     const int group = WAVES == 1 ? threadIdx.x >> 6 : 0, wave = WAVES == 1 ? 0 : threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int tid = wave * 64 + lane;
     const int64_t pair = (int64_t)blockIdx.x * GROUPS + group;
@@ -147,7 +148,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_kernel(C
     const int32_t* pin = a.position_in + at * c.max_len;
     float* wout = a.weight_out + at * c.max_len;
     int32_t* pout = a.position_out + at * c.max_len;
-    int32_t *list = a.sources + at * keep, *to = a.kept + at * keep;
+    uint16_t* list = movers[group];
+    int32_t* to = a.kept + at * keep;
     // positions from here on are recent; in 64 bits, since next - recent may pass the least int
     const int64_t young = (int64_t)(a.next_position != nullptr ? a.next_position[seq] : n) - a.recent;
     uint32_t key[KPT];
@@ -241,9 +243,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_kernel(C
         const int i = j * LANES + tid;
         const bool in = chosen[j] >> lane & 1;
         const uint64_t sources = __ballot(cut && i >= keep && in);
-        if (cut && i >= keep && in) list[(cells[group][j * WAVES + wave] >> 16) + __popcll(sources & below)] = i;
+        if (cut && i >= keep && in) list[(cells[group][j * WAVES + wave] >> 16) + __popcll(sources & below)] = (uint16_t)i;
     }
-    __syncthreads();  // the list is there (of this workgroup's own pairs)
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < KPT; ++j) {
         const int i = j * LANES + tid;
@@ -333,50 +335,76 @@ __global__ __launch_bounds__(256) void select_long_kernel(Cache c, Select a) {
     }
 }
 
-// One wavefront per (sequence, head, block below `keep`, K or V): the codes that move into it, 16 bytes per lane.
+// One workgroup per (sequence, head) and 512 slots below `keep`: which of them moved, what that makes of the scales of their
+// blocks, then the codes, 16 bytes per lane, those of K by half the threads and those of V by the others.  A block whose
+// scale rises is rounded again as a whole.  Bound by latency (few slots of a block move): 4096 pairs of 8 blocks took
+// 47 us with a wavefront per block.
+constexpr int kSpan = 512;
 template <int HD>
 __global__ __launch_bounds__(256) void move_kernel(Cache c, int keep, const int32_t* kept) {
-    constexpr int LPS = HD / 16, SIDE = 64 / LPS;  // lanes per slot, slots side by side
-    const int blocks = keep >> c.logb, B = 1 << c.logb, lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), of = item >> 1;
-    const int64_t pair = of / blocks;
-    if (pair >= (int64_t)c.n_seq * c.Hkv) return;
-    const int block = (int)(of % blocks), kv = (int)(item & 1);
-    const int32_t* list = kept + pair * keep + (block << c.logb);
-    const int f0 = lane < B ? list[lane] : -1, f1 = lane + 64 < B ? list[lane + 64] : -1;
-    if (!__any(f0 >= keep || f1 >= keep)) return;
-    float* scale = c.scale[kv] + pair * (c.max_len >> c.logb);
-    u32x4* codes = (u32x4*)(c.codes[kv] + pair * c.max_len * HD);
-    const float before = scale[block];
-    const float s0 = f0 >= keep ? scale[f0 >> c.logb] : before, s1 = f1 >= keep ? scale[f1 >> c.logb] : before;
-    float now = fmaxf(s0, s1);
+    constexpr int LPS = HD / 16, SIDE = 128 / LPS, AHEAD = 4;  // lanes per slot, slots side by side, pieces on their way
+    __shared__ int n_moved;
+    __shared__ int32_t slots[kSpan], from[kSpan];   // slots that moved, and where they come from
+    __shared__ uint32_t now[2][kSpan / 16];         // scales of K and V, as bits: positive, so they order as integers
+    __shared__ float was[2][kSpan / 16];
+    const int spans = (keep + kSpan - 1) / kSpan, tid = threadIdx.x;
+    const int64_t pair = blockIdx.x / spans;
+    const int s0 = (int)(blockIdx.x % spans) * kSpan, n = min(kSpan, keep - s0), blocks = n >> c.logb;
+    const int32_t* list = kept + pair * keep + s0;
+    const int64_t sb = pair * (c.max_len >> c.logb);
+    if (tid == 0) n_moved = 0;
+    if (tid < 2 * blocks) {
+        const int kv = tid >= blocks, b = tid - kv * blocks;
+        const float x = c.scale[kv][sb + (s0 >> c.logb) + b];
+        was[kv][b] = x;
+        now[kv][b] = __float_as_uint(x);
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += 256) {
+        const int f = list[i];
+        if (f < keep) continue;
+        const int at = atomicAdd(&n_moved, 1);  // in any order: every slot is moved by itself
+        slots[at] = i;
+        from[at] = f;
 #pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) now = fmaxf(now, __shfl_xor(now, m, 64));
-    now = fmaxf(now, before);
-    if (lane == 0) scale[block] = now;
-    const float b0 = s0 / now, b1 = s1 / now;  // powers of two
-    constexpr int AHEAD = 4;  // pieces on their way per lane
-    for (int i = 0; i < B; i += AHEAD * SIDE) {
+        for (int kv = 0; kv < 2; ++kv) atomicMax(&now[kv][i >> c.logb], __float_as_uint(c.scale[kv][sb + (f >> c.logb)]));
+    }
+    __syncthreads();
+    const int moved = n_moved;
+    if (moved == 0) return;
+    const int kv = tid >> 7, lane = tid & 127;
+    u32x4* codes = (u32x4*)(c.codes[kv] + pair * c.max_len * HD);
+    for (int i = lane / LPS; i < moved; i += SIDE * AHEAD) {
         u32x4 x[AHEAD];
         float by[AHEAD];
-        bool moves[AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const int slot = i + u * SIDE + lane / LPS;
-            const int fa = __shfl(f0, slot & 63, 64), fb = __shfl(f1, slot & 63, 64);
-            const float ba = __shfl(b0, slot & 63, 64), bb = __shfl(b1, slot & 63, 64);
-            const int from = slot < 64 ? fa : fb;
-            by[u] = slot < 64 ? ba : bb;
-            moves[u] = slot < B && from >= 0 && (from >= keep || by[u] != 1.f);
-            if (moves[u]) x[u] = codes[(int64_t)from * LPS + lane % LPS];
+        for (int u = 0; u < AHEAD; ++u) {  // past the end: the last one again, unused
+            const int f = from[min(i + u * SIDE, moved - 1)];
+            x[u] = codes[(int64_t)f * LPS + lane % LPS];
+            by[u] = c.scale[kv][sb + (f >> c.logb)];
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            if (!moves[u]) continue;
+            if (i + u * SIDE >= moved) break;
+            const int slot = slots[i + u * SIDE];
+            by[u] /= __uint_as_float(now[kv][slot >> c.logb]);  // powers of two
             if (by[u] != 1.f)
 #pragma unroll
                 for (int w = 0; w < 4; ++w) x[u][w] = rescale4(x[u][w], by[u]);
-            codes[((int64_t)(block << c.logb) + i + u * SIDE + lane / LPS) * LPS + lane % LPS] = x[u];
+            codes[(int64_t)(s0 + slot) * LPS + lane % LPS] = x[u];
+        }
+    }
+    for (int b = 0; b < blocks; ++b) {
+        const float to = __uint_as_float(now[kv][b]), by = was[kv][b] / to;
+        if (by == 1.f) continue;
+        if (lane == 0) c.scale[kv][sb + (s0 >> c.logb) + b] = to;
+        for (int i = (b << c.logb) + lane / LPS; i < (b + 1) << c.logb; i += SIDE) {  // slots that stayed
+            if (list[i] != s0 + i) continue;
+            const int64_t at = (int64_t)(s0 + i) * LPS + lane % LPS;
+            u32x4 x = codes[at];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) x[w] = rescale4(x[w], by);
+            codes[at] = x;
         }
     }
 }
@@ -412,7 +440,7 @@ void launch_evict(hipStream_t st, const Cache& c, const int32_t* held, int max_h
     else if (most <= 16384) hipLaunchKernelGGL((select_kernel<16, 16>), dim3(p), dim3(1024), 0, st, c, a);
     else hipLaunchKernelGGL(select_long_kernel, dim3(p), dim3(256), 0, st, c, a);
     if (max_held <= keep) return;
-    const dim3 grid((unsigned)((pairs * (keep >> c.logb) * 2 + 3) / 4)), block(256);
+    const dim3 grid((unsigned)(pairs * ((keep + kSpan - 1) / kSpan))), block(256);
     if (c.hd == 32) hipLaunchKernelGGL(move_kernel<32>, grid, block, 0, st, c, keep, kept);
     if (c.hd == 64) hipLaunchKernelGGL(move_kernel<64>, grid, block, 0, st, c, keep, kept);
     if (c.hd == 128) hipLaunchKernelGGL(move_kernel<128>, grid, block, 0, st, c, keep, kept);
