@@ -111,6 +111,14 @@ __device__ __forceinline__ uint32_t scan256(uint32_t v, uint32_t* total, uint32_
     return before + inc - v;
 }
 
+// Sum over the 16 lanes of a row, in every lane.
+__device__ __forceinline__ int row16_sum(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x128, 0xf, 0xf, false);  // row_ror by 8, 4, 2, 1
+    v += __builtin_amdgcn_update_dpp(0, v, 0x124, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x122, 0xf, 0xf, false);
+    return v + __builtin_amdgcn_update_dpp(0, v, 0x121, 0xf, 0xf, false);
+}
+
 // What a (sequence, head) pair selects from and writes to.
 struct Select {
     const int32_t* held;
@@ -132,6 +140,7 @@ struct Select {
 // The halving ends as soon as a bound parts off just `keep` keys, after 20 steps or so where weights differ.
 template <int WAVES, int KPT>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_kernel(Cache c, Select a) {
+    static_assert(WAVES == 1 || WAVES == 16);
     constexpr int GROUPS = WAVES == 1 ? 4 : 1, LANES = WAVES * 64, CELLS = KPT * WAVES;
     __shared__ int counts[2][WAVES];
     __shared__ uint32_t cells[GROUPS][CELLS];
@@ -153,11 +162,17 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_kernel(C
     // positions from here on are recent; in 64 bits, since next - recent may pass the least int
     const int64_t young = (int64_t)(a.next_position != nullptr ? a.next_position[seq] : n) - a.recent;
     uint32_t key[KPT];
+    {  // unconditional reads (past n the last slot again), so that all are on their way at once
+        float w[KPT];
+        int32_t pos[KPT];
 #pragma unroll
-    for (int j = 0; j < KPT; ++j) {
-        const int i = j * LANES + tid;
-        key[j] = 0;
-        if (cut && i < n) key[j] = key_of(win[i], a.recent > 0 && pin[i] >= young);
+        for (int j = 0; j < KPT; ++j) {
+            const int i = clampi(j * LANES + tid, 0, max(n - 1, 0));
+            w[j] = win[i];
+            pos[j] = pin[i];
+        }
+#pragma unroll
+        for (int j = 0; j < KPT; ++j) key[j] = cut && j * LANES + tid < n ? key_of(w[j], a.recent > 0 && pos[j] >= young) : 0u;
     }
     // keys past n count as 0, the least there is: they are told apart by their slot
     int phase = 0;
@@ -168,8 +183,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_kernel(C
         if (WAVES > 1) {
             if (lane == 0) counts[phase][wave] = sum;
             __syncthreads();
-            sum = 0;
-            for (int w = 0; w < WAVES; ++w) sum += counts[phase][w];
+            sum = row16_sum(counts[phase][lane & 15]);  // WAVES == 16
             phase ^= 1;  // the next counts go elsewhere, so that one barrier is enough
         }
         return sum;
@@ -246,18 +260,27 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_kernel(C
         if (cut && i >= keep && in) list[(cells[group][j * WAVES + wave] >> 16) + __popcll(sources & below)] = (uint16_t)i;
     }
     __syncthreads();
+    // All reads before the writes, which may go to the same tensors: one wait instead of one per step.
+    int from[KPT];
+    float w[KPT];
+    int32_t pos[KPT];
 #pragma unroll
     for (int j = 0; j < KPT; ++j) {
         const int i = j * LANES + tid;
         const bool in = chosen[j] >> lane & 1;
         const uint64_t holes = __ballot(cut && i < keep && !in);
-        if (!exists || i >= keep) continue;
-        int from = i < n ? i : -1;
-        if (cut && !in) from = list[(cells[group][j * WAVES + wave] & 0xffffu) + __popcll(holes & below)];
-        to[i] = from;
-        if (from < 0) continue;
-        if (from != i || wout != win) wout[i] = win[from];
-        if (from != i || pout != pin) pout[i] = pin[from];
+        from[j] = i < keep && i < n ? i : -1;
+        if (cut && i < keep && !in) from[j] = list[(cells[group][j * WAVES + wave] & 0xffffu) + __popcll(holes & below)];
+        w[j] = win[max(from[j], 0)];
+        pos[j] = pin[max(from[j], 0)];
+    }
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) {
+        const int i = j * LANES + tid;
+        if (exists && i < keep) to[i] = from[j];
+        if (from[j] < 0) continue;
+        if (from[j] != i || wout != win) wout[i] = w[j];
+        if (from[j] != i || pout != pin) pout[i] = pos[j];
     }
 }
 
@@ -437,6 +460,7 @@ void launch_evict(hipStream_t st, const Cache& c, const int32_t* held, int max_h
     else if (most <= 768) hipLaunchKernelGGL((select_kernel<1, 12>), dim3(p4), dim3(256), 0, st, c, a);
     else if (most <= 1024) hipLaunchKernelGGL((select_kernel<1, 16>), dim3(p4), dim3(256), 0, st, c, a);
     else if (most <= 4096) hipLaunchKernelGGL((select_kernel<16, 4>), dim3(p), dim3(1024), 0, st, c, a);
+    else if (most <= 8192) hipLaunchKernelGGL((select_kernel<16, 8>), dim3(p), dim3(1024), 0, st, c, a);
     else if (most <= 16384) hipLaunchKernelGGL((select_kernel<16, 16>), dim3(p), dim3(1024), 0, st, c, a);
     else hipLaunchKernelGGL(select_long_kernel, dim3(p), dim3(256), 0, st, c, a);
     if (max_held <= keep) return;
