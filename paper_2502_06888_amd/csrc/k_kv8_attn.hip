@@ -908,16 +908,22 @@ __global__ __launch_bounds__(256, 4) void prompt_weights_kernel(Cache c, Step s,
         }
     }
     wait_copies<0>();
+    // Sums over the 32 lanes of a row of registers: each step hands half of a lane's registers to its partner, so that 16 exchanges
+    // do (each register through all lanes would be 80).  Lane l ends up with the slot of register l/2 % 16.
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        float x = w[i];
+    for (int half = 8; half >= 1; half /= 2) {
+        const bool up = (lane & 2 * half) != 0;
 #pragma unroll
-        for (int m = 1; m < 32; m <<= 1) x += __shfl_xor(x, m, 64);
-        const int slot = j0 + row_of(i, grp);
-        if (col == i && slot < total) {
-            if (a.weight_in != nullptr && slot < q.cached) x += a.weight_in[base + slot];
-            a.weight_out[base + slot] = x;
+        for (int i = 0; i < half; ++i) {
+            const float keep = up ? w[i + half] : w[i], give = up ? w[i] : w[i + half];
+            w[i] = keep + __shfl_xor(give, 2 * half, 64);
         }
+    }
+    float x = w[0] + __shfl_xor(w[0], 1, 64);
+    const int slot = j0 + row_of(col >> 1, grp);
+    if ((col & 1) == 0 && slot < total) {
+        if (a.weight_in != nullptr && slot < q.cached) x += a.weight_in[base + slot];
+        a.weight_out[base + slot] = x;
     }
 }
 
