@@ -434,10 +434,15 @@ __global__ __launch_bounds__(256) void move_kernel(Cache c, int keep, const int3
 
 }  // namespace
 
+// Blocks that max_new tokens can fall into, and units of K and V over all pairs.
+static int append_blocks(const Cache& c, const Step& s) { return (s.max_new + (1 << c.logb) - 2) / (1 << c.logb) + 1; }
+static int64_t append_units(const Cache& c, const Step& s) { return (int64_t)c.n_seq * c.Hkv * 2 * append_blocks(c, s); }
+
+bool append_fits(const Cache& c, const Step& s) { return append_units(c, s) <= kMostGroups; }
+
 void launch_append(hipStream_t st, const Cache& c, const Step& s, const Rows& k, const Rows& v) {
-    const int B = 1 << c.logb;
-    const int blocks = (s.max_new + B - 2) / B + 1;  // blocks that max_new tokens can fall into
-    const int64_t units = (int64_t)c.n_seq * c.Hkv * 2 * blocks;
+    const int blocks = append_blocks(c, s);
+    const int64_t units = append_units(c, s);
     if (s.max_new <= 4)
         hipLaunchKernelGGL(append_kernel<1>, dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st, c, s, k, v, blocks);
     else
@@ -445,6 +450,9 @@ void launch_append(hipStream_t st, const Cache& c, const Step& s, const Rows& k,
 }
 
 static int64_t up256(int64_t v) { return (v + 255) & ~(int64_t)255; }
+
+static int64_t spans(const Cache& c, int keep) { return (int64_t)c.n_seq * c.Hkv * ((keep + kSpan - 1) / kSpan); }
+bool evict_fits(const Cache& c, int keep) { return spans(c, keep) <= kMostGroups; }
 
 int64_t evict_workspace(const Cache& c, int keep) { return 2 * up256((int64_t)c.n_seq * c.Hkv * keep * 4); }
 
@@ -464,7 +472,7 @@ void launch_evict(hipStream_t st, const Cache& c, const int32_t* held, int max_h
     else if (most <= 16384) hipLaunchKernelGGL((select_kernel<16, 16>), dim3(p), dim3(1024), 0, st, c, a);
     else hipLaunchKernelGGL(select_long_kernel, dim3(p), dim3(256), 0, st, c, a);
     if (max_held <= keep) return;
-    const dim3 grid((unsigned)(pairs * ((keep + kSpan - 1) / kSpan))), block(256);
+    const dim3 grid((unsigned)spans(c, keep)), block(256);
     if (c.hd == 32) hipLaunchKernelGGL(move_kernel<32>, grid, block, 0, st, c, keep, kept);
     if (c.hd == 64) hipLaunchKernelGGL(move_kernel<64>, grid, block, 0, st, c, keep, kept);
     if (c.hd == 128) hipLaunchKernelGGL(move_kernel<128>, grid, block, 0, st, c, keep, kept);

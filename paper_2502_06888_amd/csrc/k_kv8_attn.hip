@@ -12,7 +12,7 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kEmpty = -1.0e30f;  // finite stand-in for "no slot seen yet"
+constexpr float kEmpty = -3.0e38f;  // finite stand-in for "no slot seen yet", below any score of finite q and K that is finite
 // The reference of a running softmax lies kAbove over the largest score at the time it was set, and is set anew once a
 // score comes closer than kNear: the sums are not rescaled for every new maximum, and as weights stay below 2^-kNear,
 // the sums of 2^20 slots of any finite values stay finite.
@@ -1054,7 +1054,7 @@ bool attend_fits(const Cache& c, const Step& s, int Hq) {
     const Plan p = plan(c, s, Hq, true);
     const int64_t pairs = (int64_t)c.n_seq * c.Hkv;
     const int64_t most = pairs * p.sp.ranges * (p.tiles > 0 ? 1 : p.row_tiles);
-    return most <= 0x7fffffff && pairs * p.sp.tile_rows + pairs * ((p.sp.score_stride + kWeightSlots - 1) / kWeightSlots) <= 0x7fffffff;
+    return most <= kMostGroups && pairs * p.sp.tile_rows + pairs * ((p.sp.score_stride + kWeightSlots - 1) / kWeightSlots) <= kMostGroups;
 }
 
 int64_t attend_workspace(const Cache& c, const Step& s, int Hq, bool weights) { return plan(c, s, Hq, weights).bytes; }

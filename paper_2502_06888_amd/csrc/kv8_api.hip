@@ -149,8 +149,7 @@ moe_status check_append(const moe_kv8_cache* cache, const moe_kv8_step* step, co
     if (step->n_rows == 0) return MOE_OK;
     TRY(check_rows(k_new, "k_new", row_stride, head_stride, &w));
     TRY(check_rows(v_new, "v_new", row_stride, head_stride, &w));
-    const int64_t blocks = (step->max_new + cache->block - 2) / cache->block + 1;
-    if ((int64_t)cache->n_seq * cache->n_kv_heads * 2 * blocks > 0x7fffffff) return fail(MOE_ERR_SHAPE, "too many blocks: bring fewer sequences or tokens at once");
+    if (!append_fits(cache_of(cache), step_of(step))) return fail(MOE_ERR_SHAPE, "too many workgroups: bring fewer sequences or tokens at once");
     return MOE_OK;
 }
 
@@ -263,6 +262,7 @@ moe_status moe_kv8_evict_workspace_bytes(const moe_kv8_cache* cache, int32_t kee
     if (!bytes_out) return fail(MOE_ERR_INVALID_ARG, "bytes_out is null");
     TRY(check_sizes(cache));
     TRY(check_keep(cache, keep));
+    if (!evict_fits(cache_of(cache), keep)) return fail(MOE_ERR_SHAPE, "too many workgroups: evict from fewer sequences at once");
     *bytes_out = evict_workspace(cache_of(cache), keep);
     return MOE_OK;
 }
@@ -284,8 +284,8 @@ moe_status moe_kv8_evict(void* stream, const moe_kv8_cache* cache, const int32_t
     if (position_out) TRY(w.on(position_out, "position_out", 4));
     if (kept) TRY(w.on(kept, "kept", 4));
     const Cache c = cache_of(cache);
+    if (!evict_fits(c, keep)) return fail(MOE_ERR_SHAPE, "too many workgroups: evict from fewer sequences at once");
     TRY(check_workspace(workspace, workspace_bytes, evict_workspace(c, keep), &w));
-    if ((int64_t)c.n_seq * c.Hkv * (keep >> c.logb) > 0x7fffffff) return fail(MOE_ERR_SHAPE, "too many blocks");
     OnDevice on(w.device);
     if (on.failed()) return fail(MOE_ERR_HIP, "device %d cannot be made current", w.device);
     launch_evict((hipStream_t)stream, c, held, max_held, keep, recent, next_position, weight_in, weight_out,

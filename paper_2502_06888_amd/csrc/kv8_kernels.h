@@ -42,9 +42,15 @@ struct Attend {
     uint8_t* ws;
 };
 
-void launch_append(hipStream_t st, const Cache& c, const Step& s, const Rows& k, const Rows& v);
-// Whether the grids of launch_attend stay within what a launch can have.
+// Workgroups of 256 threads of a launch, at most: it counts its threads in 32 bits.
+constexpr int64_t kMostGroups = (1 << 24) - 1;
+
+// Whether the grids of the launches stay within that.
+bool append_fits(const Cache& c, const Step& s);
+bool evict_fits(const Cache& c, int keep);
 bool attend_fits(const Cache& c, const Step& s, int Hq);
+
+void launch_append(hipStream_t st, const Cache& c, const Step& s, const Rows& k, const Rows& v);
 int64_t attend_workspace(const Cache& c, const Step& s, int Hq, bool weights);
 void launch_attend(hipStream_t st, const Cache& c, const Step& s, const Attend& a);
 int64_t evict_workspace(const Cache& c, int keep);

@@ -567,6 +567,41 @@ def test_numbers_outside_their_bounds_stay_inside_the_tensors():
             assert bool((f[:guard] == 77).all()) and bool((f[-guard:] == 77).all())
 
 
+def test_offsets_beyond_32_bits():
+    """The last sequence of a cache of 5.4 GB for K alone."""
+    block, hd, kv, n, L, keep = 64, 128, 1, 41, 1 << 20, 128
+    g = torch.Generator().manual_seed(24)
+    cache = Q.Kv8Cache.empty(n, kv, hd, L, block, DEV)
+    tail = [t[-1:] for t in (cache.k, cache.v, cache.k_scale, cache.v_scale, cache.position)]
+    assert tail[0].data_ptr() - cache.k.data_ptr() > 1 << 32
+    small, codes, scale = filled(g, 1, kv, 192, hd, block, [150], poison=False)
+    small.position.copy_(torch.arange(192, dtype=torch.int32))
+    for t, o in zip(tail, (small.k, small.v, small.k_scale, small.v_scale, small.position)):
+        t[:, :, :o.shape[2]] = o
+    weight = torch.zeros((n, kv, L), device=DEV)
+    for new in (1, 40):
+        off = [0] * n + [new]
+        step = Q.Kv8Step(ints([0] * (n - 1) + [150]), new, new, 150, row_offsets=ints(off))
+        q, k, v = (rand(g, (new, h, hd)) for h in (2, kv, kv))
+        out = torch.zeros((new, 2, hd), dtype=torch.bfloat16, device=DEV)
+        Q.append(cache, step, k.to(DEV), v.to(DEV))
+        Q.attend(cache, step, q.to(DEV), out, None, weight)
+        for i, x in enumerate((k, v)):
+            R.append(codes[i], scale[i], x, [150], [0, new], block)
+        same(tail[0][:, :, :192], codes[0])
+        same(tail[1][:, :, :192], codes[1])
+        ref, w, spread, mag = R.attend(codes[0], scale[0], codes[1], scale[1], q, [150], [0, new], block)
+        assert bool(((out.cpu().double() - ref).abs() <= bounds(ref, spread, mag, hd)).all())
+        held = 150 + new
+        assert bool(((weight[-1, :, :held].cpu().double() - w[0, :, :held]).abs() <= weight_bounds(w, mag, hd)[0, :, :held]).all())
+    held, w_in = [0] * (n - 1) + [190], weight.cpu()[-1:]
+    pos = tail[4][:, :, :192].cpu()
+    Q.evict(cache, ints(held), 190, keep, 16, None, weight)
+    R.evict(codes, scale, w_in[:, :, :192], pos, [190], keep, 16, [190], block)
+    same(tail[0][:, :, :192], codes[0])
+    same(tail[1][:, :, :192], codes[1])
+
+
 def test_refusals_that_need_device_memory():
     c = Q.Kv8Cache.empty(2, 2, 64, 128, 32, DEV)
     s = Q.Kv8Step(ints([3, 4]), 2, 1, 4)

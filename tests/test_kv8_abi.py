@@ -76,6 +76,17 @@ def test_keep_is_a_number_of_whole_blocks(keep):
     assert e.value.status == B.MOE_ERR_INVALID_ARG
 
 
+def test_more_workgroups_than_a_launch_has_are_refused():
+    c, n = cache(), 1 << 20
+    c.c.n_seq, c.c.n_kv_heads, c.c.max_len = 65536, 16, n
+    for call in (lambda: Q.evict_workspace(c, n),
+                 lambda: Q.attend_workspace_bytes(c, Q.Kv8Step(ints(0), n, n, 0, row_offsets=ints(0, 1)), 16, True),
+                 lambda: Q.attend_workspace_bytes(c, Q.Kv8Step(ints(0), n, 1, n - 1, row_offsets=ints(0, 1)), 128, True)):
+        with pytest.raises(B.MoeError) as e:
+            call()
+        assert e.value.status == B.MOE_ERR_SHAPE and "workgroups" in e.value.message
+
+
 def test_null_arguments_and_host_tensors_are_refused():
     lib, c, s = Q.load_library(), cache(), Q.Kv8Step(ints(3, 4), 2, 1, 4)
     n = C.c_int64(0)
