@@ -8,7 +8,11 @@ namespace {
 //
 // One unit of WAVES wavefronts per (sequence, head, K or V, block of slots that the new tokens fall into): the largest
 // magnitude of the new rows, the scale, then the codes; the codes that the block held are rounded again only where the
-// scale rose.  A lane takes 16-byte pieces of the rows (8 elements) and writes 8 codes.
+// scale rose.  A lane takes 16-byte pieces of the rows (8 elements), keeps them in registers between the two uses, and
+// writes 8 codes.  Dividing by the scale is exact (a power of two), so a code has the one rounding to e4m3.
+// Bound by the bytes for prompts (32 x 512 tokens of 8 heads of 128: 101 MB in 23.5 us, 4.3 TB/s, 4.8 being what a large copy
+// reaches), by latency for single tokens (512 sequences: 7 us), where a unit is a wavefront: up to four tokens of 128
+// elements are one piece per lane.
 template <int WAVES>
 __global__ __launch_bounds__(256) void append_kernel(Cache c, Step s, Rows k, Rows v, int blocks) {
     constexpr int UNITS = 4 / WAVES, N = 64 * WAVES, PER = WAVES == 1 ? 1 : 8;
@@ -138,6 +142,7 @@ struct Select {
 // by ballots and one scan over the (step, wavefront) counts.  Reads weights and positions once: 4096 pairs of 576 slots
 // take one wavefront each; a few pairs of thousands of slots would leave the chip idle, so 16 wavefronts share one.
 // The halving ends as soon as a bound parts off just `keep` keys, after 20 steps or so where weights differ.
+// Bound by latency: 4096 pairs of 545 slots 19 us (45 MB), 32 pairs of 7500 slots 17 us.
 template <int WAVES, int KPT>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_kernel(Cache c, Select a) {
     static_assert(WAVES == 1 || WAVES == 16);
@@ -360,8 +365,8 @@ __global__ __launch_bounds__(256) void select_long_kernel(Cache c, Select a) {
 
 // One workgroup per (sequence, head) and 512 slots below `keep`: which of them moved, what that makes of the scales of their
 // blocks, then the codes, 16 bytes per lane, those of K by half the threads and those of V by the others.  A block whose
-// scale rises is rounded again as a whole.  Bound by latency (few slots of a block move): 4096 pairs of 8 blocks took
-// 47 us with a wavefront per block.
+// scale rises is rounded again as a whole.  Bound by latency (few slots of a block move): 4096 pairs of 8 blocks of which 31
+// slots move take 24 us (47 with a wavefront per block), 32 pairs of 64 blocks of which 1900 move 11.
 constexpr int kSpan = 512;
 template <int HD>
 __global__ __launch_bounds__(256) void move_kernel(Cache c, int keep, const int32_t* kept) {
@@ -464,6 +469,8 @@ void launch_evict(hipStream_t st, const Cache& c, const int32_t* held, int max_h
     const Select a{held, max_held, keep, recent, next_position, weight_in, weight_out, c.position, position_out, (int32_t*)ws, kept};
     const int most = max_held > keep ? max_held : keep;  // slots that the lanes have to cover
     const unsigned p = (unsigned)pairs, p4 = (unsigned)((pairs + 3) / 4);
+    // a wavefront per pair as long as 16 keys per lane do, then 16 of them, then from memory; no more keys per lane than
+    // needed, since the compares are what a step of the halving costs (8000 slots: 18 us with 8 keys per lane, 25 with 16)
     if (most <= 512) hipLaunchKernelGGL((select_kernel<1, 8>), dim3(p4), dim3(256), 0, st, c, a);
     else if (most <= 768) hipLaunchKernelGGL((select_kernel<1, 12>), dim3(p4), dim3(256), 0, st, c, a);
     else if (most <= 1024) hipLaunchKernelGGL((select_kernel<1, 16>), dim3(p4), dim3(256), 0, st, c, a);

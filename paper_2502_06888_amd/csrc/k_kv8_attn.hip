@@ -49,6 +49,9 @@ __device__ __forceinline__ void transpose4(const uint32_t (&a)[4], uint32_t (&o)
 //             weights never leave their lane: V is read by slots in that order, byte-transposed in registers.
 // A tile of 16 matrix rows serves 8 rows twice: the second half multiplies what rounding the weights to bf16 left over,
 // so the weights count with 16 bits at no matrix cost.
+// Bound by the bytes where there are enough of them: 512 sequences of 513 slots, 8 heads of 128 (538 MB of codes) take 90 us,
+// 6.0 TB/s; with the weights summed 114.  4 sequences of 7500 slots and 6 query heads per group (61 MB) take 15 us and 5 for
+// merge and weights, 1 of 701 slots 7 + 3: latency.
 constexpr int kRows = 128, kSlots = 64;  // rows and slots of a tile where there are many new tokens
 
 struct Split {
@@ -475,6 +478,12 @@ __global__ __launch_bounds__(256) void merge_kernel(Cache c, Step s, Attend a, S
 //
 // Where a tile serves many row tiles it is dequantised once, by pack_kernel, into the workspace in this order, and
 // comes from there into LDS without passing through registers; else the workgroup dequantises it on the way.
+// The weights are rounded once, to bf16, as the operand of the second product; their sum takes the unrounded ones.
+//
+// Two prompts of 3907 and 4096 tokens, 32 / 8 heads of 128: 258 us, 12 of them for dequantising ahead, 1.04 PFLOP/s (a large
+// library product of bf16 reaches 1.30 on this card): the matrix cores are busy 48 % of the time at the 2.0 GHz that the power
+// limit leaves, vector instructions (half of them exponentials) 60 %, two wavefronts per SIMD.  32 prompts of 512 tokens:
+// 130 us, 0.53 PFLOP/s and 2.3 TB/s: the start and end of a tile of rows weigh as much as its 4.5 steps.
 template <int HD>
 struct Tile {
     static constexpr int kUnits = HD / 8;            // of K, and of V
@@ -813,7 +822,8 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
 // The weights of 128 slots (32 per wavefront, K in registers) from all rows that see them: S^T again, then
 // exp2(score - reference) / sum with the row's statistics, which are the lane's; added up over the rows in the lane, over
 // the lanes at the end.  32 rows of q at a time come into LDS in the order of the matrix instructions, shared by the
-// wavefronts.  Bound by the exponentials and, next to them, the matrix cores.
+// wavefronts, three tiles ahead of their use.  Bound by the exponentials and, next to them, the matrix cores: 1941 tokens of 2
+// query heads per group over up to 6801 slots (39 GFLOP of the first product) 72 us.
 constexpr int kWeightSlots = 128;
 template <int HD>
 __global__ __launch_bounds__(256, 4) void prompt_weights_kernel(Cache c, Step s, Attend a, Split sp, int chunks) {
@@ -941,6 +951,8 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
     Plan p{};
     const int64_t pairs = (int64_t)c.n_seq * c.Hkv, rows = (int64_t)s.max_new * (Hq / c.Hkv);
     const int most = (int)min((int64_t)s.max_cached + s.max_new, (int64_t)c.max_len);
+    // decode_kernel up to 16 rows, the most whose sums its registers hold.  4 tokens of 4 query heads that way / as a prompt: 64
+    // sequences of 1000 slots 29 / 36 us, 512 of 512 146 / 163, 8 of 8000 32 / 39; 3 tokens of 512 with weights 165 / 340.
     p.tiles = rows == 0 ? 0 : rows <= 8 ? 1 : rows <= 16 ? 2 : 0;  // without rows prompt_weights_kernel carries the weights over
     p.row_tiles = (int)((rows + kRows - 1) / kRows);
     p.sp.tile_rows = p.tiles > 0 ? p.tiles * 8 : p.row_tiles * kRows;
@@ -989,7 +1001,8 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
     p.o_final = o;
     if (weights && p.tiles == 0) o += up256(pairs * p.sp.tile_rows * 8);
     p.o_packed = o;
-    // dequantised once where several row tiles use a tile, and the copy stays under 4 GiB
+    // Dequantised once where many row tiles use a tile, and the copy stays under 4 GiB.  Ahead / on the way: 32 prompts of 512
+    // (16 row tiles) 144 / 134 us, 16 of 1024 (32) 212 / 217, 8 of 2048 (64) 319 / 343, 1 of 4096 (128) 232 / 270.
     const int64_t tiles = (most + kSlots - 1) / kSlots, copy = pairs * tiles * kSlots * c.hd * 4;
     if (p.tiles == 0 && p.row_tiles >= 32 && copy <= (int64_t)4 << 30) {
         p.sp.packed_tiles = (int)tiles;
