@@ -11,6 +11,7 @@ using namespace kkv8;
 namespace {
 
 thread_local char g_error[256];
+constexpr double kLog2e = 1.4426950408889634;
 
 moe_status fail(moe_status s, const char* fmt, ...) {
     va_list ap;
@@ -160,7 +161,10 @@ moe_status check_attend(const moe_kv8_cache* cache, const moe_kv8_step* step, in
     TRY(check_sizes(cache));
     TRY(check_step_sizes(cache, step));
     TRY(check_heads(cache, n_q_heads));
-    if (!(softmax_scale >= 0.f) || std::isinf(softmax_scale)) return fail(MOE_ERR_INVALID_ARG, "softmax_scale must be finite and not negative");
+    if (!(softmax_scale >= 0.f) || std::isinf(softmax_scale * (float)kLog2e))
+        return fail(MOE_ERR_INVALID_ARG, "softmax_scale must be finite, times log2(e) too, and not negative");
+    if ((n_q_heads > 1 && out_head_stride < cache->head_dim) || (step->n_rows > 1 && out_row_stride < cache->head_dim))
+        return fail(MOE_ERR_INVALID_ARG, "strides of out are under head_dim: its rows or heads overlap");
     Where w;
     TRY(check_cache(cache, &w));
     TRY(check_step(step, &w));
@@ -193,7 +197,7 @@ moe_status check_layer_call(const moe_kv8_cache* cache, const moe_kv8_step* step
                             const float* weight_in, const float* weight_out, const void* workspace, int64_t workspace_bytes) {
     int device = 0;
     TRY(check_append(cache, step, rows, rows, 8, 8, &device));
-    return check_attend(cache, step, n_q_heads, rows, 8, 8, 0.f, (const uint8_t*)rows + 16, 8, 8, weight_in, weight_out, workspace,
+    return check_attend(cache, step, n_q_heads, rows, 8, 8, 0.f, (const uint8_t*)rows + 16, 128, 128, weight_in, weight_out, workspace,
                         workspace_bytes, &device);
 }
 
@@ -243,7 +247,7 @@ moe_status moe_kv8_attend(void* stream, const moe_kv8_cache* cache, const moe_kv
     const Step s = step_of(step);
     Attend a{};
     a.Hq = n_q_heads;
-    a.qscale = (float)(1.4426950408889634 * (softmax_scale == 0.f ? 1.0 / std::sqrt((double)c.hd) : (double)softmax_scale));
+    a.qscale = (float)(kLog2e * (softmax_scale == 0.f ? 1.0 / std::sqrt((double)c.hd) : (double)softmax_scale));
     a.q = Rows{(const uint16_t*)q, q_row_stride, q_head_stride};
     a.out = RowsOut{(uint16_t*)out, out_row_stride, out_head_stride};
     a.weight_in = weight_in;

@@ -105,9 +105,17 @@ def test_null_arguments_and_host_tensors_are_refused():
     assert b"position" in lib.moe_kv8_last_error()
     assert lib.moe_kv8_evict(None, cache().ref, None, 4, 32, 33, None, None, None, None, None, None, 0) == B.MOE_ERR_INVALID_ARG
     assert lib.moe_kv8_evict(None, cache().ref, None, 129, 32, 0, None, None, None, None, None, None, 0) == B.MOE_ERR_INVALID_ARG
-    for scale in (-1.0, float("nan"), float("inf")):
+    for scale in (-1.0, float("nan"), float("inf"), 3e38):                    # the last one overflows with log2(e)
         assert lib.moe_kv8_attend(None, cache().ref, s.ref, 4, None, 0, 0, scale, None, 0, 0, None, None, None, 0) == B.MOE_ERR_INVALID_ARG
         assert b"softmax_scale" in lib.moe_kv8_last_error()
+
+
+def test_outputs_whose_rows_or_heads_overlap_are_refused():
+    lib, c, s = Q.load_library(), cache(), Q.Kv8Step(ints(3, 4), 2, 1, 4)
+    x = torch.zeros((2, 4, 64), dtype=torch.bfloat16)
+    for row, head in ((0, 64), (256, 0), (64, 32), (56, 128)):
+        assert lib.moe_kv8_attend(None, c.ref, s.ref, 4, x.data_ptr(), 256, 64, 0.0, x.data_ptr(), row, head, None, None, None, 0) == B.MOE_ERR_INVALID_ARG
+        assert b"overlap" in lib.moe_kv8_last_error()
 
 
 def test_shapes_and_types_of_tensors_are_checked_by_the_binding():
