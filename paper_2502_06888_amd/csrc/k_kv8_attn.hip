@@ -12,11 +12,21 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kEmpty = -3.0e38f;  // finite stand-in for "no slot seen yet", below any score of finite q and K that is finite
+constexpr float kEmpty = -3.40282347e38f;  // finite stand-in for "no slot seen yet": the lowest number, not above any finite score
 // The reference of a running softmax lies kAbove over the largest score at the time it was set, and is set anew once a
 // score comes closer than kNear: the sums are not rescaled for every new maximum, and as weights stay below 2^-kNear,
 // the sums of 2^20 slots of any finite values stay finite.
 constexpr float kAbove = 28.f, kNear = 20.f;
+// score * factor - reference is one fused operation, whose product is exact while the reference comes from a rounded one.
+// That is half a step of the score, as any of its roundings; but from where a step is no longer small beside 1 the largest
+// score itself would be put far above or below its reference.  Beyond kFar the product is rounded first, by itself.
+constexpr float kFar = 0x1p18f;
+template <class T>
+__device__ __forceinline__ float near_factor(float reference, float factor, T&& scale_scores) {
+    if (!__any(fabsf(reference) > kFar)) return factor;
+    scale_scores();
+    return 1.f;
+}
 
 // The wavefront's number in its workgroup, in a scalar register.
 __device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
@@ -235,9 +245,13 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
                 }
             }
             float pr[8];
+            const float by = near_factor(m[n], a.qscale, [&] {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] *= a.qscale;
+            });
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                pr[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], a.qscale, -m[n]));
+                pr[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], by, -m[n]));
                 l[n] += pr[j];
             }
 #pragma unroll
@@ -324,10 +338,13 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
     }
     if (!SCORES || many > 1) return;
     __syncthreads();  // statistics and scores are there, those of this workgroup
+    float far = 0.f, first_by = 1.f;
+    for (int r = 0; r < rows; ++r) far = fmaxf(far, fabsf(done[r].x));
+    const float by = near_factor(far, a.qscale, [&] { first_by = a.qscale; });
     for (int j = threadIdx.x; j < len; j += 256) {
         float w = a.weight_in != nullptr && j < q.cached ? a.weight_in[base * c.max_len + j] : 0.f;
         for (int r = max(0, j - q.cached) * G; r < rows; ++r) {
-            w += __builtin_amdgcn_exp2f(__builtin_fmaf(scores[(int64_t)r * sp.score_stride + j], a.qscale, -done[r].x)) * done[r].y;
+            w += __builtin_amdgcn_exp2f(__builtin_fmaf(scores[(int64_t)r * sp.score_stride + j] * first_by, by, -done[r].x)) * done[r].y;
         }
         a.weight_out[base * c.max_len + j] = w;
     }
@@ -434,11 +451,14 @@ __global__ __launch_bounds__(256) void finish_kernel(Cache c, Step s, Attend a, 
         }
     __syncthreads();
     if (j >= len) return;
+    float far = 0.f, first_by = 1.f;
+    for (int r = 0; r < rows; ++r) far = fmaxf(far, fabsf(stat[r].x));
+    const float by = near_factor(far, a.qscale, [&] { first_by = a.qscale; });
     const int64_t at = (int64_t)pair * c.max_len + j;
     float w = a.weight_in != nullptr && j < q.cached ? a.weight_in[at] : 0.f;
     for (int r = max(0, j - q.cached) * G; r < rows; ++r) {
-        const float z = sp.scores[((int64_t)pair * sp.tile_rows + r) * sp.score_stride + j];
-        w += __builtin_amdgcn_exp2f(__builtin_fmaf(z, a.qscale, -stat[r].x)) * stat[r].y;
+        const float z = sp.scores[((int64_t)pair * sp.tile_rows + r) * sp.score_stride + j] * first_by;
+        w += __builtin_amdgcn_exp2f(__builtin_fmaf(z, by, -stat[r].x)) * stat[r].y;
     }
     a.weight_out[at] = w;
 }
@@ -742,13 +762,19 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
 #pragma unroll
                     for (int i = 0; i < 16; ++i) acc[m][i] *= f;
             }
+            const float by = near_factor(ref, a.qscale, [&] {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[t][i] *= a.qscale;
+            });
             u32x4 pf[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 float p[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u >> 1][(u & 1) * 8 + i], a.qscale, -ref));
+                    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u >> 1][(u & 1) * 8 + i], by, -ref));
                     sum += p[i];
                 }
 #pragma unroll
@@ -904,15 +930,19 @@ __global__ __launch_bounds__(256, 4) void prompt_weights_kernel(Cache c, Step s,
         for (int i = 0; i < 16; ++i) z[i] = 0.f;
 #pragma unroll
         for (int f = 0; f < F; ++f) z = mfma32(kf[f], qt[at][f * 64 + lane], z);
+        const float by = near_factor(e.x, a.qscale, [&] {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] *= a.qscale;
+        });
         if (r0 + 32 <= rows && r0 >= r_whole) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                w[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(z[i], a.qscale, -e.x)), e.y, w[i]);
+                w[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(z[i], by, -e.x)), e.y, w[i]);
         } else {
             const int within = r0 + col < rows ? q.cached + (r0 + col) / G + 1 - j0 - 4 * grp : 0;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], a.qscale, -e.x)) * e.y;
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], by, -e.x)) * e.y;
                 w[i] += row_of(i, 0) < within ? x : 0.f;
             }
         }

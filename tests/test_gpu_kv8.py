@@ -213,7 +213,10 @@ ATTENDS = [
     (64, 64, 64, 32, [3, 0, 100], [600, 580, 33]),
     (64, 128, 48, 16, [0, 5], [350, 400]),
     (32, 64, 8, 2, [60, 5, 0, 33], [0, 200, 0, 0]),                          # sequences without tokens before and behind
-    (32, 64, 128, 128, [0, 70, 64, 1], [250, 200, 129, 128]),               # two row tiles per pair, not dequantised ahead
+    (32, 64, 128, 128, [0, 70, 64, 1], [250, 200, 129, 128]),               # two row tiles per pair
+    (64, 128, 8, 1, [0, 37, 500], [530, 1, 450]),                            # 32 row tiles and more: dequantised ahead
+    (16, 64, 8, 1, [1, 900], [600, 33]),
+    (128, 32, 16, 2, [0, 70], [513, 515]),
 ]
 
 
@@ -279,6 +282,58 @@ def test_nan_codes_in_prompts_stay_with_those_who_see_them():
         nan[max(0, 70 - cached):, heads // kv:, 3] = True
         nan[300 - cached:, heads // kv:, 60] = True
         assert torch.equal(out.cpu().isnan(), nan)
+
+
+@pytest.mark.parametrize("hd,kv,cached", [(32, 1, 0), (64, 2, 75), (128, 1, 1100)])
+def test_nan_codes_dequantised_ahead_stay_with_those_who_see_them(hd, kv, cached):
+    """The same with 32 row tiles and more, in one range of slots and in several."""
+    block, heads, new = 32, 8 * kv, 520
+    g = torch.Generator().manual_seed(20)
+    cache, codes, scale = filled(g, 1, kv, 1664, hd, block, [cached + new])
+    for slot, e in ((70, 3), (cached + 300, hd - 4), (cached + new - 1, 0)):
+        cache.v[0, kv - 1, slot, e] = 0xff
+    q = rand(g, (new, heads, hd))
+    out = torch.zeros((new, heads, hd), dtype=torch.bfloat16, device=DEV)
+    Q.attend(cache, Q.Kv8Step(ints([cached]), new, new, cached), q.to(DEV), out)
+    nan = torch.zeros((new, heads, hd), dtype=torch.bool)
+    nan[max(0, 70 - cached):, -8:, 3] = True
+    nan[300:, -8:, hd - 4] = True
+    nan[-1:, -8:, 0] = True
+    assert torch.equal(out.cpu().isnan(), nan)
+
+
+@pytest.mark.parametrize("query,power,code,fifth", [
+    (-1.0625, 119, 0x7e, False),           # every score is -3.16e38, close to the lowest number
+    (1.0625 * 2.0 ** 60, 0, 0x7d, False),  # every score is 5.1e20
+    (1.0625 * 2.0 ** 30, 0, 0x7d, True),   # of every five slots the first wins by 4.8e11
+    (-1.0625 * 2.0 ** 60, 9, 0x7d, True),  # of every five slots the first is the only one that does not lose by 2.6e23
+])
+@pytest.mark.parametrize("cached,new", [(700, 1), (40, 4), (0, 150), (300, 520)])
+def test_equal_scores_of_any_size_share_alike(cached, new, query, power, code, fifth):
+    block, hd, heads, kv, L = 32, 32, 8, 1, 832
+    g = torch.Generator().manual_seed(21)
+    cache, codes, scale = filled(g, 1, kv, L, hd, block, [L], poison=False)
+    loses = torch.arange(L) % 5 != 0
+    codes[0][:] = 0
+    codes[0][..., 5] = torch.where(loses == (query < 0), code, 0) if fifth else code
+    cache.k.copy_(codes[0])
+    cache.k_scale.fill_(2.0 ** power)
+    q = torch.zeros((new, heads, hd), dtype=torch.bfloat16)
+    q[..., 5] = query
+    out = torch.zeros((new, heads, hd), dtype=torch.bfloat16, device=DEV)
+    w = torch.zeros((1, kv, L), device=DEV)
+    Q.attend(cache, Q.Kv8Step(ints([cached]), new, new, cached), q.to(DEV), out, None, w, softmax_scale=0.6875)
+    v = R.TABLE[codes[1][0, 0].long()] * scale[1][0, 0].repeat_interleave(block)[:, None]
+    want, mean = torch.zeros(L, dtype=torch.float64), torch.zeros((new, 1, hd), dtype=torch.float64)
+    for i in range(new):
+        share = (~loses if fifth else torch.ones(L)).double() * (torch.arange(L) <= cached + i)
+        share /= share.sum()
+        want += heads * share
+        mean[i, 0] = share @ v
+    # equal scores are equal in 32 bits too, and the others' weights are zero: what is left is the rounding of the weights and of
+    # the result, and sums in 32 bits
+    assert bool(((out.cpu().double() - mean).abs() <= 2.0 ** -8 * mean.abs() + (2.0 ** -8 + 2.0 ** -20) * v.abs().max()).all())
+    assert bool(((w[0, 0].cpu().double() - want).abs() <= 2.0 ** -18 * want).all())
 
 
 @pytest.mark.parametrize("cached,new", [(700, 1), (0, 150), (300, 5)])
