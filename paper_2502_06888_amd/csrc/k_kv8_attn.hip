@@ -977,6 +977,31 @@ struct Plan {
     int64_t o_ml, o_scores, o_final, o_packed, o_odd, bytes;
 };
 
+// Slots of a range where there are many new tokens: `rows` in about `tiles` row tiles, which see `most` slots at most.
+// More row tiles than compute units stay whole: 352 tiles of 8700 slots take 286 us, and 278 in the best of all splits; 384 of 8500
+// 271 and 274; 512 of 4000 to 6000 181 and 227.  Fewer are split into as many ranges as make one workgroup per unit, two, or two rounds
+// of two, by what a split costs in steps of kSlots of a workgroup alone on its unit: two run at 1.45 times that (1.6 and 2.3 us), each
+// has three more for its start and end, a merge costs a launch and fp32 sums written and read.  Whole / as chosen: 128 tiles of 8500
+// slots 213 / 96 us, 256 of 16500 409 / 321, 80 of 4300 110 / 46, 24 of 260 to 2060 32 / 15.
+int64_t prompt_range(int64_t most, int64_t tiles, int64_t rows) {
+    const int64_t steps = (most + kSlots - 1) / kSlots;
+    int64_t best = steps;
+    double least = (double)steps + 3.;
+    if (tiles > 256 || tiles < 1) return best * kSlots;
+    for (int fill = 1; fill <= 4 && steps >= 8; fill *= 2) {
+        int64_t n = 256 * fill / tiles;
+        n = n > steps / 4 ? steps / 4 : n;
+        const int64_t per = (steps + n - 1) / n, ranges = (steps + per - 1) / per, groups = tiles * ranges;
+        const double rounds = groups <= 512 ? 1. : (groups / 512. + (groups + 511) / 512) / 2;  // the last one not quite full
+        const double cost = (groups <= 256 ? 1. : 1.45 * rounds) * (double)(per + 3) + 1. + rows * ranges / (70. * kRows);
+        if (cost < least) {
+            least = cost;
+            best = per;
+        }
+    }
+    return best * kSlots;
+}
+
 Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
     Plan p{};
     const int64_t pairs = (int64_t)c.n_seq * c.Hkv, rows = (int64_t)s.max_new * (Hq / c.Hkv);
@@ -994,14 +1019,9 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
         per = ((int64_t)most * pairs / 512 + 127) / 128 * 128;
         per = per < 256 ? 256 : per;
     } else {
-        // Ranges only where the row tiles do not fill the chip (two workgroups per compute unit; half of that where most
-        // slots are the new tokens' own, so that many tiles see few): their fp32 sums, written and read, cost more than
-        // what they even out.  One prompt of 2048 tokens, 512 tiles: 54 us whole, 79-84 in ranges; one of 4096: 156 and 234.
-        // Two of 512 behind 16000 slots, 256 tiles: in 2 ranges 382, 3 331, 4 327, 5 334 us.
-        const int64_t tiles = pairs * p.row_tiles;
-        const bool fills = tiles >= 512 || (tiles >= 256 && s.max_cached <= s.max_new);
-        per = fills ? (most + kSlots) / kSlots * kSlots : (most * tiles / 1024 + kSlots - 1) / kSlots * kSlots;
-        per = per < 1024 ? 1024 : per;
+        const int64_t rows2 = 2 * s.n_rows * (int64_t)(Hq / c.Hkv) / kRows, about = (rows2 + c.n_seq + 1) / 2;  // half a tile over each
+        const int64_t tiles = c.Hkv * (about > c.n_seq ? about : (int64_t)c.n_seq);
+        per = prompt_range(most, min(pairs * p.row_tiles, tiles), s.n_rows * (int64_t)Hq);
     }
     const int64_t ranges = most > per ? (most + per - 1) / per : 1;
     p.sp.per = (int)per;

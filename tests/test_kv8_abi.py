@@ -87,6 +87,19 @@ def test_more_workgroups_than_a_launch_has_are_refused():
         assert e.value.status == B.MOE_ERR_SHAPE and "workgroups" in e.value.message
 
 
+@pytest.mark.parametrize("seqs,kv,heads", [(1, 1, 1), (2, 2, 8), (64, 8, 64)])
+def test_workspace_is_found_for_every_bound(seqs, kv, heads):
+    c = cache(n_seq=seqs, kv=kv, max_len=1 << 16)
+    for new in (0, 1, 4, 5, 17, 128, 1000, 65536):
+        for cached in (0, 1, 63, 2000, 65536):
+            for rows in sorted({min(new, 1), new, min(seqs * new, 1 << 20)}):
+                s = Q.Kv8Step(ints(*[0] * seqs), rows, new, cached, row_offsets=ints(*[0] * (seqs + 1)))
+                try:
+                    assert 0 <= Q.attend_workspace_bytes(c, s, heads, False) <= Q.attend_workspace_bytes(c, s, heads, True)
+                except B.MoeError as e:                                      # found, or refused: 64 prompts of up to 65536 tokens
+                    assert seqs * new > 1 << 20 and "workgroups" in e.message
+
+
 def test_null_arguments_and_host_tensors_are_refused():
     lib, c, s = Q.load_library(), cache(), Q.Kv8Step(ints(3, 4), 2, 1, 4)
     n = C.c_int64(0)
