@@ -76,6 +76,8 @@ struct Split {
     u32x4* packed;      // [pair, tile of kSlots] dequantised (see Tile), or null
     int32_t* odd;       // [pair, tile]
     int packed_tiles;   // tiles per pair
+    float* part;        // [split of the rows, pair, slot] weights of prompt_weights_kernel where it splits the rows
+    int splits;
 };
 
 template <bool STREAM, class T>
@@ -859,7 +861,7 @@ __global__ __launch_bounds__(256, 4) void prompt_weights_kernel(Cache c, Step s,
     __shared__ float2 ml[RING][32];
     const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, grp = lane >> 5;
     const int pairs = c.n_seq * c.Hkv;
-    const int pair = blockIdx.x % pairs, chunk = blockIdx.x / pairs;
+    const int pair = blockIdx.x % pairs, chunk = blockIdx.x / pairs % chunks, split = blockIdx.x / pairs / chunks;
     const int seq = pair / c.Hkv, hk = pair % c.Hkv, G = a.Hq / c.Hkv;
     const Seq q = sequence(c, s, seq);
     const int total = q.cached + q.n_new, rows = q.n_new * G;
@@ -882,7 +884,9 @@ __global__ __launch_bounds__(256, 4) void prompt_weights_kernel(Cache c, Step s,
     float w[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) w[i] = 0.f;
-    const int r_first = max(0, w0 - q.cached) * G / 32 * 32;
+    // tiles of 32 rows from the first that sees one of the slots on, those of this split
+    const int tile0 = max(0, w0 - q.cached) * G / 32, tiles = (rows + 31) / 32 - tile0;
+    const int r_first = (tile0 + tiles * split / sp.splits) * 32, r_end = (tile0 + tiles * (split + 1) / sp.splits) * 32;
     const uint32_t qt_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4*)&qt[0][0];
     const uint32_t ml_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float2*)&ml[0][0];
     const float* stats = (const float*)(sp.final_ml + (int64_t)pair * sp.tile_rows);
@@ -919,7 +923,7 @@ __global__ __launch_bounds__(256, 4) void prompt_weights_kernel(Cache c, Step s,
     }
     const int r_see = (j0 - q.cached) * G, r_whole = (j0 + 31 - q.cached) * G;  // first rows that see a slot of the wavefront, and all
     int at = 0;
-    for (int r0 = r_first; r0 < rows; r0 += 32, at = (at + 1) % RING) {
+    for (int r0 = r_first; r0 < r_end; r0 += 32, at = (at + 1) % RING) {
         wait_copies<(RING - 2) * (U + 1)>();  // all but the two youngest tiles
         __syncthreads();
         copy((at + RING - 1) % RING, r0 + (RING - 1) * 32);  // past the end: again, so that the count stays
@@ -962,9 +966,24 @@ __global__ __launch_bounds__(256, 4) void prompt_weights_kernel(Cache c, Step s,
     float x = w[0] + __shfl_xor(w[0], 1, 64);
     const int slot = j0 + row_of(col >> 1, grp);
     if ((col & 1) == 0 && slot < total) {
+        if (sp.splits > 1) {
+            sp.part[((int64_t)split * pairs + pair) * sp.score_stride + slot] = x;
+            return;
+        }
         if (a.weight_in != nullptr && slot < q.cached) x += a.weight_in[base + slot];
         a.weight_out[base + slot] = x;
     }
+}
+
+// Where the rows were split: what the splits gave each slot, in order.
+__global__ __launch_bounds__(256) void sum_weights_kernel(Cache c, Step s, Attend a, Split sp) {
+    const int pairs = c.n_seq * c.Hkv, pair = blockIdx.x % pairs, slot = blockIdx.x / pairs * 256 + (int)threadIdx.x;
+    const Seq q = sequence(c, s, pair / c.Hkv);
+    if (slot >= q.cached + q.n_new) return;
+    const int64_t at = (int64_t)pair * c.max_len + slot;
+    float w = a.weight_in != nullptr && slot < q.cached ? a.weight_in[at] : 0.f;
+    for (int i = 0; i < sp.splits; ++i) w += sp.part[((int64_t)i * pairs + pair) * sp.score_stride + slot];
+    a.weight_out[at] = w;
 }
 
 int64_t up256(int64_t v) { return (v + 255) & ~(int64_t)255; }
@@ -974,7 +993,7 @@ struct Plan {
     int tiles;  // row tiles of decode_kernel; 0: many new tokens, in `row_tiles` tiles of kRows
     int row_tiles, each;  // `each`: row tiles of a workgroup
     Split sp;
-    int64_t o_ml, o_scores, o_final, o_packed, o_odd, bytes;
+    int64_t o_ml, o_scores, o_final, o_part, o_packed, o_odd, bytes;
 };
 
 // Slots of a range where there are many new tokens: `rows` in about `tiles` row tiles, which see `most` slots at most.
@@ -1001,6 +1020,8 @@ int64_t prompt_range(int64_t most, int64_t tiles, int64_t rows) {
     }
     return best * kSlots;
 }
+
+int64_t weight_chunks(const Split& sp) { return (sp.score_stride + kWeightSlots - 1) / kWeightSlots; }
 
 Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
     Plan p{};
@@ -1049,7 +1070,18 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
         }
     }
     p.o_final = o;
-    if (weights && p.tiles == 0) o += up256(pairs * p.sp.tile_rows * 8);
+    p.sp.splits = 1;
+    if (weights && p.tiles == 0) {
+        o += up256(pairs * p.sp.tile_rows * 8);
+        // prompt_weights_kernel: where the slots alone make less than 450 workgroups the rows are split, too, down to eight tiles of
+        // 32; with 64 tiles and more per split up to 2048 workgroups, since those of late slots see few rows.  The whole call, not
+        // split / split: 1 prompt of 700 tokens of 16/2 heads 106 / 38 us, of 32/8 heads 77 / 41, of 4096 415 / 278, 2 of 4096
+        // 564 / 490; splits of four tiles and of two instead of eight: 700 tokens of 16/2 heads 42 and 53.
+        const int64_t groups = pairs * weight_chunks(p.sp), split = groups > 0 ? max(min(900 / groups, rows / 256), min(2048 / groups, rows / 2048)) : 1;
+        p.sp.splits = split > 1 ? (int)split : 1;
+    }
+    p.o_part = o;
+    if (p.sp.splits > 1) o += up256(p.sp.splits * pairs * p.sp.score_stride * 4);
     p.o_packed = o;
     // Dequantised once where many row tiles use a tile, and the copy stays under 4 GiB.  Ahead / on the way: 32 prompts of 512
     // (16 row tiles) 144 / 134 us, 16 of 1024 (32) 212 / 217, 8 of 2048 (64) 319 / 343, 1 of 4096 (128) 232 / 270.
@@ -1106,9 +1138,10 @@ void launch_hd(hipStream_t st, const Cache& c, const Step& s, const Attend& a, c
         }
     }
     if (a.weight_out == nullptr || p.tiles > 0) return;
-    const int chunks = (p.sp.score_stride + kWeightSlots - 1) / kWeightSlots;
-    if (chunks > 0)
-        hipLaunchKernelGGL(prompt_weights_kernel<HD>, dim3((unsigned)(pairs * chunks)), block, 0, st, c, s, a, p.sp, chunks);
+    const int chunks = (int)weight_chunks(p.sp);
+    if (chunks == 0) return;
+    hipLaunchKernelGGL(prompt_weights_kernel<HD>, dim3((unsigned)(pairs * chunks * p.sp.splits)), block, 0, st, c, s, a, p.sp, chunks);
+    if (p.sp.splits > 1) hipLaunchKernelGGL(sum_weights_kernel, dim3((unsigned)(pairs * ((p.sp.score_stride + 255) / 256))), block, 0, st, c, s, a, p.sp);
 }
 
 }  // namespace
@@ -1117,7 +1150,7 @@ bool attend_fits(const Cache& c, const Step& s, int Hq) {
     const Plan p = plan(c, s, Hq, true);
     const int64_t pairs = (int64_t)c.n_seq * c.Hkv;
     const int64_t most = pairs * p.sp.ranges * (p.tiles > 0 ? 1 : p.row_tiles);
-    return most <= kMostGroups && pairs * p.sp.tile_rows + pairs * ((p.sp.score_stride + kWeightSlots - 1) / kWeightSlots) <= kMostGroups;
+    return most <= kMostGroups && pairs * p.sp.tile_rows + pairs * weight_chunks(p.sp) <= kMostGroups;
 }
 
 int64_t attend_workspace(const Cache& c, const Step& s, int Hq, bool weights) { return plan(c, s, Hq, weights).bytes; }
@@ -1127,6 +1160,7 @@ void launch_attend(hipStream_t st, const Cache& c, const Step& s, const Attend& 
     p.sp.acc = (float*)a.ws;
     p.sp.ml = (float2*)(a.ws + p.o_ml);
     p.sp.scores = (float*)(a.ws + p.o_scores);
+    p.sp.part = (float*)(a.ws + p.o_part);
     p.sp.packed = (u32x4*)(a.ws + p.o_packed);
     p.sp.odd = (int32_t*)(a.ws + p.o_odd);
     p.sp.final_ml = a.weight_out != nullptr ? (float2*)(a.ws + p.o_final) : nullptr;
