@@ -833,7 +833,8 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
 #pragma unroll
             for (int i = 0; i < PPR / 2; ++i) {
                 const int in = i * APART + lane / PPR;
-                if (at < rows) *(u32x4*)o = mine[in * PPR + (lane % PPR ^ in % PPR)];
+                // past the caches, which K and V need: 32 prompts of 512 tokens 126 us instead of 130, 64 of 256 95 and 100
+                if (at < rows) __builtin_nontemporal_store(mine[in * PPR + (lane % PPR ^ in % PPR)], (u32x4*)o);
                 at += APART;
                 o += step;
                 g += step_g;
