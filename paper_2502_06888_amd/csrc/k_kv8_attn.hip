@@ -1040,6 +1040,10 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
         // 256 of 100 to 1500 96, 117, 149; 16 of 2000 19, 21, 21.
         per = ((int64_t)most * pairs / 512 + 127) / 128 * 128;
         per = per < 256 ? 256 : per;
+        // Short sequences whole, since that takes one launch.  1 sequence, heads of 128, in ranges / whole: 300 slots 9.9 / 7.9 us, 700
+        // 10.3 / 9.9, 1000 10.4 / 11.2, with weights 600 11.9 / 11.0, 700 11.1 / 11.8; of 64: 1500 11.1 / 10.9, with weights 1000 11.9 /
+        // 11.1; of 32: 1500 11.1 / 9.9, with weights 11.9 / 12.9.  48 sequences of 700: 21.7 / 16.1.
+        if (most <= (weights ? c.hd == 128 ? 640 : 1024 : c.hd == 128 ? 768 : 1536)) per = (most + 127) / 128 * 128;
     } else {
         const int64_t rows2 = 2 * s.n_rows * (int64_t)(Hq / c.Hkv) / kRows, about = (rows2 + c.n_seq + 1) / 2;  // half a tile over each
         const int64_t tiles = c.Hkv * (about > c.n_seq ? about : (int64_t)c.n_seq);

@@ -217,6 +217,11 @@ ATTENDS = [
     (64, 128, 8, 1, [0, 37, 500], [530, 1, 450]),                            # 32 row tiles and more: dequantised ahead
     (16, 64, 8, 1, [1, 900], [600, 33]),
     (128, 32, 16, 2, [0, 70], [513, 515]),
+    (32, 64, 8, 2, [1700, 3], [1, 1]),                                       # a few ranges of slots, and whole beside them
+    (64, 32, 4, 4, [1800, 1600, 0], [2, 1, 0]),
+    (64, 128, 8, 2, [900, 20], [4, 1]),                                      # 16 rows, and 12
+    (16, 64, 12, 3, [2000], [3]),
+    (64, 128, 16, 2, [4000, 130, 0], [5, 0, 3]),                             # 40 rows over many ranges
 ]
 
 
