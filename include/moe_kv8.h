@@ -85,7 +85,7 @@ moe_status moe_kv8_append(void* stream, const moe_kv8_cache* cache, const moe_kv
  *     step's tokens and the head's query heads gave it; weight_in may be weight_out.  Slots a sequence does
  *     not hold are left as they were.
  * Rows of no sequence are left as they were.  Scores, softmax and sums are kept in 32 bits.  The result of a
- * sequence does not depend on what the others hold; how its sums are split follows from the bounds of the launch
+ * sequence does not depend on what the others hold; how its sums are split follows from the numbers in the structs
  * and its own length.
  * workspace: moe_kv8_attend_workspace_bytes() of device memory, 256-byte aligned (may be null when that is 0).  It
  * depends on the sizes and bounds only.
