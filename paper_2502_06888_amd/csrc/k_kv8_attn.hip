@@ -52,7 +52,7 @@ __device__ __forceinline__ void transpose4(const uint32_t (&a)[4], uint32_t (&o)
 
 // ---- few new tokens: bound by the bytes of the cache ----------------------------------------------------
 //
-// One workgroup of four wavefronts per (sequence, key-value head, range of slots); all rows (token, query head of the
+// One workgroup of W wavefronts, four or eight, per (sequence, key-value head, range of slots); all rows (token, query head of the
 // group) of the pair share what is read, in tiles of 8.  A wavefront takes 32 slots at a time, in two tiles of 16:
 //   scores    S^T[slot][row] = K Q^T, 16x16x32: lane l holds row l%16 and slots 4*(l/16)..+3 of each tile;
 //   sums      O[row][element] = P V with the eight weights a lane holds as its eight steps of the reduction, so that the
@@ -71,6 +71,7 @@ struct Split {
     float* acc;         // [pair, range, row, hd] unnormalised sums; with float2 `ml` (reference, sum of weights)
     float2* ml;
     float* scores;      // [pair, row, slot] products q . K
+    int waves;          // of a workgroup of decode_kernel
     int lds_scores;     // bytes of LDS that hold those of a pair instead, 0: they are in `scores`
     float2* final_ml;   // [pair, row] with many new tokens: reference of all ranges, 1 / sum of weights
     u32x4* packed;      // [pair, tile of kSlots] dequantised (see Tile), or null
@@ -89,13 +90,13 @@ __device__ __forceinline__ T fetch(const T* p) {
 // Where the products q . K go: nowhere, to the workspace, or into LDS (where they fit and a sequence is one range).
 enum { kNoScores, kScores, kScoresLds };
 
-template <int HD, int NT, int SCORES, bool STREAM>
-__global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) void decode_kernel(Cache c, Step s, Attend a, Split sp) {
+template <int HD, int NT, int SCORES, bool STREAM, int W>
+__global__ __launch_bounds__(W * 64, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) void decode_kernel(Cache c, Step s, Attend a, Split sp) {
     constexpr int KW = HD / 16;             // words of a K row that a lane holds: HD/4 bytes
     constexpr int VT = HD / 16;             // tiles of 16 elements of the sums
     constexpr int VW = VT >= 4 ? VT / 4 : 1;  // words of a V row that a lane holds: VT bytes
-    __shared__ float sm_o[4][NT * 8][HD];
-    __shared__ float2 sm_ml[4][NT * 8], done[NT * 8];
+    __shared__ float sm_o[W][NT * 8][HD];
+    __shared__ float2 sm_ml[W][NT * 8], done[NT * 8];
     extern __shared__ __attribute__((aligned(16))) float lds_scores[];
     const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 15, grp = lane >> 4;
     const int range = blockIdx.x % sp.ranges, pair = blockIdx.x / sp.ranges;
@@ -107,7 +108,7 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
     const int many = (len + sp.per - 1) / sp.per;  // ranges of this sequence
     float* scores = SCORES == kScoresLds ? lds_scores : sp.scores + (int64_t)pair * sp.tile_rows * sp.score_stride;
     if (SCORES && rows == 0 && many <= 1 && range == 0)  // no new tokens: the weights stay
-        for (int j = threadIdx.x; j < len; j += 256) a.weight_out[base * c.max_len + j] = a.weight_in != nullptr ? a.weight_in[base * c.max_len + j] : 0.f;
+        for (int j = threadIdx.x; j < len; j += W * 64) a.weight_out[base * c.max_len + j] = a.weight_in != nullptr ? a.weight_in[base * c.max_len + j] : 0.f;
     if (rows == 0 || first >= end) return;
     const uint8_t *K = c.codes[0] + base * c.max_len * HD, *V = c.codes[1] + base * c.max_len * HD;
     const float *ks = c.scale[0] + base * (c.max_len >> c.logb), *vs = c.scale[1] + base * (c.max_len >> c.logb);
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
                 for (int f = 0; f < HD / 32; ++f) z[n][t] = mfma16(kf[f], qf[n][f], z[n][t]);
             }
         }
-        if (p0 + 128 < end) load_k(p0 + 128);
+        if (p0 + 32 * W < end) load_k(p0 + 32 * W);
         bool odd = false;
         if (!whole) {  // weight 0 times a NaN code would be NaN: such codes are taken out, and put back where they are seen
             uint32_t nan = 0;
@@ -278,7 +279,7 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
                 for (int n = 0; n < NT; ++n) acc[n][w * 4 + b] = mfma16(pf[n], vf, acc[n][w * 4 + b]);
             }
         }
-        if (p0 + 128 < end) load_v(p0 + 128);
+        if (p0 + 32 * W < end) load_v(p0 + 32 * W);
         if (odd) {
             for (int j = p0; j < min(p0 + 32, end); ++j)
 #pragma unroll
@@ -293,8 +294,8 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
         }
     };
     const int sure = min(end, q.cached + 1);
-    for (; p0 + 32 <= sure; p0 += 128) chunk(std::true_type{});
-    for (; p0 < end; p0 += 128) chunk(std::false_type{});
+    for (; p0 + 32 <= sure; p0 += 32 * W) chunk(std::true_type{});
+    for (; p0 < end; p0 += 32 * W) chunk(std::false_type{});
     // the lane groups of a column, the two halves of the weights, then the wavefronts
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -311,15 +312,15 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
     }
     __syncthreads();
     const int total = min(rows, NT * 8) * HD;
-    for (int i = threadIdx.x * 4; i < total; i += 1024) {
+    for (int i = threadIdx.x * 4; i < total; i += W * 256) {
         const int r = i / HD, d = i % HD;
         float mm = kEmpty;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sm_ml[w][r].x);
+        for (int w = 0; w < W; ++w) mm = fmaxf(mm, sm_ml[w][r].x);
         float ll = 0.f;
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < W; ++w) {
             const float f = __builtin_amdgcn_exp2f(sm_ml[w][r].x - mm);
             ll += sm_ml[w][r].y * f;
 #pragma unroll
@@ -343,7 +344,7 @@ __global__ __launch_bounds__(256, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2) vo
     float far = 0.f, first_by = 1.f;
     for (int r = 0; r < rows; ++r) far = fmaxf(far, fabsf(done[r].x));
     const float by = near_factor(far, a.qscale, [&] { first_by = a.qscale; });
-    for (int j = threadIdx.x; j < len; j += 256) {
+    for (int j = threadIdx.x; j < len; j += W * 64) {
         float w = a.weight_in != nullptr && j < q.cached ? a.weight_in[base * c.max_len + j] : 0.f;
         for (int r = max(0, j - q.cached) * G; r < rows; ++r) {
             w += __builtin_amdgcn_exp2f(__builtin_fmaf(scores[(int64_t)r * sp.score_stride + j] * first_by, by, -done[r].x)) * done[r].y;
@@ -1066,8 +1067,12 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
     if (weights && p.tiles > 0) {
         // The products stay in LDS where a sequence is one range and they fit the 64 KiB that a workgroup can have beside the
         // sums: 512 sequences of 513 slots 114 us instead of 137, 96 of up to 3002 (48 KB, two workgroups per unit) 52, not 63.
+        // From 32 KiB on, where few workgroups share a unit, they have eight wavefronts.  Four / eight: 96 of up to 3002 slots
+        // (48 KB) 53 / 41 us, 200 of 2101 (34 KB) 103 / 94, 256 of 1001 with 8 rows (33 KB) 69 / 64, 200 of up to 1701 (28 KB) 45 / 48.
         const int64_t stride = (most + 63) / 64 * 64 + 16, lds = rows * stride * 4;  // rows 16 banks apart
-        if (ranges == 1 && lds <= (64 << 10) - p.tiles * 8 * (16 * c.hd + 40)) {
+        const auto room = [&](int waves) { return (64 << 10) - p.tiles * 8 * (4 * waves * c.hd + 8 * waves + 8); };
+        if (ranges == 1 && lds <= room(4)) {
+            p.sp.waves = lds > (32 << 10) && lds <= room(8) ? 8 : 4;
             p.sp.score_stride = (int)stride;
             p.sp.lds_scores = (int)lds;
         } else {
@@ -1109,8 +1114,15 @@ void launch_decode(hipStream_t st, const dim3& grid, const Cache& c, const Step&
     auto launch = [&](auto mode) {
         constexpr int SCORES = decltype(mode)::value;
         const unsigned lds = SCORES == kScoresLds ? (unsigned)sp.lds_scores : 0u;
-        if (stream) hipLaunchKernelGGL((decode_kernel<HD, NT, SCORES, true>), grid, dim3(256), lds, st, c, s, a, sp);
-        else hipLaunchKernelGGL((decode_kernel<HD, NT, SCORES, false>), grid, dim3(256), lds, st, c, s, a, sp);
+        if constexpr (SCORES == kScoresLds && NT * HD <= 64) {  // with larger sums eight wavefronts leave no 32 KiB
+            if (sp.waves == 8) {
+                if (stream) hipLaunchKernelGGL((decode_kernel<HD, NT, SCORES, true, 8>), grid, dim3(512), lds, st, c, s, a, sp);
+                else hipLaunchKernelGGL((decode_kernel<HD, NT, SCORES, false, 8>), grid, dim3(512), lds, st, c, s, a, sp);
+                return;
+            }
+        }
+        if (stream) hipLaunchKernelGGL((decode_kernel<HD, NT, SCORES, true, 4>), grid, dim3(256), lds, st, c, s, a, sp);
+        else hipLaunchKernelGGL((decode_kernel<HD, NT, SCORES, false, 4>), grid, dim3(256), lds, st, c, s, a, sp);
     };
     if (a.weight_out == nullptr) launch(std::integral_constant<int, kNoScores>{});
     else if (sp.lds_scores > 0) launch(std::integral_constant<int, kScoresLds>{});

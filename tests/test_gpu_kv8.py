@@ -222,6 +222,9 @@ ATTENDS = [
     (64, 128, 8, 2, [900, 20], [4, 1]),                                      # 16 rows, and 12
     (16, 64, 12, 3, [2000], [3]),
     (64, 128, 16, 2, [4000, 130, 0], [5, 0, 3]),                             # 40 rows over many ranges
+    (16, 64, 512, 128, [2100, 700, 3, 0], [1, 1, 1, 1]),                     # scores of more than 32 KiB in LDS: one range of 512 pairs,
+    (32, 64, 16, 2, [999, 31, 500], [1, 0, 1]),                              # 8 rows of 1000 slots,
+    (64, 32, 10, 2, [600, 0, 697, 64], [3, 1, 2, 0]),                        # 15 rows of 700
 ]
 
 
