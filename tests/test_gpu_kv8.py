@@ -225,6 +225,7 @@ ATTENDS = [
     (16, 64, 512, 128, [2100, 700, 3, 0], [1, 1, 1, 1]),                     # scores of more than 32 KiB in LDS: one range of 512 pairs,
     (32, 64, 16, 2, [999, 31, 500], [1, 0, 1]),                              # 8 rows of 1000 slots,
     (64, 32, 10, 2, [600, 0, 697, 64], [3, 1, 2, 0]),                        # 15 rows of 700
+    (32, 32, 64, 64, [2000, 30], [203, 7]),                                  # ranges of many rows
 ]
 
 
