@@ -61,7 +61,7 @@ __device__ __forceinline__ void transpose4(const uint32_t (&a)[4], uint32_t (&o)
 // so the weights count with 16 bits at no matrix cost.
 // Bound by the bytes where there are enough of them: 512 sequences of 513 slots, 8 heads of 128 (538 MB of codes) take 90 us,
 // 6.0 TB/s; with the weights summed 114.  4 sequences of 7500 slots and 6 query heads per group (61 MB) take 15 us and 5 for
-// merge and weights, 1 of 701 slots 7 + 3: latency.
+// merge and weights, 1 of 701 slots 10: latency.
 constexpr int kRows = 128, kSlots = 64;  // rows and slots of a tile where there are many new tokens
 
 struct Split {
@@ -526,10 +526,10 @@ __global__ __launch_bounds__(256) void merge_kernel(Cache c, Step s, Attend a, S
 // comes from there into LDS without passing through registers; else the workgroup dequantises it on the way.
 // The weights are rounded once, to bf16, as the operand of the second product; their sum takes the unrounded ones.
 //
-// Two prompts of 3907 and 4096 tokens, 32 / 8 heads of 128: 258 us, 12 of them for dequantising ahead, 1.04 PFLOP/s (a large
+// Two prompts of 3907 and 4096 tokens, 32 / 8 heads of 128: 266 us, 9 of them for dequantising ahead, 1.01 PFLOP/s (a large
 // library product of bf16 reaches 1.30 on this card): the matrix cores are busy 48 % of the time at the 2.0 GHz that the power
 // limit leaves, vector instructions (half of them exponentials) 60 %, two wavefronts per SIMD.  32 prompts of 512 tokens:
-// 130 us, 0.53 PFLOP/s and 2.3 TB/s: the start and end of a tile of rows weigh as much as its 4.5 steps.
+// 128 us, 0.54 PFLOP/s and 2.4 TB/s: the start and end of a tile of rows weigh as much as its 4.5 steps.
 template <int HD>
 struct Tile {
     static constexpr int kUnits = HD / 8;            // of K, and of V
