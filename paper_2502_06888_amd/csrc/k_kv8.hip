@@ -97,8 +97,9 @@ __device__ __forceinline__ uint32_t key_of(float w, bool recent) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// Exclusive sum over the 256 threads of two counts packed into one word.
-__device__ __forceinline__ uint32_t scan256(uint32_t v, uint32_t* total, uint32_t* part) {
+// Exclusive sum over the workgroup's kLong threads of two counts packed into one word.
+constexpr int kLong = 1024;
+__device__ __forceinline__ uint32_t scan_long(uint32_t v, uint32_t* total, uint32_t* part) {
     uint32_t inc = v;
     const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -109,9 +110,14 @@ __device__ __forceinline__ uint32_t scan256(uint32_t v, uint32_t* total, uint32_
     __syncthreads();  // `part` may still be read from the call before
     if (lane == 63) part[threadIdx.x >> 6] = inc;
     __syncthreads();
-    uint32_t before = 0;
-    for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) before += part[w];
-    *total = part[0] + part[1] + part[2] + part[3];
+    uint32_t before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kLong / 64; ++w) {
+        const uint32_t p = part[w];
+        if (w < (int)(threadIdx.x >> 6)) before += p;
+        all += p;
+    }
+    *total = all;
     return before + inc - v;
 }
 
@@ -289,10 +295,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_kernel(C
     }
 }
 
-// The same for sequences of any length, 256 slots at a time: the key digit by digit (four passes over 8 bits), then the
-// chosen slots in order.
-__global__ __launch_bounds__(256) void select_long_kernel(Cache c, Select a) {
-    __shared__ uint32_t hist[256], part[4], found[2];
+// The same for sequences of any length, kLong slots at a time: the key digit by digit (four passes over 8 bits), then the
+// chosen slots in order.  Bound by latency: 8 pairs of 40000 slots, with the move, 129 us (by 256 threads 356), of 131072 364.
+__global__ __launch_bounds__(kLong) void select_long_kernel(Cache c, Select a) {
+    __shared__ uint32_t hist[256], part[kLong / 64], found[2];
     const int64_t pair = blockIdx.x;
     const int seq = (int)(pair / c.Hkv), tid = threadIdx.x, keep = a.keep;
     const int n = clampi(a.held[seq], 0, a.max_held);
@@ -303,7 +309,7 @@ __global__ __launch_bounds__(256) void select_long_kernel(Cache c, Select a) {
     int32_t* list = a.sources + pair * keep;
     int32_t* to = a.kept + pair * keep;
     if (n <= keep) {
-        for (int i = tid; i < keep; i += 256) {
+        for (int i = tid; i < keep; i += kLong) {
             to[i] = i < n ? i : -1;
             if (i < n) {
                 if (wout != win) wout[i] = win[i];
@@ -317,18 +323,18 @@ __global__ __launch_bounds__(256) void select_long_kernel(Cache c, Select a) {
     uint32_t prefix = 0;
     int want = keep;  // how many of the slots that share the prefix are chosen
     for (int shift = 24; shift >= 0; shift -= 8) {
-        hist[tid] = 0;
+        if (tid < 256) hist[tid] = 0;
         __syncthreads();
         const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
-        for (int i = tid; i < n; i += 256) {
+        for (int i = tid; i < n; i += kLong) {
             const uint32_t k = key(i);
             if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
         }
         __syncthreads();
         // thread t looks at digit 255 - t: how many lie above it
         uint32_t all;
-        const uint32_t mine = hist[255 - tid], above = scan256(mine, &all, part);
-        if (above < (uint32_t)want && above + mine >= (uint32_t)want) {
+        const uint32_t mine = tid < 256 ? hist[255 - tid] : 0u, above = scan_long(mine, &all, part);
+        if (tid < 256 && above < (uint32_t)want && above + mine >= (uint32_t)want) {
             found[0] = 255u - tid;
             found[1] = above;
         }
@@ -339,23 +345,23 @@ __global__ __launch_bounds__(256) void select_long_kernel(Cache c, Select a) {
     }
     // slots above the key are chosen, and the first `want` of those at it
     uint32_t ties = 0, moved = 0, holes = 0;
-    for (int base = 0; base < n; base += 256) {
+    for (int base = 0; base < n; base += kLong) {
         const int i = base + tid;
         const uint32_t k = i < n ? key(i) : 0u;
         const bool tie = i < n && k == prefix;
         uint32_t all;
-        const uint32_t rank = ties + scan256(tie ? 1u : 0u, &all, part);
+        const uint32_t rank = ties + scan_long(tie ? 1u : 0u, &all, part);
         ties += all;
         const bool chosen = i < n && (k > prefix || (tie && rank < (uint32_t)want));
         const bool hole = i < keep && !chosen, source = i >= keep && chosen;
-        const uint32_t at = scan256((hole ? 1u : 0u) | (source ? 1u << 16 : 0u), &all, part);
+        const uint32_t at = scan_long((hole ? 1u : 0u) | (source ? 1u << 16 : 0u), &all, part);
         if (source) list[moved + (at >> 16)] = i;
         if (i < keep) to[i] = hole ? -2 - (int)(holes + (at & 0xffffu)) : i;
         holes += all & 0xffffu;
         moved += all >> 16;
     }
     __syncthreads();
-    for (int i = tid; i < keep; i += 256) {
+    for (int i = tid; i < keep; i += kLong) {
         int from = to[i];
         if (from < 0) to[i] = from = list[-2 - from];
         if (from != i || wout != win) wout[i] = win[from];
@@ -469,7 +475,8 @@ void launch_evict(hipStream_t st, const Cache& c, const int32_t* held, int max_h
     const Select a{held, max_held, keep, recent, next_position, weight_in, weight_out, c.position, position_out, (int32_t*)ws, kept};
     const int most = max_held > keep ? max_held : keep;  // slots that the lanes have to cover
     const unsigned p = (unsigned)pairs, p4 = (unsigned)((pairs + 3) / 4);
-    // a wavefront per pair as long as 16 keys per lane do, then 16 of them, then from memory; no more keys per lane than
+    // a wavefront per pair as long as 16 keys per lane do, then 16 of them up to 32 keys per lane (8 pairs of 32000 slots, with the
+    // move, 60 us, from memory by 256 threads 290), then from memory; no more keys per lane than
     // needed, since the compares are what a step of the halving costs (8000 slots: 18 us with 8 keys per lane, 25 with 16)
     if (most <= 512) hipLaunchKernelGGL((select_kernel<1, 8>), dim3(p4), dim3(256), 0, st, c, a);
     else if (most <= 768) hipLaunchKernelGGL((select_kernel<1, 12>), dim3(p4), dim3(256), 0, st, c, a);
@@ -477,7 +484,8 @@ void launch_evict(hipStream_t st, const Cache& c, const int32_t* held, int max_h
     else if (most <= 4096) hipLaunchKernelGGL((select_kernel<16, 4>), dim3(p), dim3(1024), 0, st, c, a);
     else if (most <= 8192) hipLaunchKernelGGL((select_kernel<16, 8>), dim3(p), dim3(1024), 0, st, c, a);
     else if (most <= 16384) hipLaunchKernelGGL((select_kernel<16, 16>), dim3(p), dim3(1024), 0, st, c, a);
-    else hipLaunchKernelGGL(select_long_kernel, dim3(p), dim3(256), 0, st, c, a);
+    else if (most <= 32768) hipLaunchKernelGGL((select_kernel<16, 32>), dim3(p), dim3(1024), 0, st, c, a);
+    else hipLaunchKernelGGL(select_long_kernel, dim3(p), dim3(kLong), 0, st, c, a);
     if (max_held <= keep) return;
     const dim3 grid((unsigned)spans(c, keep)), block(256);
     if (c.hd == 32) hipLaunchKernelGGL(move_kernel<32>, grid, block, 0, st, c, keep, kept);

@@ -441,6 +441,10 @@ EVICTS = [
     (128, 32, 1, [16384, 9000], 16256, 8000, "random"),
     (128, 32, 1, [20000, 70], 128, 0, "ties"),                    # longer than the lanes hold
     (128, 32, 2, [17000], 16896, 3, "random"),
+    (128, 32, 1, [32768, 20000], 16384, 100, "random"),
+    (128, 32, 2, [40000], 4096, 3, "random"),                     # longer than any lanes hold
+    (128, 32, 1, [33000, 50, 2000], 1024, 0, "ties"),
+    (128, 32, 1, [36000], 33024, 500, "nan"),
 ]
 
 
