@@ -439,7 +439,7 @@ EVICTS = [
     (16, 32, 1, [1024, 1, 1025], 1008, 1, "random"),              # around what a wavefront takes
     (128, 32, 2, [4097, 4095], 3968, 100, "ties"),
     (128, 32, 1, [16384, 9000], 16256, 8000, "random"),
-    (128, 32, 1, [20000, 70], 128, 0, "ties"),                    # longer than the lanes hold
+    (128, 32, 1, [20000, 70], 128, 0, "ties"),                    # more than 16 per lane
     (128, 32, 2, [17000], 16896, 3, "random"),
     (128, 32, 1, [32768, 20000], 16384, 100, "random"),
     (128, 32, 2, [40000], 4096, 3, "random"),                     # longer than any lanes hold
