@@ -127,8 +127,9 @@ class AttnContext:
         _check(self.lib.moe_attn_forward_group(self.h, layer, len(batches), arr), self.h)
 
     def kv8_workspace(self, cache: Q.Kv8Cache, step: Q.Kv8Step, with_weights: bool):
-        """Workspace of forward_kv8 for steps of these bounds."""
-        return Q.attend_workspace(cache, step, self.cfg.n_q_heads, with_weights)
+        """Workspace of forward_kv8 for steps of these bounds, in the order of the compute stream."""
+        with Q._made_on(self.compute):
+            return Q.attend_workspace(cache, step, self.cfg.n_q_heads, with_weights)
 
     def forward_kv8(self, cache: Q.Kv8Cache, step: Q.Kv8Step, h_in, h_out, workspace, layer: int = 0, weight_in=None,
                     weight_out=None):

@@ -133,11 +133,12 @@ def _rows(t, name: str, step: Kv8Step, cache: Kv8Cache, heads):
     return stride
 
 
-def _own(workspace, stream):
-    """A workspace made for one call: not given to others before the call's stream is done with it."""
-    if stream is not None:
-        workspace.record_stream(stream)
-    return workspace
+def _made_on(stream):
+    """Where a workspace for work on `stream` is made: with that stream current, so that the allocator, which hands memory on
+    in the order of the stream it was asked on, neither gives it away early nor gives out what another stream still uses."""
+    import contextlib
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 def _same_sequences(cache: Kv8Cache, step: Kv8Step):
@@ -177,7 +178,8 @@ def attend(cache: Kv8Cache, step: Kv8Step, q, out, weight_in=None, weight_out=No
         if t is not None:
             _whole(t, name, torch.float32, cache.slots)
     if workspace is None:
-        workspace = _own(attend_workspace(cache, step, heads, weight_out is not None), stream)
+        with _made_on(stream):
+            workspace = attend_workspace(cache, step, heads, weight_out is not None)
     _check(load_library().moe_kv8_attend(
         _stream(cache, stream), cache.ref, step.ref, heads, q.data_ptr(), qs[0], qs[1], softmax_scale,
         out.data_ptr(), os[0], os[1], _ptr(weight_in), _ptr(weight_out), workspace.data_ptr(), workspace.numel()))
@@ -207,7 +209,8 @@ def evict(cache: Kv8Cache, held, max_held: int, keep: int, recent: int, next_pos
     if kept is not None:
         _whole(kept, "kept", torch.int32, cache.slots[:2] + (keep,))
     if workspace is None:
-        workspace = _own(evict_workspace(cache, keep), stream)
+        with _made_on(stream):
+            workspace = evict_workspace(cache, keep)
     _check(load_library().moe_kv8_evict(
         _stream(cache, stream), cache.ref, _ptr(held), max_held, keep, recent, _ptr(next_position), _ptr(weight_in),
         _ptr(weight_out), _ptr(position_out), _ptr(kept), workspace.data_ptr(), workspace.numel()))

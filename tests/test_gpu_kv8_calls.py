@@ -1,0 +1,58 @@
+"""The 8-bit key-value cache on the GPU, called in ways that a program may: other streams, large numbers, strides of its own,
+long ragged steps.  Compared with the fp64 reference within bounds that are derived from the formats."""
+import pytest
+import torch
+
+from oracle import kv8_ref as R
+from paper_2502_06888_amd import kv8_binding as Q
+from test_gpu_kv8 import bounds, filled, ints, rand, step_for, weight_bounds
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def busy(x, times=40):
+    """Work on the current stream that takes some milliseconds and leaves x as it is."""
+    for _ in range(times):
+        torch.mm(x, x)
+
+
+def test_workspaces_of_calls_on_another_stream_beside_a_busy_one():
+    """What the current stream has freed, but still uses, is not given to a call on another stream."""
+    block, hd, heads, kv, L, keep = 64, 128, 16, 4, 4096, 128
+    g = torch.Generator().manual_seed(31)
+    cache, _, _ = filled(g, 2, kv, L, hd, block, [4000] * 2, poison=False)
+    cache.position.copy_(torch.arange(L, dtype=torch.int32))
+    step = Q.Kv8Step(ints([3999, 700]), 2, 1, 3999)
+    held, nxt = ints([4000, 701]), ints([4000, 701])
+    q = rand(g, (2, heads, hd)).to(DEV)
+    w_in = torch.rand((2, kv, L), generator=g).to(DEV)
+    sizes = [Q.attend_workspace(cache, step, heads, True).numel(), Q.evict_workspace(cache, keep).numel()]
+    state = [t.clone() for t in (cache.k, cache.v, cache.k_scale, cache.v_scale, cache.position)]
+    eye = torch.eye(4096, device=DEV)
+
+    def one(stream):
+        for t, s in zip((cache.k, cache.v, cache.k_scale, cache.v_scale, cache.position), state):
+            t.copy_(s)
+        out, w = torch.zeros_like(q), torch.zeros_like(w_in)
+        torch.cuda.synchronize()
+        guards = []
+        if stream is not None:
+            busy(eye)
+            for n in sizes:                                      # written behind the busy work, then freed
+                t = torch.empty(n, dtype=torch.uint8, device=DEV)
+                t.fill_(0x5a)
+                guards.append(t.sum(dtype=torch.int64))
+                del t
+        Q.attend(cache, step, q, out, w_in, w, stream=stream)
+        Q.evict(cache, held, 4000, keep, 16, nxt, w, stream=stream)
+        torch.cuda.synchronize()
+        for n, s in zip(sizes, guards):
+            assert int(s) == n * 0x5a
+        return [out, w, cache.k.clone(), cache.v.clone(), cache.position.clone()]
+
+    want = one(None)
+    side = torch.cuda.Stream()
+    for _ in range(2):
+        for a, b in zip(want, one(side)):
+            assert torch.equal(a, b)
