@@ -143,6 +143,7 @@ class AttnContext:
                 Q._whole(t, name, torch.float32, cache.slots)
         _check(self.lib.moe_attn_forward_kv8(self.h, layer, cache.ref, step.ref, h_in.data_ptr(), h_out.data_ptr(),
                                              Q._ptr(weight_in), Q._ptr(weight_out), workspace.data_ptr(), workspace.numel()), self.h)
+        Q._used(self.compute, *cache.tensors, *step.tensors, h_in, h_out, weight_in, weight_out, workspace)
 
     def set_profiling(self, level: int):
         """0 off; n >= 1 on, kernels repeated n times between their events."""

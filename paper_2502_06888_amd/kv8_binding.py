@@ -1,7 +1,8 @@
 """Thin ctypes binding of the 8-bit key-value cache (``include/moe_kv8.h``).
 
 Argument marshalling and shape checks only: quantisation, attention and eviction run in the HIP library.  torch is
-used for device memory and streams; every call goes to the current stream of the cache's device unless one is given.
+used for device memory and streams; every call goes to the current stream of the cache's device unless one is given.  On a
+given stream the caller sees to it that the tensors are ready; they may be dropped as soon as the call returns.
 """
 from __future__ import annotations
 
@@ -83,6 +84,7 @@ class Kv8Cache:
         self.k, self.v, self.k_scale, self.v_scale, self.position, self.block = k, v, k_scale, v_scale, position, block
         self.n_seq, self.n_kv_heads, self.max_len, self.head_dim = n_seq, kv, max_len, hd
         self.device, self.slots = k.device, k.shape[:3]
+        self.tensors = (k, v, k_scale, v_scale, position)
         self.c = MoeKv8Cache(n_seq, kv, hd, max_len, block, 0, _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(position))
         self.ref = C.byref(self.c)
 
@@ -110,6 +112,7 @@ class Kv8Step:
             _whole(next_position, "next_position", torch.int32, (n_seq,))
         self.cached, self.row_offsets, self.next_position = cached, row_offsets, next_position
         self.n_seq, self.n_rows = n_seq, n_rows
+        self.tensors = (cached, row_offsets, next_position)
         self.c = MoeKv8Step(n_rows, max_new, max_cached, 0, _ptr(row_offsets), _ptr(cached), _ptr(next_position))
         self.ref = C.byref(self.c)
 
@@ -141,6 +144,14 @@ def _made_on(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
+def _used(stream, *tensors):
+    """Tensors of a call on `stream`: the caller may drop them behind the call, so the allocator is told who still uses them."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
 def _same_sequences(cache: Kv8Cache, step: Kv8Step):
     if step.n_seq != cache.n_seq:
         _refuse("the step is for another number of sequences")
@@ -154,6 +165,7 @@ def append(cache: Kv8Cache, step: Kv8Step, k_new, v_new, stream=None):
         _refuse("k_new and v_new must have the same strides")
     _check(load_library().moe_kv8_append(_stream(cache, stream), cache.ref, step.ref, k_new.data_ptr(), v_new.data_ptr(),
                                          stride[0], stride[1]))
+    _used(stream, *cache.tensors, *step.tensors, k_new, v_new)
 
 
 def attend_workspace_bytes(cache: Kv8Cache, step: Kv8Step, n_q_heads: int, with_weights: bool) -> int:
@@ -183,6 +195,7 @@ def attend(cache: Kv8Cache, step: Kv8Step, q, out, weight_in=None, weight_out=No
     _check(load_library().moe_kv8_attend(
         _stream(cache, stream), cache.ref, step.ref, heads, q.data_ptr(), qs[0], qs[1], softmax_scale,
         out.data_ptr(), os[0], os[1], _ptr(weight_in), _ptr(weight_out), workspace.data_ptr(), workspace.numel()))
+    _used(stream, *cache.tensors, *step.tensors, q, out, weight_in, weight_out, workspace)
     return out
 
 
@@ -214,3 +227,4 @@ def evict(cache: Kv8Cache, held, max_held: int, keep: int, recent: int, next_pos
     _check(load_library().moe_kv8_evict(
         _stream(cache, stream), cache.ref, _ptr(held), max_held, keep, recent, _ptr(next_position), _ptr(weight_in),
         _ptr(weight_out), _ptr(position_out), _ptr(kept), workspace.data_ptr(), workspace.numel()))
+    _used(stream, *cache.tensors, held, next_position, weight_in, weight_out, position_out, kept, workspace)

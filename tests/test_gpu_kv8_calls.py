@@ -56,3 +56,34 @@ def test_workspaces_of_calls_on_another_stream_beside_a_busy_one():
     for _ in range(2):
         for a, b in zip(want, one(side)):
             assert torch.equal(a, b)
+
+
+def test_tensors_dropped_behind_a_call_on_another_stream():
+    """The lengths of a step, taken by others on the current stream while the other stream is yet to read them."""
+    block, hd, heads, kv, L = 32, 64, 8, 2, 512
+    g = torch.Generator().manual_seed(32)
+    cache, _, _ = filled(g, 3, kv, L, hd, block, [400] * 3, poison=False)
+    q, k, v = (rand(g, (3, h, hd)).to(DEV) for h in (heads, kv, kv))
+    held = ([399, 20, 111], [60, 200, 7])
+    side, eye = torch.cuda.Stream(), torch.eye(4096, device=DEV)
+    want, got = [], []
+    state = [t.clone() for t in cache.tensors]
+    for stream, outs in ((None, want), (side, got)):
+        for h in held:
+            for t, s in zip(cache.tensors, state):
+                t.copy_(s)
+            out, w = torch.zeros_like(q), torch.zeros((3, kv, L), device=DEV)
+            step = Q.Kv8Step(ints(h), 3, 1, 399, row_offsets=ints([0, 1, 2, 3]), next_position=ints(h))
+            torch.cuda.synchronize()
+            if stream is not None:
+                with torch.cuda.stream(stream):
+                    busy(eye)
+            Q.append(cache, step, k, v, stream=stream)
+            Q.attend(cache, step, q, out, None, w, stream=stream)
+            del step
+            other = [torch.zeros(4, dtype=torch.int32, device=DEV) for _ in range(3)]
+            torch.cuda.synchronize()
+            outs += [out, w, cache.k.clone(), cache.position.clone()]
+            del other
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
