@@ -22,6 +22,12 @@
  * tensors.  Calls that share neither cache, workspace nor outputs may run at once; a workspace may be used again by
  * the next call on the same stream (not by two graphs that may run at once).  Every tensor must be on one device,
  * which need not be the current one.  The error text of a failed call is moe_kv8_last_error() on the same thread.
+ * A launch has at most 2^24 - 1 workgroups; a call whose sizes and bounds ask for more is MOE_ERR_SHAPE.  With pairs = n_seq *
+ * n_kv_heads, and divisions rounded up, calls are within that if these are:
+ *   append  2 * pairs * (blocks of a sequence that min(max_new, n_rows) tokens can fall into)
+ *   attend  pairs * (min(max_new, n_rows) * n_q_heads / n_kv_heads / 128), and with weight_out
+ *           pairs * (min(max_cached + max_new, max_len) / 128), too
+ *   evict   pairs * (keep / 512)
  */
 #ifndef KLOTSKI_MOE_KV8_H
 #define KLOTSKI_MOE_KV8_H

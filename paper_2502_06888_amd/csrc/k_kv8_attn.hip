@@ -1073,6 +1073,7 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
         const int64_t tiles = c.Hkv * (about > c.n_seq ? about : (int64_t)c.n_seq);
         per = prompt_range(most, min(pairs * p.row_tiles, tiles), s.n_rows * (int64_t)Hq);
     }
+    per = min(per, ((int64_t)most + 127) / 128 * 128);
     const int64_t ranges = most > per ? (most + per - 1) / per : 1;
     p.sp.per = (int)per;
     p.sp.ranges = (int)ranges;
@@ -1129,6 +1130,33 @@ Plan plan(const Cache& c, const Step& s, int Hq, bool weights) {
     return p;
 }
 
+// Workgroups of the launches of a step.
+struct Grids {
+    int64_t attend;           // decode_kernel or prompt_kernel
+    int64_t pack;             // pack_kernel
+    int64_t merges, chunks;   // merge_kernel; with few new tokens finish_kernel, `chunks` per pair behind them
+    int64_t weights, sums;    // prompt_weights_kernel, sum_weights_kernel
+};
+Grids grids(const Cache& c, const Step& s, const Plan& p, bool weights) {
+    Grids g{};
+    const int64_t pairs = (int64_t)c.n_seq * c.Hkv, rows = pairs * p.sp.tile_rows;
+    if (s.n_rows > 0) {
+        g.attend = pairs * p.sp.ranges * (p.tiles > 0 ? 1 : (p.row_tiles + p.each - 1) / p.each);
+        g.pack = pairs * p.sp.packed_tiles;
+        if (p.sp.ranges > 1 && p.tiles > 0) {
+            g.merges = p.sp.ranges > 8 ? rows : (rows + 3) / 4;
+            g.chunks = weights ? (p.sp.score_stride + 255) / 256 : 0;
+        } else if (p.sp.ranges > 1) {
+            g.merges = rows <= 4 * 2048 ? (rows + 3) / 4 : (rows / 4 + 3) / 4;
+        }
+    }
+    if (weights && p.tiles == 0) {
+        g.weights = pairs * weight_chunks(p.sp) * p.sp.splits;
+        if (p.sp.splits > 1) g.sums = pairs * ((p.sp.score_stride + 255) / 256);
+    }
+    return g;
+}
+
 template <int HD, int NT>
 void launch_decode(hipStream_t st, const dim3& grid, const Cache& c, const Step& s, const Attend& a, const Split& sp) {
     // Caches beyond the last-level cache of 256 MiB are read past it: 512 sequences of 513 slots (538 MB) 98 us with ordinary
@@ -1154,45 +1182,39 @@ void launch_decode(hipStream_t st, const dim3& grid, const Cache& c, const Step&
 
 template <int HD>
 void launch_hd(hipStream_t st, const Cache& c, const Step& s, const Attend& a, const Plan& p) {
-    const int64_t pairs = (int64_t)c.n_seq * c.Hkv;
+    const Grids g = grids(c, s, p, a.weight_out != nullptr);
+    const auto grid = [](int64_t n) { return dim3((unsigned)n); };
     const dim3 block(256);
-    if (s.n_rows > 0) {
-        const int groups = p.tiles > 0 ? 1 : (p.row_tiles + p.each - 1) / p.each;
-        const dim3 grid((unsigned)(pairs * p.sp.ranges * groups));
-        if (p.tiles == 1) launch_decode<HD, 1>(st, grid, c, s, a, p.sp);
-        else if (p.tiles == 2) launch_decode<HD, 2>(st, grid, c, s, a, p.sp);
-        else if (p.sp.packed_tiles > 0) {
-            hipLaunchKernelGGL(pack_kernel<HD>, dim3((unsigned)(pairs * p.sp.packed_tiles)), block, 0, st, c, s, p.sp.packed, p.sp.odd, p.sp.packed_tiles);
-            hipLaunchKernelGGL((prompt_kernel<HD, true>), grid, block, 0, st, c, s, a, p.sp, groups, p.each);
+    const int groups = (int)(g.attend / ((int64_t)c.n_seq * c.Hkv * p.sp.ranges));  // of a pair and range
+    if (g.attend > 0) {
+        if (p.tiles == 1) launch_decode<HD, 1>(st, grid(g.attend), c, s, a, p.sp);
+        else if (p.tiles == 2) launch_decode<HD, 2>(st, grid(g.attend), c, s, a, p.sp);
+        else if (g.pack > 0) {
+            hipLaunchKernelGGL(pack_kernel<HD>, grid(g.pack), block, 0, st, c, s, p.sp.packed, p.sp.odd, p.sp.packed_tiles);
+            hipLaunchKernelGGL((prompt_kernel<HD, true>), grid(g.attend), block, 0, st, c, s, a, p.sp, groups, p.each);
         } else
-            hipLaunchKernelGGL((prompt_kernel<HD, false>), grid, block, 0, st, c, s, a, p.sp, groups, p.each);
-        if (p.sp.ranges > 1 && p.tiles > 0) {
-            const bool wide = p.sp.ranges > 8;
-            const int64_t merges = wide ? pairs * p.sp.tile_rows : (pairs * p.sp.tile_rows + 3) / 4;
-            const int64_t chunks = a.weight_out != nullptr ? (p.sp.score_stride + 255) / 256 : 0;
-            const dim3 all((unsigned)(merges + pairs * chunks));
-            if (wide) hipLaunchKernelGGL((finish_kernel<HD, true>), all, block, 0, st, c, s, a, p.sp, (int)merges, (int)chunks);
-            else hipLaunchKernelGGL((finish_kernel<HD, false>), all, block, 0, st, c, s, a, p.sp, (int)merges, (int)chunks);
-        } else if (p.sp.ranges > 1) {
-            const int64_t rows = pairs * p.sp.tile_rows;
-            if (rows <= 4 * 2048) hipLaunchKernelGGL((merge_kernel<HD, 1>), dim3((unsigned)((rows + 3) / 4)), block, 0, st, c, s, a, p.sp);
-            else hipLaunchKernelGGL((merge_kernel<HD, 4>), dim3((unsigned)((rows / 4 + 3) / 4)), block, 0, st, c, s, a, p.sp);
-        }
+            hipLaunchKernelGGL((prompt_kernel<HD, false>), grid(g.attend), block, 0, st, c, s, a, p.sp, groups, p.each);
     }
-    if (a.weight_out == nullptr || p.tiles > 0) return;
-    const int chunks = (int)weight_chunks(p.sp);
-    if (chunks == 0) return;
-    hipLaunchKernelGGL(prompt_weights_kernel<HD>, dim3((unsigned)(pairs * chunks * p.sp.splits)), block, 0, st, c, s, a, p.sp, chunks);
-    if (p.sp.splits > 1) hipLaunchKernelGGL(sum_weights_kernel, dim3((unsigned)(pairs * ((p.sp.score_stride + 255) / 256))), block, 0, st, c, s, a, p.sp);
+    if (g.merges > 0) {
+        const dim3 all = grid(g.merges + (int64_t)c.n_seq * c.Hkv * g.chunks);
+        if (p.tiles > 0 && p.sp.ranges > 8) hipLaunchKernelGGL((finish_kernel<HD, true>), all, block, 0, st, c, s, a, p.sp, (int)g.merges, (int)g.chunks);
+        else if (p.tiles > 0) hipLaunchKernelGGL((finish_kernel<HD, false>), all, block, 0, st, c, s, a, p.sp, (int)g.merges, (int)g.chunks);
+        else if ((int64_t)c.n_seq * c.Hkv * p.sp.tile_rows <= 4 * 2048) hipLaunchKernelGGL((merge_kernel<HD, 1>), all, block, 0, st, c, s, a, p.sp);
+        else hipLaunchKernelGGL((merge_kernel<HD, 4>), all, block, 0, st, c, s, a, p.sp);
+    }
+    if (g.weights > 0) hipLaunchKernelGGL(prompt_weights_kernel<HD>, grid(g.weights), block, 0, st, c, s, a, p.sp, (int)weight_chunks(p.sp));
+    if (g.sums > 0) hipLaunchKernelGGL(sum_weights_kernel, grid(g.sums), block, 0, st, c, s, a, p.sp);
 }
 
 }  // namespace
 
-bool attend_fits(const Cache& c, const Step& s, int Hq) {
-    const Plan p = plan(c, s, Hq, true);
-    const int64_t pairs = (int64_t)c.n_seq * c.Hkv;
-    const int64_t most = pairs * p.sp.ranges * (p.tiles > 0 ? 1 : p.row_tiles);
-    return most <= kMostGroups && pairs * p.sp.tile_rows + pairs * weight_chunks(p.sp) <= kMostGroups;
+bool attend_fits(const Cache& c, const Step& s, int Hq, bool weights) {
+    const Plan p = plan(c, s, Hq, weights);
+    const Grids g = grids(c, s, p, weights);
+    const int64_t pairs = (int64_t)c.n_seq * c.Hkv, most = min((int64_t)s.max_cached + s.max_new, (int64_t)c.max_len);
+    if (weights && pairs * ((most + kWeightSlots - 1) / kWeightSlots) > kMostGroups) return false;  // whichever kernel sums them
+    return g.attend <= kMostGroups && g.pack <= kMostGroups && g.merges + pairs * g.chunks <= kMostGroups &&
+           g.weights <= kMostGroups && g.sums <= kMostGroups;
 }
 
 int64_t attend_workspace(const Cache& c, const Step& s, int Hq, bool weights) { return plan(c, s, Hq, weights).bytes; }

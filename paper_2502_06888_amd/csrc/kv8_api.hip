@@ -136,7 +136,10 @@ Cache cache_of(const moe_kv8_cache* c) {
     return k;
 }
 
-Step step_of(const moe_kv8_step* s) { return Step{s->n_rows, s->max_new, s->max_cached, s->row_offsets, s->cached, s->next_position}; }
+// No sequence brings more than all rows there are: a bound beyond that sizes no launch.
+Step step_of(const moe_kv8_step* s) {
+    return Step{s->n_rows, s->max_new < s->n_rows ? s->max_new : s->n_rows, s->max_cached, s->row_offsets, s->cached, s->next_position};
+}
 
 // Everything that moe_kv8_append refuses; *device: where the tensors are.
 moe_status check_append(const moe_kv8_cache* cache, const moe_kv8_step* step, const void* k_new, const void* v_new,
@@ -180,7 +183,7 @@ moe_status check_attend(const moe_kv8_cache* cache, const moe_kv8_step* step, in
     if (weight_in && weight_in != weight_out) TRY(w.on(weight_in, "weight_in", 4));
     const Cache c = cache_of(cache);
     const Step s = step_of(step);
-    if (!attend_fits(c, s, n_q_heads)) return fail(MOE_ERR_SHAPE, "too many workgroups: bring fewer sequences or tokens at once");
+    if (!attend_fits(c, s, n_q_heads, weight_out != nullptr)) return fail(MOE_ERR_SHAPE, "too many workgroups: bring fewer sequences or tokens at once");
     return check_workspace(workspace, workspace_bytes, attend_workspace(c, s, n_q_heads, weight_out != nullptr), &w);
 }
 
@@ -228,7 +231,7 @@ moe_status moe_kv8_attend_workspace_bytes(const moe_kv8_cache* cache, const moe_
     TRY(check_sizes(cache));
     TRY(check_step_sizes(cache, step));
     TRY(check_heads(cache, n_q_heads));
-    if (!attend_fits(cache_of(cache), step_of(step), n_q_heads)) return fail(MOE_ERR_SHAPE, "too many workgroups: bring fewer sequences or tokens at once");
+    if (!attend_fits(cache_of(cache), step_of(step), n_q_heads, with_weights != 0)) return fail(MOE_ERR_SHAPE, "too many workgroups: bring fewer sequences or tokens at once");
     *bytes_out = attend_workspace(cache_of(cache), step_of(step), n_q_heads, with_weights != 0);
     return MOE_OK;
 }

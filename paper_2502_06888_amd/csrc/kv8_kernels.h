@@ -48,7 +48,7 @@ constexpr int64_t kMostGroups = (1 << 24) - 1;
 // Whether the grids of the launches stay within that.
 bool append_fits(const Cache& c, const Step& s);
 bool evict_fits(const Cache& c, int keep);
-bool attend_fits(const Cache& c, const Step& s, int Hq);
+bool attend_fits(const Cache& c, const Step& s, int Hq, bool weights);
 
 void launch_append(hipStream_t st, const Cache& c, const Step& s, const Rows& k, const Rows& v);
 int64_t attend_workspace(const Cache& c, const Step& s, int Hq, bool weights);

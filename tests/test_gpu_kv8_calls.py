@@ -87,3 +87,28 @@ def test_tensors_dropped_behind_a_call_on_another_stream():
             del other
     for a, b in zip(want, got):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("weights", [False, True])
+def test_one_long_prompt_among_single_tokens(weights):
+    """512 sequences, one of which brings 513 tokens: the bounds allow every pair 33 tiles of rows."""
+    block, hd, heads, kv, n = 64, 32, 64, 8, 512
+    g = torch.Generator().manual_seed(33)
+    cached, new = [(7 * s) % 23 for s in range(n)], [513 if s == 300 else 1 for s in range(n)]
+    total = [c + m for c, m in zip(cached, new)]
+    L = -(-max(total) // block) * block
+    cache, codes, scale = filled(g, n, kv, L, hd, block, total)
+    step, off = step_for(cached, new)
+    q = rand(g, (off[-1] + 1, heads, hd), 2.0)
+    out = torch.full_like(q, -3.0, device=DEV)
+    w_in, w = torch.rand((n, kv, L), generator=g), torch.full((n, kv, L), -5.0, device=DEV)
+    Q.attend(cache, step, q.to(DEV), out, *((w_in.to(DEV), w) if weights else ()))
+    torch.cuda.synchronize()
+    ref, want, spread, mag = R.attend(codes[0], scale[0], codes[1], scale[1], q, cached, off, block, w_in)
+    m = off[-1]
+    assert bool(((out.cpu().double() - ref)[:m].abs() <= bounds(ref, spread, mag, hd)[:m]).all())
+    assert bool((out[m:] == -3).all())
+    if weights:
+        held = ~want.isnan()
+        assert bool(((w.cpu().double() - want).abs() <= weight_bounds(want, mag[:m], hd))[held].all())
+        assert bool((w.cpu()[~held] == -5).all())

@@ -93,3 +93,45 @@ def test_tensors_of_a_call_on_another_stream_are_recorded_on_it(monkeypatch):
         used.clear()
         call(None)
         assert not used
+
+
+@pytest.mark.parametrize("seqs,kv,heads,hd,rows,new,cached,max_len", [
+    (512, 8, 32, 128, 512 + 1024, 1024, 512, 2048),     # one chunk of a prompt among single tokens
+    (512, 8, 32, 128, 512 + 1024, 1025, 512, 2048),
+    (64, 8, 32, 128, 64 * 8192, 8192, 0, 8192),         # 64 long prompts
+    (64, 8, 32, 128, 1 << 20, 16384, 0, 16384),
+    (256, 8, 32, 128, 4096, 2048, 0, 4096),
+    (65536, 8, 64, 32, 1 << 20, 17, 100, 128),
+    (1, 1, 8, 128, 1 << 20, 1 << 20, 0, 1 << 20),
+])
+def test_steps_whose_launches_fit_are_accepted(seqs, kv, heads, hd, rows, new, cached, max_len):
+    """The limit is one of workgroups, of 128 rows each, not of the rows that the bounds allow every sequence."""
+    c = cache(kv=kv)
+    c.c.n_seq, c.c.n_kv_heads, c.c.head_dim, c.c.max_len, c.c.block = seqs, kv, hd, max_len, 64
+    s = Q.Kv8Step(ints(0), rows, new, cached, row_offsets=ints(0, 1))
+    assert 0 <= Q.attend_workspace_bytes(c, s, heads, False) <= Q.attend_workspace_bytes(c, s, heads, True)
+
+
+def test_the_limit_of_a_launch_is_the_documented_one():
+    """Tiles of 128 rows per pair, and slots / 128 where weights are summed."""
+    most = (1 << 24) - 1
+    c = cache(kv=16)
+    for seqs, kv, heads, max_len in ((64, 16, 64, 1 << 18), (65536, 16, 128, 1 << 11), (4096, 16, 16, 1 << 16), (3, 16, 64, 1 << 20),
+                                     (700, 16, 32, 1 << 17), (1, 1, 8, 1 << 20), (256, 1, 8, 1 << 20), (30, 8, 64, 1 << 20)):
+        c.c.n_seq, c.c.n_kv_heads, c.c.max_len = seqs, kv, max_len
+        pairs, g = seqs * kv, heads // kv
+        for new in (1, 16, 17, 300, 4000, 70000, 1 << 20):
+            for cached in (0, 3, max_len // 2, max_len):
+                for rows in {1, new // 2 + 1, new, min(seqs * new, 1 << 20)}:
+                    if new > max_len:
+                        continue
+                    s = Q.Kv8Step(ints(0), rows, new, cached, row_offsets=ints(0, 1))
+                    fits = pairs * -(-min(new, rows) * g // 128) <= most
+                    sums = pairs * -(-min(new + cached, max_len) // 128) <= most
+                    if fits:
+                        assert Q.attend_workspace_bytes(c, s, heads, False) >= 0
+                        assert not sums or Q.attend_workspace_bytes(c, s, heads, True) >= 0
+                    if not sums:
+                        with pytest.raises(B.MoeError) as e:
+                            Q.attend_workspace_bytes(c, s, heads, True)
+                        assert e.value.status == B.MOE_ERR_SHAPE and "workgroups" in e.value.message
