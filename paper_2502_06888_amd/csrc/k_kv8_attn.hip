@@ -13,19 +13,32 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kEmpty = -3.40282347e38f;  // finite stand-in for "no slot seen yet": the lowest number, not above any finite score
-// The reference of a running softmax lies kAbove over the largest score at the time it was set, and is set anew once a
-// score comes closer than kNear: the sums are not rescaled for every new maximum, and as weights stay below 2^-kNear,
-// the sums of 2^20 slots of any finite values stay finite.
-constexpr float kAbove = 28.f, kNear = 20.f;
-// score * factor - reference is one fused operation, whose product is exact while the reference comes from a rounded one.
-// That is half a step of the score, as any of its roundings; but from where a step is no longer small beside 1 the largest
-// score itself would be put far above or below its reference.  Beyond kFar the product is rounded first, by itself.
+// The reference of a running softmax is the largest score at the time it was set, and is set anew once a score exceeds it by
+// more than kRise: the sums are not rescaled for every new maximum.  Weights are 2^(score - reference - kAbove): the largest
+// one is a power of two at first, so that rounding it to bf16 takes nothing, and none is over 2^-20, so that the sums of 2^20
+// slots of any finite values stay finite.
+constexpr float kAbove = 28.f, kRise = 8.f, kBelow = 0x1p-28f;  // kBelow = 2^-kAbove
+// score * factor - (reference + kAbove) is one fused operation; but the reference comes from a rounded product, where this
+// one is exact.  That is half a step of the score, as any of its roundings; but from where a step is no longer
+// small beside 1 the largest score itself would be put far above or below its reference, and from 2^29 on kAbove would be
+// lost beside it.  Beyond kFar the product is rounded first, by itself, and reference and kAbove are taken off one after the other.
 constexpr float kFar = 0x1p18f;
+// The reference for a largest score: up to kFar one to which kAbove can be added without rounding, half a step of the sum off.
+__device__ __forceinline__ float reference_of(float top) { return fabsf(top) > kFar ? top : (top + kAbove) - kAbove; }
+__device__ __forceinline__ float apart(float score, float factor, float reference) {
+#pragma clang fp contract(off)
+    const float z = score * factor;
+    return z - reference;
+}
+// Scores to exponents of the weights: score * factor - reference - above.  `each` takes what to make of every score of a lane.
 template <class T>
-__device__ __forceinline__ float near_factor(float reference, float factor, T&& scale_scores) {
-    if (!__any(fabsf(reference) > kFar)) return factor;
-    scale_scores();
-    return 1.f;
+__device__ __forceinline__ void exponents(float reference, float above, float factor, T&& each) {
+    if (!__any(fabsf(reference) > kFar)) {
+        const float less = reference + above;
+        each([&](float score) { return __builtin_fmaf(score, factor, -less); });
+    } else {
+        each([&](float score) { return apart(score, factor, reference) - above; });
+    }
 }
 
 // The wavefront's number in its workgroup, in a scalar register.
@@ -73,7 +86,7 @@ struct Split {
     float* scores;      // [pair, row, slot] products q . K
     int waves;          // of a workgroup of decode_kernel
     int lds_scores;     // bytes of LDS that hold those of a pair instead, 0: they are in `scores`
-    float2* final_ml;   // [pair, row] with many new tokens: reference of all ranges, 1 / sum of weights
+    float2* final_ml;   // [pair, row] with many new tokens: reference of all ranges, 2^-kAbove / sum of weights
     u32x4* packed;      // [pair, tile of kSlots] dequantised (see Tile), or null
     int32_t* odd;       // [pair, tile]
     int packed_tiles;   // tiles per pair
@@ -233,10 +246,10 @@ __global__ __launch_bounds__(W * 64, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2)
 #pragma unroll
             for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
             top *= a.qscale;
-            if (__any(top > m[n] - kNear)) {
+            if (__any(top > m[n] + kRise)) {
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float mn = top > m[n] - kNear ? fmaxf(m[n], top + kAbove) : m[n];
+                const float mn = top > m[n] + kRise ? reference_of(top) : m[n];
                 const float f = __builtin_amdgcn_exp2f(m[n] - mn);
                 m[n] = mn;
                 l[n] *= f;
@@ -248,13 +261,13 @@ __global__ __launch_bounds__(W * 64, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2)
                 }
             }
             float pr[8];
-            const float by = near_factor(m[n], a.qscale, [&] {
+            exponents(m[n], kAbove, a.qscale, [&](auto&& of) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] *= a.qscale;
+                for (int j = 0; j < 8; ++j) x[j] = of(x[j]);
             });
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                pr[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], by, -m[n]));
+                pr[j] = __builtin_amdgcn_exp2f(x[j]);
                 l[n] += pr[j];
             }
 #pragma unroll
@@ -336,18 +349,18 @@ __global__ __launch_bounds__(W * 64, NT * HD <= 64 ? 4 : NT * HD <= 128 ? 3 : 2)
             w.x = pack_bf16(o[0] * inv, o[1] * inv);
             w.y = pack_bf16(o[2] * inv, o[3] * inv);
             *(u32x2*)(a.out.p + (int64_t)(q.row0 + r / G) * a.out.row + (int64_t)(hk * G + r % G) * a.out.head + d) = w;
-            if (SCORES && d == 0) done[r] = make_float2(mm, inv);
+            if (SCORES && d == 0) done[r] = make_float2(mm, inv * kBelow);
         }
     }
     if (!SCORES || many > 1) return;
     __syncthreads();  // statistics and scores are there, those of this workgroup
-    float far = 0.f, first_by = 1.f;
-    for (int r = 0; r < rows; ++r) far = fmaxf(far, fabsf(done[r].x));
-    const float by = near_factor(far, a.qscale, [&] { first_by = a.qscale; });
+    bool far = false;
+    for (int r = 0; r < rows; ++r) far |= fabsf(done[r].x) > kFar;
     for (int j = threadIdx.x; j < len; j += W * 64) {
         float w = a.weight_in != nullptr && j < q.cached ? a.weight_in[base * c.max_len + j] : 0.f;
         for (int r = max(0, j - q.cached) * G; r < rows; ++r) {
-            w += __builtin_amdgcn_exp2f(__builtin_fmaf(scores[(int64_t)r * sp.score_stride + j] * first_by, by, -done[r].x)) * done[r].y;
+            const float z = scores[(int64_t)r * sp.score_stride + j];
+            w += __builtin_amdgcn_exp2f(far ? apart(z, a.qscale, done[r].x) : __builtin_fmaf(z, a.qscale, -done[r].x)) * done[r].y;
         }
         a.weight_out[base * c.max_len + j] = w;
     }
@@ -450,18 +463,17 @@ __global__ __launch_bounds__(256) void finish_kernel(Cache c, Step s, Attend a, 
                 l = l * __builtin_amdgcn_exp2f(m - mn) + l2 * __builtin_amdgcn_exp2f(m2 - mn);
                 m = mn;
             }
-            if (lane % 16 == 0 && row < rows) stat[row] = make_float2(m, 1.f / l);
+            if (lane % 16 == 0 && row < rows) stat[row] = make_float2(m, 1.f / l * kBelow);
         }
     __syncthreads();
     if (j >= len) return;
-    float far = 0.f, first_by = 1.f;
-    for (int r = 0; r < rows; ++r) far = fmaxf(far, fabsf(stat[r].x));
-    const float by = near_factor(far, a.qscale, [&] { first_by = a.qscale; });
+    bool far = false;
+    for (int r = 0; r < rows; ++r) far |= fabsf(stat[r].x) > kFar;
     const int64_t at = (int64_t)pair * c.max_len + j;
     float w = a.weight_in != nullptr && j < q.cached ? a.weight_in[at] : 0.f;
     for (int r = max(0, j - q.cached) * G; r < rows; ++r) {
-        const float z = sp.scores[((int64_t)pair * sp.tile_rows + r) * sp.score_stride + j] * first_by;
-        w += __builtin_amdgcn_exp2f(__builtin_fmaf(z, by, -stat[r].x)) * stat[r].y;
+        const float z = sp.scores[((int64_t)pair * sp.tile_rows + r) * sp.score_stride + j];
+        w += __builtin_amdgcn_exp2f(far ? apart(z, a.qscale, stat[r].x) : __builtin_fmaf(z, a.qscale, -stat[r].x)) * stat[r].y;
     }
     a.weight_out[at] = w;
 }
@@ -506,7 +518,7 @@ __global__ __launch_bounds__(256) void merge_kernel(Cache c, Step s, Attend a, S
         const int r = r0 + k;
         if (lane >= LPR || r >= rows) continue;
         t[k].write(a.out.p + (int64_t)(q.row0 + r / G) * a.out.row + (int64_t)(pair % c.Hkv * G + r % G) * a.out.head + lane * 4);
-        if (sp.final_ml != nullptr && lane == 0) sp.final_ml[(int64_t)pair * sp.tile_rows + r] = make_float2(t[k].m, 1.f / t[k].l);
+        if (sp.final_ml != nullptr && lane == 0) sp.final_ml[(int64_t)pair * sp.tile_rows + r] = make_float2(t[k].m, 1.f / t[k].l * kBelow);
     }
 }
 
@@ -777,9 +789,9 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, z[t][i]);
             top *= a.qscale;
-            if (__any(top > ref - kNear)) {
+            if (__any(top > ref + kRise)) {
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float now = top > ref - kNear ? fmaxf(ref, top + kAbove) : ref;
+                const float now = top > ref + kRise ? reference_of(top) : ref;
                 const float f = __builtin_amdgcn_exp2f(ref - now);
                 ref = now;
                 sum *= f;
@@ -788,11 +800,11 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
 #pragma unroll
                     for (int i = 0; i < 16; ++i) acc[m][i] *= f;
             }
-            const float by = near_factor(ref, a.qscale, [&] {
+            exponents(ref, kAbove, a.qscale, [&](auto&& of) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) z[t][i] *= a.qscale;
+                    for (int i = 0; i < 16; ++i) z[t][i] = of(z[t][i]);
             });
             u32x4 pf[4];
 #pragma unroll
@@ -800,7 +812,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
                 float p[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u >> 1][(u & 1) * 8 + i], by, -ref));
+                    p[i] = __builtin_amdgcn_exp2f(z[u >> 1][(u & 1) * 8 + i]);
                     sum += p[i];
                 }
 #pragma unroll
@@ -833,7 +845,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
             }
         } else {
             const float inv = 1.f / sum;
-            if (sp.final_ml != nullptr && grp == 0 && r < rows) sp.final_ml[(int64_t)pair * sp.tile_rows + r] = make_float2(ref, inv);
+            if (sp.final_ml != nullptr && grp == 0 && r < rows) sp.final_ml[(int64_t)pair * sp.tile_rows + r] = make_float2(ref, inv * kBelow);
             // The rows go through the buffer that is done with, so that each leaves in one piece; its 16-byte pieces lie
             // at an xor of the row, which spreads them over the banks.
             constexpr int PPR = HD / 8;  // pieces of a row
@@ -873,7 +885,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(Cache c, Step s, Attend 
 }
 
 // The weights of 128 slots (32 per wavefront, K in registers) from all rows that see them: S^T again, then
-// exp2(score - reference) / sum with the row's statistics, which are the lane's; added up over the rows in the lane, over
+// exp2(score - reference) * 2^-kAbove / sum with the row's statistics, which are the lane's; added up over the rows in the lane, over
 // the lanes at the end.  32 rows of q at a time come into LDS in the order of the matrix instructions, shared by the
 // wavefronts, three tiles ahead of their use.  Bound by the exponentials and, next to them, the matrix cores: 1941 tokens of 2
 // query heads per group over up to 6801 slots (39 GFLOP of the first product) 72 us.
@@ -953,25 +965,25 @@ __global__ __launch_bounds__(256, 4) void prompt_weights_kernel(Cache c, Step s,
         __syncthreads();
         copy((at + RING - 1) % RING, r0 + (RING - 1) * 32);  // past the end: again, so that the count stays
         if (r0 + 31 < r_see) continue;
-        const float2 e = ml[at][col];
+        const float2 stat = ml[at][col];
         f32x16 z;
 #pragma unroll
         for (int i = 0; i < 16; ++i) z[i] = 0.f;
 #pragma unroll
         for (int f = 0; f < F; ++f) z = mfma32(kf[f], qt[at][f * 64 + lane], z);
-        const float by = near_factor(e.x, a.qscale, [&] {
+        exponents(stat.x, 0.f, a.qscale, [&](auto&& of) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] *= a.qscale;
+            for (int i = 0; i < 16; ++i) z[i] = of(z[i]);
         });
         if (r0 + 32 <= rows && r0 >= r_whole) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                w[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(z[i], by, -e.x)), e.y, w[i]);
+                w[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(z[i]), stat.y, w[i]);
         } else {
             const int within = r0 + col < rows ? q.cached + (r0 + col) / G + 1 - j0 - 4 * grp : 0;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], by, -e.x)) * e.y;
+                const float x = __builtin_amdgcn_exp2f(z[i]) * stat.y;
                 w[i] += row_of(i, 0) < within ? x : 0.f;
             }
         }

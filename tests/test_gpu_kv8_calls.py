@@ -112,3 +112,34 @@ def test_one_long_prompt_among_single_tokens(weights):
         held = ~want.isnan()
         assert bool(((w.cpu().double() - want).abs() <= weight_bounds(want, mag[:m], hd))[held].all())
         assert bool((w.cpu()[~held] == -5).all())
+
+
+@pytest.mark.parametrize("query", [1.0625 * 2.0 ** 10, 1.0625 * 2.0 ** 18, 1.0625 * 2.0 ** 20, 1.0625 * 2.0 ** 21, -1.0625 * 2.0 ** 21,
+                                   1.0625 * 2.0 ** 60, -1.0625 * 2.0 ** 60])
+@pytest.mark.parametrize("cached,new", [(700, 1), (3000, 1), (40, 4), (0, 150), (300, 520)])
+def test_equal_scores_of_any_size_over_the_largest_values(cached, new, query):
+    """Scores from 4.5e5 to 5e20 in magnitude over values up to 448 * 2^119: their mean is finite, so the sums have to be."""
+    block, hd, heads, kv, L = 32, 32, 8, 1, 3008
+    g = torch.Generator().manual_seed(34)
+    cache, codes, scale = filled(g, 1, kv, L, hd, block, [L], poison=False)
+    codes[0][:] = 0
+    codes[0][..., 5] = 0x7d                                                  # 416
+    codes[1] = torch.tensor([0x7e, 0x7e, 0x7a, 0x70], dtype=torch.uint8)[torch.randint(0, 4, codes[1].shape, generator=g)]
+    cache.k.copy_(codes[0])
+    cache.v.copy_(codes[1])
+    cache.k_scale.fill_(1.0)
+    cache.v_scale.fill_(2.0 ** 119)
+    q = torch.zeros((new, heads, hd), dtype=torch.bfloat16)
+    q[..., 5] = query
+    out = torch.zeros((new, heads, hd), dtype=torch.bfloat16, device=DEV)
+    w = torch.zeros((1, kv, L), device=DEV)
+    Q.attend(cache, Q.Kv8Step(ints([cached]), new, new, cached), q.to(DEV), out, None, w, softmax_scale=0.6875)
+    v = R.TABLE[codes[1][0, 0].long()] * 2.0 ** 119
+    want, mean = torch.zeros(L, dtype=torch.float64), torch.zeros((new, 1, hd), dtype=torch.float64)
+    for i in range(new):
+        share = (torch.arange(L) <= cached + i).double() / (cached + i + 1)
+        want += heads * share
+        mean[i, 0] = share @ v
+    # equal scores are equal in 32 bits too: what is left is the rounding of the weights and of the result, and sums in 32 bits
+    assert bool(((out.cpu().double() - mean).abs() <= 2.0 ** -8 * mean + (2.0 ** -8 + 2.0 ** -20) * v.max()).all())
+    assert bool(((w[0, 0].cpu().double() - want).abs() <= 2.0 ** -18 * want).all())
