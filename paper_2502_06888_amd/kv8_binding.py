@@ -146,10 +146,9 @@ def _made_on(stream):
 
 def _used(stream, *tensors):
     """Tensors of a call on `stream`: the caller may drop them behind the call, so the allocator is told who still uses them."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
 
 
 def _same_sequences(cache: Kv8Cache, step: Kv8Step):
@@ -165,7 +164,8 @@ def append(cache: Kv8Cache, step: Kv8Step, k_new, v_new, stream=None):
         _refuse("k_new and v_new must have the same strides")
     _check(load_library().moe_kv8_append(_stream(cache, stream), cache.ref, step.ref, k_new.data_ptr(), v_new.data_ptr(),
                                          stride[0], stride[1]))
-    _used(stream, *cache.tensors, *step.tensors, k_new, v_new)
+    if stream is not None:
+        _used(stream, *cache.tensors, *step.tensors, k_new, v_new)
 
 
 def attend_workspace_bytes(cache: Kv8Cache, step: Kv8Step, n_q_heads: int, with_weights: bool) -> int:
@@ -195,7 +195,8 @@ def attend(cache: Kv8Cache, step: Kv8Step, q, out, weight_in=None, weight_out=No
     _check(load_library().moe_kv8_attend(
         _stream(cache, stream), cache.ref, step.ref, heads, q.data_ptr(), qs[0], qs[1], softmax_scale,
         out.data_ptr(), os[0], os[1], _ptr(weight_in), _ptr(weight_out), workspace.data_ptr(), workspace.numel()))
-    _used(stream, *cache.tensors, *step.tensors, q, out, weight_in, weight_out, workspace)
+    if stream is not None:
+        _used(stream, *cache.tensors, *step.tensors, q, out, weight_in, weight_out, workspace)
     return out
 
 
@@ -227,4 +228,5 @@ def evict(cache: Kv8Cache, held, max_held: int, keep: int, recent: int, next_pos
     _check(load_library().moe_kv8_evict(
         _stream(cache, stream), cache.ref, _ptr(held), max_held, keep, recent, _ptr(next_position), _ptr(weight_in),
         _ptr(weight_out), _ptr(position_out), _ptr(kept), workspace.data_ptr(), workspace.numel()))
-    _used(stream, *cache.tensors, held, next_position, weight_in, weight_out, position_out, kept, workspace)
+    if stream is not None:
+        _used(stream, *cache.tensors, held, next_position, weight_in, weight_out, position_out, kept, workspace)
