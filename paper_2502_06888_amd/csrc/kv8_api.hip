@@ -115,6 +115,22 @@ moe_status check_rows(const void* p, const char* name, int64_t row, int64_t head
     return MOE_OK;
 }
 
+// Whether two of rows x heads pieces of `width` elements, at these strides, share an element.
+bool pieces_overlap(int64_t rows, int64_t heads, int64_t row, int64_t head, int64_t width) {
+    if ((heads > 1 && head < width) || (rows > 1 && row < width)) return true;
+    if (rows <= 1 || heads <= 1) return false;
+    typedef __int128 wide;  // any stride times any number of rows
+    if (row >= (wide)(heads - 1) * head + width || head >= (wide)(rows - 1) * row + width) return false;  // one inside the other
+    // `down` rows on and `back` heads back there is another piece, |down * row - back * head| away
+    for (int64_t back = 1; back < heads; ++back) {
+        const wide to = (wide)back * head;
+        const int64_t down = (int64_t)(to / row);
+        if (down >= 1 && down < rows && to - (wide)down * row < width) return true;
+        if (down + 1 < rows && (wide)(down + 1) * row - to < width) return true;
+    }
+    return false;
+}
+
 moe_status check_workspace(const void* ws, int64_t bytes, int64_t need, Where* w) {
     if (need == 0) return MOE_OK;
     if (bytes < need) return fail(MOE_ERR_OOM, "workspace of %lld bytes, need %lld", (long long)bytes, (long long)need);
@@ -166,8 +182,8 @@ moe_status check_attend(const moe_kv8_cache* cache, const moe_kv8_step* step, in
     TRY(check_heads(cache, n_q_heads));
     if (!(softmax_scale >= 0.f) || std::isinf(softmax_scale * (float)kLog2e))
         return fail(MOE_ERR_INVALID_ARG, "softmax_scale must be finite, times log2(e) too, and not negative");
-    if ((n_q_heads > 1 && out_head_stride < cache->head_dim) || (step->n_rows > 1 && out_row_stride < cache->head_dim))
-        return fail(MOE_ERR_INVALID_ARG, "strides of out are under head_dim: its rows or heads overlap");
+    if (pieces_overlap(step->n_rows, n_q_heads, out_row_stride, out_head_stride, cache->head_dim))
+        return fail(MOE_ERR_INVALID_ARG, "rows or heads of out overlap");
     Where w;
     TRY(check_cache(cache, &w));
     TRY(check_step(step, &w));
@@ -200,8 +216,8 @@ moe_status check_layer_call(const moe_kv8_cache* cache, const moe_kv8_step* step
                             const float* weight_in, const float* weight_out, const void* workspace, int64_t workspace_bytes) {
     int device = 0;
     TRY(check_append(cache, step, rows, rows, 8, 8, &device));
-    return check_attend(cache, step, n_q_heads, rows, 8, 8, 0.f, (const uint8_t*)rows + 16, 128, 128, weight_in, weight_out, workspace,
-                        workspace_bytes, &device);
+    return check_attend(cache, step, n_q_heads, rows, 8, 8, 0.f, (const uint8_t*)rows + 16, (int64_t)n_q_heads * cache->head_dim,
+                        cache->head_dim, weight_in, weight_out, workspace, workspace_bytes, &device);
 }
 
 Cache cache_of_call(const moe_kv8_cache* c) { return cache_of(c); }

@@ -135,3 +135,27 @@ def test_the_limit_of_a_launch_is_the_documented_one():
                         with pytest.raises(B.MoeError) as e:
                             Q.attend_workspace_bytes(c, s, heads, True)
                         assert e.value.status == B.MOE_ERR_SHAPE and "workgroups" in e.value.message
+
+
+def attend_strides(c, s, heads, row, head):
+    """Text of what moe_kv8_attend says to host tensors with these strides of out: it asks for device memory after the strides."""
+    x = torch.zeros(8, dtype=torch.bfloat16)
+    assert Q.load_library().moe_kv8_attend(None, c.ref, s.ref, heads, x.data_ptr(), 256, 64, 0.0, x.data_ptr(), row, head, None, None, None, 0) == B.MOE_ERR_INVALID_ARG
+    return Q.load_library().moe_kv8_last_error()
+
+
+def test_outputs_are_refused_if_and_only_if_pieces_share_an_element():
+    for rows, heads, hd in ((2, 2, 64), (2, 4, 64), (3, 2, 32), (7, 4, 32), (5, 6, 64), (1, 4, 32), (9, 2, 128), (1, 2, 128)):
+        c, s = cache(n_seq=rows, kv=2, hd=hd), Q.Kv8Step(ints(*[3] * rows), rows, 1, 4)
+        for row in range(0, 6 * hd * heads // 4, 8):
+            for head in range(0, 6 * hd * rows // 4, 24):
+                starts = sorted(r * row + h * head for r in range(rows) for h in range(heads))
+                share = any(b - a < hd for a, b in zip(starts, starts[1:]))
+                assert (b"overlap" in attend_strides(c, s, heads, row, head)) == share, (rows, heads, hd, row, head)
+
+
+def test_strides_of_any_size_are_judged():
+    c, s = cache(), Q.Kv8Step(ints(3, 4), 2, 1, 4)
+    far = 1 << 62
+    for row, head, share in ((far, 64, False), (64, far, False), (far, far, True), (far, far - 64, False), (far, far - 56, True)):
+        assert (b"overlap" in attend_strides(c, s, 2, row, head)) == share
