@@ -182,7 +182,7 @@ moe_status check_attend(const moe_kv8_cache* cache, const moe_kv8_step* step, in
     TRY(check_heads(cache, n_q_heads));
     if (!(softmax_scale >= 0.f) || std::isinf(softmax_scale * (float)kLog2e))
         return fail(MOE_ERR_INVALID_ARG, "softmax_scale must be finite, times log2(e) too, and not negative");
-    if (pieces_overlap(step->n_rows, n_q_heads, out_row_stride, out_head_stride, cache->head_dim))
+    if (step->n_rows > 0 && pieces_overlap(step->n_rows, n_q_heads, out_row_stride, out_head_stride, cache->head_dim))
         return fail(MOE_ERR_INVALID_ARG, "rows or heads of out overlap");
     Where w;
     TRY(check_cache(cache, &w));
@@ -191,9 +191,9 @@ moe_status check_attend(const moe_kv8_cache* cache, const moe_kv8_step* step, in
     if (step->n_rows > 0) {
         TRY(check_rows(q, "q", q_row_stride, q_head_stride, &w));
         TRY(check_rows(out, "out", out_row_stride, out_head_stride, &w));
+        if (q == out && (weight_out || q_row_stride != out_row_stride || q_head_stride != out_head_stride))
+            return fail(MOE_ERR_INVALID_ARG, "out may be q only without weight_out and with the same strides");
     }
-    if (q && q == out && (weight_out || q_row_stride != out_row_stride || q_head_stride != out_head_stride))
-        return fail(MOE_ERR_INVALID_ARG, "out may be q only without weight_out and with the same strides");
     if (weight_in && !weight_out) return fail(MOE_ERR_INVALID_ARG, "weight_in without weight_out");
     if (weight_out) TRY(w.on(weight_out, "weight_out", 4));
     if (weight_in && weight_in != weight_out) TRY(w.on(weight_in, "weight_in", 4));

@@ -143,3 +143,21 @@ def test_equal_scores_of_any_size_over_the_largest_values(cached, new, query):
     # equal scores are equal in 32 bits too: what is left is the rounding of the weights and of the result, and sums in 32 bits
     assert bool(((out.cpu().double() - mean).abs() <= 2.0 ** -8 * mean + (2.0 ** -8 + 2.0 ** -20) * v.max()).all())
     assert bool(((w[0, 0].cpu().double() - want).abs() <= 2.0 ** -18 * want).all())
+
+
+def test_a_step_without_rows_carries_the_weights_over_and_needs_no_rows():
+    block, hd, kv, n, L = 32, 64, 2, 2, 128
+    g = torch.Generator().manual_seed(35)
+    cache, _, _ = filled(g, n, kv, L, hd, block, [60, 0])
+    step = Q.Kv8Step(ints([60, 0]), 0, 0, 60, row_offsets=ints([0, 0, 0]))
+    w_in = torch.rand((n, kv, L), generator=g).to(DEV)
+    q = torch.zeros(8, dtype=torch.bfloat16, device=DEV)
+    for p in (None, q.data_ptr()):
+        w = torch.full_like(w_in, -5.0)
+        assert Q.load_library().moe_kv8_attend(torch.cuda.current_stream().cuda_stream, cache.ref, step.ref, 4, p, 0, 0, 0.0, p, 0, 0,
+                                               w_in.data_ptr(), w.data_ptr(), None, 0) == 0
+        assert torch.equal(w[0, :, :60], w_in[0, :, :60]) and bool((w[0, :, 60:] == -5).all()) and bool((w[1] == -5).all())
+    rows = torch.zeros((0, 4, hd), dtype=torch.bfloat16, device=DEV)
+    w = torch.full_like(w_in, -5.0)
+    Q.attend(cache, step, rows, rows, w_in, w)
+    assert torch.equal(w[0, :, :60], w_in[0, :, :60]) and bool((w[1] == -5).all())

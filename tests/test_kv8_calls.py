@@ -159,3 +159,11 @@ def test_strides_of_any_size_are_judged():
     far = 1 << 62
     for row, head, share in ((far, 64, False), (64, far, False), (far, far, True), (far, far - 64, False), (far, far - 56, True)):
         assert (b"overlap" in attend_strides(c, s, 2, row, head)) == share
+
+
+def test_nothing_is_asked_of_q_and_out_where_there_are_no_rows():
+    c, lib = cache(), Q.load_library()
+    s = Q.Kv8Step(ints(3, 4), 0, 0, 4, row_offsets=ints(0, 0, 0))
+    for p in (None, torch.zeros(8, dtype=torch.bfloat16).data_ptr()):
+        assert lib.moe_kv8_attend(None, c.ref, s.ref, 4, p, 0, 0, 0.0, p, 0, 0, None, None, None, 0) == B.MOE_ERR_INVALID_ARG
+        assert b"cache.k is not device memory" in lib.moe_kv8_last_error()
