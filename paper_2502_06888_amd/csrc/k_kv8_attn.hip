@@ -646,17 +646,21 @@ __global__ __launch_bounds__(256) void pack_kernel(Cache c, Step s, u32x4* packe
 }
 
 // 16 bytes per lane from `from` (the lane's own address) to LDS at `to` + 16 * lane, without registers; the wavefront waits
-// for it with wait_copies().
+// for it with wait_copies().  The instruction takes the LDS address from m0, which is named as overwritten; the compiler
+// keeps that register for itself and says so, though nothing else in these kernels uses it.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void copy_to_lds(const void* from, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory", "m0");
 }
 // The same from `base` (uniform) + `offset` bytes (the lane's): the addresses then cost no vector instructions.
 __device__ __forceinline__ void copy_to_lds(const void* base, uint32_t offset, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to) : "memory", "m0");
 }
 __device__ __forceinline__ void copy_word_to_lds(const void* from, uint32_t to) {  // 4 bytes per lane, to `to` + 4 * lane
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 // Until at most N of the wavefront's copies (and other accesses) are on their way.
 template <int N>
 __device__ __forceinline__ void wait_copies() {

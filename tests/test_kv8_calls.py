@@ -1,6 +1,8 @@
 """Calls of the 8-bit key-value cache that the host decides on its own: streams of workspaces, sizes and strides that are
 accepted or refused.  No GPU needed."""
 import contextlib
+import os
+import re
 
 import pytest
 import torch
@@ -167,3 +169,16 @@ def test_nothing_is_asked_of_q_and_out_where_there_are_no_rows():
     for p in (None, torch.zeros(8, dtype=torch.bfloat16).data_ptr()):
         assert lib.moe_kv8_attend(None, c.ref, s.ref, 4, p, 0, 0, 0.0, p, 0, 0, None, None, None, 0) == B.MOE_ERR_INVALID_ARG
         assert b"cache.k is not device memory" in lib.moe_kv8_last_error()
+
+
+def test_assembly_that_writes_m0_names_it():
+    """The compiler is told of every register that inline assembly overwrites."""
+    folder = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2502_06888_amd", "csrc")
+    found = 0
+    for name in os.listdir(folder):
+        for text in re.findall(r"asm volatile\((.*?)\);\n", open(os.path.join(folder, name)).read(), flags=re.S):
+            code, _, rest = text.partition('" ::')
+            if re.search(r"\bm0\b", code):
+                found += 1
+                assert '"m0"' in rest, text
+    assert found >= 3
