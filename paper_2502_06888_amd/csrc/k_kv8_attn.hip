@@ -931,8 +931,6 @@ __global__ __launch_bounds__(256, 4) void prompt_weights_kernel(Cache c, Step s,
     const uint32_t qt_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) u32x4*)&qt[0][0];
     const uint32_t ml_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float2*)&ml[0][0];
     const float* stats = (const float*)(sp.final_ml + (int64_t)pair * sp.tile_rows);
-    // U + 1 copies of every wavefront, so that it can count them (rows past the end: the last one again; where there
-    // are more wavefronts than units some copy the same, and so do all the statistics)
     // The lane's row of q in the next tile to copy, stepped on by 32 rows; past the end the last row again.
     const uint16_t* heads = a.q.p + (int64_t)hk * G * a.q.head + grp * 8;
     const uint16_t* last = heads + (int64_t)(q.row0 + q.n_new - 1) * a.q.row + (int64_t)(G - 1) * a.q.head;
