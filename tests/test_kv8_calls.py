@@ -175,7 +175,7 @@ def test_assembly_that_writes_m0_names_it():
     """The compiler is told of every register that inline assembly overwrites."""
     folder = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2502_06888_amd", "csrc")
     found = 0
-    for name in os.listdir(folder):
+    for name in sorted(n for n in os.listdir(folder) if n.endswith((".hip", ".h"))):
         for text in re.findall(r"asm volatile\((.*?)\);\n", open(os.path.join(folder, name)).read(), flags=re.S):
             code, _, rest = text.partition('" ::')
             if re.search(r"\bm0\b", code):
