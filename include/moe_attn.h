@@ -136,6 +136,9 @@ moe_status moe_attn_prefetch(moe_attn_ctx* ctx, const moe_attn_batch* first);
  * step->next_position, null: cached, plus the token's place) as above; the new k and v (rounded to bf16) go through
  * moe_kv8_append, q (rounded to bf16) through moe_kv8_attend, then the output projection and the residual.
  *   cache: n_kv_heads and head_dim of the context; step->n_rows at most max(max_seqs, max_group_seqs).
+ *     Of the context the call uses weights, activations and partial sums: max_len, which sizes the staging of bf16 caches, may
+ *     be 1 where moe_attn_forward_group is not called, whatever the length of the 8-bit cache, and max_seqs 1 beside
+ *     max_group_seqs rows.
  *   h_in, h_out: device, bf16 [n_rows, d_model]; h_out may be h_in.  Rows of no sequence are left as they were.
  *   weight_in, weight_out, workspace: as for moe_kv8_attend (moe_kv8_attend_workspace_bytes with the context's n_q_heads).
  * Runs on the compute stream, whose order it follows; everything is on the device, so the call is a plain run of kernels

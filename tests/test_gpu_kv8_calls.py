@@ -161,3 +161,40 @@ def test_a_step_without_rows_carries_the_weights_over_and_needs_no_rows():
     w = torch.full_like(w_in, -5.0)
     Q.attend(cache, step, rows, rows, w_in, w)
     assert torch.equal(w[0, :, :60], w_in[0, :, :60]) and bool((w[1] == -5).all())
+
+
+@pytest.mark.parametrize("hd,heads,kv,cached,new", [
+    (128, 8, 2, [100, 31], [1, 1]),                  # decode_kernel, one range
+    (64, 12, 2, [5000, 17], [2, 1]),                 # several
+    (64, 8, 2, [10, 64], [40, 23]),                  # prompts: four, three, five and eight heads of a group, and one
+    (128, 9, 3, [0, 300, 5], [130, 257, 0]),
+    (32, 10, 2, [33], [150]),
+    (64, 8, 1, [0, 900], [530, 300]),
+    (32, 4, 4, [70, 0], [200, 33]),
+    (64, 14, 2, [1500], [700]),                      # rows split between workgroups
+])
+def test_strides_with_weights(hd, heads, kv, cached, new):
+    """q as a slice of a fused projection, out as a slice of something wider, rows and heads apart by strides of their own."""
+    block = 32
+    g = torch.Generator().manual_seed(36 + heads + hd)
+    n, total = len(cached), [c + m for c, m in zip(cached, new)]
+    L = -(-max(total) // block) * block + block
+    cache, codes, scale = filled(g, n, kv, L, hd, block, total)
+    step, off = step_for(cached, new)
+    m = off[-1]
+    fused = rand(g, (m + 2, heads + 2 * kv, hd), 2.0).to(DEV)
+    q = fused[:, :heads]
+    wide = torch.full((heads + 1, m + 3, hd + 24), -3.0, dtype=torch.bfloat16, device=DEV)
+    out = wide[1:, 1:, 8:8 + hd].transpose(0, 1)     # heads farther apart than rows
+    w_in = torch.rand((n, kv, L), generator=g)
+    w = torch.full((n, kv, L), -5.0, device=DEV)
+    before = fused.clone()
+    Q.attend(cache, step, q, out, w_in.to(DEV), w)
+    torch.cuda.synchronize()
+    ref, want, spread, mag = R.attend(codes[0], scale[0], codes[1], scale[1], q.cpu(), cached, off, block, w_in)
+    assert bool(((out[:m].cpu().double() - ref[:m]).abs() <= bounds(ref, spread, mag, hd)[:m]).all())
+    out[:m] = -3.0
+    assert bool((wide == -3).all()) and torch.equal(fused, before)               # nothing beside the heads is written
+    held = ~want.isnan()
+    assert bool(((w.cpu().double() - want).abs() <= weight_bounds(want, mag[:m], hd))[held].all())
+    assert bool((w.cpu()[~held] == -5).all())
