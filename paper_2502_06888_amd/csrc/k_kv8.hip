@@ -145,8 +145,8 @@ struct Select {
 // One group of WAVES wavefronts per (sequence, head), KPT keys per lane in registers (slot = step * lanes + lane).  The key
 // of the keep-th largest weight is found by halving the range of keys, 32 times: the compares of a step leave a count in
 // scalar registers, groups of several wavefronts add theirs up through LDS.  Then the ranks of the chosen slots,
-// by ballots and one scan over the (step, wavefront) counts.  Reads weights and positions once: 4096 pairs of 576 slots
-// take one wavefront each; a few pairs of thousands of slots would leave the chip idle, so 16 wavefronts share one.
+// by ballots and one scan over the (step, wavefront) counts.  Reads weights and positions once.  Pairs that fill the chip
+// take one wavefront each; a few pairs would leave it idle, so 16 wavefronts share one.
 // The halving ends as soon as a bound parts off just `keep` keys, after 20 steps or so where weights differ.
 // Bound by latency: 4096 pairs of 545 slots 19 us (45 MB), 32 pairs of 7500 slots 17 us.
 template <int WAVES, int KPT>
@@ -475,12 +475,20 @@ void launch_evict(hipStream_t st, const Cache& c, const int32_t* held, int max_h
     const Select a{held, max_held, keep, recent, next_position, weight_in, weight_out, c.position, position_out, (int32_t*)ws, kept};
     const int most = max_held > keep ? max_held : keep;  // slots that the lanes have to cover
     const unsigned p = (unsigned)pairs, p4 = (unsigned)((pairs + 3) / 4);
-    // a wavefront per pair as long as 16 keys per lane do, then 16 of them up to 32 keys per lane (8 pairs of 32000 slots, with the
-    // move, 60 us, from memory by 256 threads 290), then from memory; no more keys per lane than
-    // needed, since the compares are what a step of the halving costs (8000 slots: 18 us with 8 keys per lane, 25 with 16)
+    // Up to 512 slots a wavefront per pair.  Up to 1024, and up to 2048, 16 wavefronts as long as the chip takes all pairs at once, one
+    // and two workgroups on every unit; with more pairs one.  16 wavefronts / one, us: 500 slots of 8 pairs 8.8 / 8.1, of 4096 112 / 15;
+    // 1000 of 8 pairs 9.5 / 13.8, of 256 12.2 / 16.2, of 384 18.3 / 16.7, of 4096 137 / 30; 1500 of 8 pairs 10.2 / 20.9, of 512 19.9 /
+    // 24.0, of 640 26.5 / 26.3, of 4096 143 / 45; 2000 of 512 21.2 / 30.2, of 4096 150 / 76.
+    // Beyond, 16 wavefronts up to 32 keys per lane (8 pairs of 32000 slots, with the move, 60 us, from memory by 256 threads 290), then from
+    // memory.  No more keys per lane than needed, since the compares are what a step of the halving costs (8000 slots: 18 us with 8
+    // keys per lane, 25 with 16).
+    const bool one = pairs > (most <= 1024 ? 256 : 512);
     if (most <= 512) hipLaunchKernelGGL((select_kernel<1, 8>), dim3(p4), dim3(256), 0, st, c, a);
-    else if (most <= 768) hipLaunchKernelGGL((select_kernel<1, 12>), dim3(p4), dim3(256), 0, st, c, a);
-    else if (most <= 1024) hipLaunchKernelGGL((select_kernel<1, 16>), dim3(p4), dim3(256), 0, st, c, a);
+    else if (one && most <= 768) hipLaunchKernelGGL((select_kernel<1, 12>), dim3(p4), dim3(256), 0, st, c, a);
+    else if (one && most <= 1024) hipLaunchKernelGGL((select_kernel<1, 16>), dim3(p4), dim3(256), 0, st, c, a);
+    else if (one && most <= 1280) hipLaunchKernelGGL((select_kernel<1, 20>), dim3(p4), dim3(256), 0, st, c, a);
+    else if (one && most <= 1536) hipLaunchKernelGGL((select_kernel<1, 24>), dim3(p4), dim3(256), 0, st, c, a);
+    else if (one && most <= 2048) hipLaunchKernelGGL((select_kernel<1, 32>), dim3(p4), dim3(256), 0, st, c, a);
     else if (most <= 4096) hipLaunchKernelGGL((select_kernel<16, 4>), dim3(p), dim3(1024), 0, st, c, a);
     else if (most <= 8192) hipLaunchKernelGGL((select_kernel<16, 8>), dim3(p), dim3(1024), 0, st, c, a);
     else if (most <= 16384) hipLaunchKernelGGL((select_kernel<16, 16>), dim3(p), dim3(1024), 0, st, c, a);

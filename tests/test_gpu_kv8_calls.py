@@ -5,7 +5,7 @@ import torch
 
 from oracle import kv8_ref as R
 from paper_2502_06888_amd import kv8_binding as Q
-from test_gpu_kv8 import bounds, filled, ints, rand, step_for, weight_bounds
+from test_gpu_kv8 import bounds, evict_state, filled, ints, rand, same, step_for, weight_bounds
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -198,3 +198,25 @@ def test_strides_with_weights(hd, heads, kv, cached, new):
     held = ~want.isnan()
     assert bool(((w.cpu().double() - want).abs() <= weight_bounds(want, mag[:m], hd))[held].all())
     assert bool((w.cpu()[~held] == -5).all())
+
+
+@pytest.mark.parametrize("most,keep,recent,kind", [(500, 448, 9, "random"), (700, 512, 0, "ties"), (1000, 512, 64, "random"), (1024, 16, 0, "nan"),
+                                                   (1200, 1024, 30, "ties"), (1280, 640, 0, "nan"), (1500, 1024, 64, "random"), (1536, 1520, 3, "ties"),
+                                                   (2000, 1024, 0, "nan"), (2048, 1008, 1008, "random")])
+def test_many_pairs_keep_what_few_keep(most, keep, recent, kind):
+    """Pairs that fill the chip have a wavefront each, few share many: the same result, to the last bit."""
+    block, hd, kv, n = 16, 32, 8, 66
+    held = [(most - 37 * s) % (most + 1) if s else most for s in range(n)]
+    many, _, _, w, pos, nxt = evict_state(block, hd, kv, held, kind, most + keep)
+    few = Q.Kv8Cache(*(t.clone() for t in (many.k, many.v, many.k_scale, many.v_scale)), block, many.position.clone())
+    outs = []
+    for cache, parts in ((many, [(0, n)]), (few, [(s, min(s + 16, n)) for s in range(0, n, 16)])):
+        w_out, kept = torch.full((n, kv, w.shape[2]), -5.0, device=DEV), torch.full((n, kv, keep), -9, dtype=torch.int32, device=DEV)
+        p_out = torch.full_like(cache.position, -5)
+        for a, b in parts:
+            one = Q.Kv8Cache(*(t[a:b] for t in cache.tensors[:4]), block, cache.position[a:b])
+            Q.evict(one, ints(held[a:b]), most, keep, recent, ints(nxt[a:b]), w[a:b].to(DEV), w_out[a:b], p_out[a:b], kept[a:b])
+        torch.cuda.synchronize()
+        outs.append((*cache.tensors[:4], w_out, p_out, kept))
+    for a, b in zip(*outs):
+        same(a, b)
