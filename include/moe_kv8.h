@@ -84,14 +84,18 @@ moe_status moe_kv8_append(void* stream, const moe_kv8_cache* cache, const moe_kv
  * moe_kv8_attend -- softmax attention of the new tokens over the cache, after moe_kv8_append of the same step: token i
  * of sequence s sees slots 0 .. cached[s] + i, so the whole past and the new tokens up to itself.
  *   q, out: bf16, element (row, head, i) at row * row_stride + head * head_stride + i; 16-byte aligned, strides
- *     multiples of 8; no two (row, head) of out may share an element.  Without weight_out, out may be q with the same strides; else they share no element.  n_q_heads: a multiple of n_kv_heads, at most 8 times it.
+ *     multiples of 8; no two (row, head) of out may share an element.  Without weight_out, out may be q with the same
+ *     strides; else they share no element.  n_q_heads: a multiple of n_kv_heads, at most 8 times it.
  *   softmax_scale: factor of the scores; 0 stands for 1 / sqrt(head_dim).
  *   weight_out (may be null): [n_seq, n_kv_heads, max_len] accumulated attention weights.  Slot j of sequence s
  *     gets weight_in's value (0 for new slots, or for all when weight_in is null) plus the softmax weights that the
  *     step's tokens and the head's query heads gave it; weight_in may be weight_out.  Slots a sequence does
  *     not hold are left as they were.
- * Rows of no sequence are left as they were; of a step without rows q and out are not looked at.  Scores, softmax and sums are kept in 32 bits.  The result of a
- * sequence does not depend on what the others hold; how its sums are split follows from the numbers in the structs
+ * Rows of no sequence are left as they were; of a step without rows q and out are not looked at.  Scores, the softmax's
+ * statistics and all sums are kept in 32 bits, and so are the accumulated weights.  The weights enter the matrix product with V
+ * as bf16: as two of them, with 16 bits together, where min(max_new, n_rows) * n_q_heads / n_kv_heads is at most 16, rounded once
+ * (by up to 2^-8 of each weight) where it is more, so that a token's output is more exact decoded than within a prompt.  The result of
+ * a sequence does not depend on what the others hold; how its sums are split follows from the numbers in the structs
  * and its own length.
  * workspace: moe_kv8_attend_workspace_bytes() of device memory, 256-byte aligned (may be null when that is 0).  It
  * depends on the sizes and bounds only.
