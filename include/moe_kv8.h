@@ -65,7 +65,8 @@ typedef struct {
     int32_t reserved;   /* 0 */
     const int32_t* row_offsets;   /* [n_seq + 1], non-decreasing; null: every sequence brings max_new rows */
     const int32_t* cached;        /* [n_seq] slots held before the step */
-    const int32_t* next_position; /* [n_seq] position of the first new token; null: cached */
+    const int32_t* next_position; /* [n_seq] position of the first new token; null: cached, for sequences that have never been
+                                     evicted from (behind an eviction positions run ahead of the slots held) */
 } moe_kv8_step;
 
 /*
@@ -109,13 +110,15 @@ moe_status moe_kv8_attend(void* stream, const moe_kv8_cache* cache, const moe_kv
 
 /*
  * moe_kv8_evict -- brings every sequence that holds more than `keep` slots down to `keep`, per key-value head: the slots
- * whose position is at least next_position[s] - recent stay, and of the others those with the largest weight (ties: the
- * lower slot; NaN: last), `keep` in all.  Chosen slots below `keep` stay where they are; the i-th slot below `keep` that
+ * whose position is at least next_position[s] - recent stay (recent 0: none for its position), and of the others those with
+ * the largest weight (ties: the lower slot; NaN: last), `keep` in all.  Chosen slots below `keep` stay where they are; the i-th slot below `keep` that
  * was not chosen takes over the i-th chosen slot from `keep` on: codes, weight, position.  A block's scale becomes the
  * largest of its own and those that come in, and its codes are rounded to it.  The caller then sets the
  * sequence's number of slots to min(held, keep).  Sequences that hold `keep` or fewer keep everything.
  *   keep: a multiple of block, 1..max_len;  recent: 0..keep;  held: [n_seq], at most max_held <= max_len.
- *   next_position: [n_seq], position of the token to come; null: held.
+ *   next_position: [n_seq], position of the token to come; null: held, which is that position only in sequences that have
+ *     never been evicted from and began at position 0.  Behind an eviction positions run ahead of the slots held: with null all
+ *     of them would count as recent, and weights decide nothing.
  *   weight_in -> weight_out: as in moe_kv8_attend, the same tensor or two that do not overlap; of weight_out
  *     only slots below min(held, keep) are written.
  *   position_out: where the positions go (again only below min(held, keep)); null: into cache->position itself.

@@ -100,7 +100,8 @@ class Kv8Cache:
 
 class Kv8Step:
     """The new tokens of one step.  `cached` and the other arrays are read when the kernels run, so they may be updated
-    in place between steps (also between replays of a captured graph) within the bounds given here."""
+    in place between steps (also between replays of a captured graph) within the bounds given here.  ``next_position`` may be
+    left out for sequences that have never been evicted from."""
 
     def __init__(self, cached, n_rows: int, max_new: int, max_cached: int, row_offsets=None, next_position=None):
         import torch
@@ -209,7 +210,8 @@ def evict_workspace(cache: Kv8Cache, keep: int):
 
 def evict(cache: Kv8Cache, held, max_held: int, keep: int, recent: int, next_position, weight_in, weight_out=None,
           position_out=None, kept=None, workspace=None, stream=None):
-    """Brings every sequence down to `keep` slots; weights go to `weight_out` (in place when None)."""
+    """Brings every sequence down to `keep` slots; weights go to `weight_out` (in place when None).  ``next_position`` may be
+    None for sequences that have never been evicted from and began at position 0."""
     import torch
     if weight_out is None:
         weight_out = weight_in

@@ -220,3 +220,26 @@ def test_many_pairs_keep_what_few_keep(most, keep, recent, kind):
         outs.append((*cache.tensors[:4], w_out, p_out, kept))
     for a, b in zip(*outs):
         same(a, b)
+
+
+@pytest.mark.parametrize("most", [200, 700, 40000])
+def test_a_second_eviction_goes_by_the_positions_that_the_caller_gives(most):
+    """Positions run ahead of the slots held once a sequence has been evicted from; without `recent` no slot stays for its position."""
+    block, hd, kv, keep = 16, 32, 2, 64
+    held, seen = [most, most - 9], [most, most - 9]
+    cache, codes, scale, w, pos, _ = evict_state(block, hd, kv, held, "random", most)
+    cache.position.copy_(torch.arange(w.shape[2], dtype=torch.int32))
+    pos[:] = torch.arange(w.shape[2], dtype=torch.int32)
+    weight = w.to(DEV)
+    for gone, recent, to in ((0, 20, 64), (5, 16, 48), (10, 0, 16)):         # gone: positions whose tokens are no longer held
+        nxt = None if to == 64 else ints(seen)                               # never evicted from: the slots held
+        w_ref, p_ref, _ = R.evict(codes, scale, w, pos, held, to, recent, seen, block)
+        Q.evict(cache, ints(held), max(held), to, recent, nxt, weight)
+        held = [min(h, to) for h in held]
+        for s, h in enumerate(held):
+            same(weight[s, :, :h], w_ref[s, :, :h])
+            assert torch.equal(cache.position[s, :, :h].cpu().long(), p_ref[s, :, :h])
+            if recent:
+                assert int((cache.position[s, :, :h] >= seen[s] - recent).sum()) == kv * (recent - gone)
+        w, pos = weight.cpu(), cache.position.cpu()
+        seen = [p + 5 for p in seen]                                         # as if tokens had come and gone
