@@ -539,10 +539,10 @@ __global__ __launch_bounds__(256) void merge_kernel(Cache c, Step s, Attend a, S
 // The weights are rounded once, to bf16 (by up to 2^-8), as the operand of the second product; their sum takes the unrounded
 // ones.  The 16 bits that decode_kernel gives them for nothing would be a second product here, of the two that bound the kernel.
 //
-// Two prompts of 3907 and 4096 tokens, 32 / 8 heads of 128: 266 us, 9 of them for dequantising ahead, 1.01 PFLOP/s (a large
-// library product of bf16 reaches 1.30 on this card): the matrix cores are busy 48 % of the time at the 2.0 GHz that the power
-// limit leaves, vector instructions (half of them exponentials) 60 %, two wavefronts per SIMD.  32 prompts of 512 tokens:
-// 128 us, 0.54 PFLOP/s and 2.4 TB/s: the start and end of a tile of rows weigh as much as its 4.5 steps.
+// Two prompts of 3907 and 4096 tokens, 32 / 8 heads of 128: 265 to 271 us, 9 of them for dequantising ahead, 1.0 PFLOP/s (a large
+// library product of bf16 reaches 1.30 on this card): the matrix cores are busy 50 % of the time at the 1.9 GHz that the power
+// limit leaves, vector instructions (half of them exponentials) 44 %, two wavefronts per SIMD.  32 prompts of 512 tokens:
+// 129 us, 0.53 PFLOP/s and 2.3 TB/s: the start and end of a tile of rows weigh as much as its 4.5 steps.
 template <int HD>
 struct Tile {
     static constexpr int kUnits = HD / 8;            // of K, and of V
