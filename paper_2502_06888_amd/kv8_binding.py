@@ -2,7 +2,8 @@
 
 Argument marshalling and shape checks only: quantisation, attention and eviction run in the HIP library.  torch is
 used for device memory and streams; every call goes to the current stream of the cache's device unless one is given.  On a
-given stream the caller sees to it that the tensors are ready; they may be dropped as soon as the call returns.
+given stream the caller sees to it that the tensors are ready; they may be dropped as soon as the call returns, but for calls on
+a ``torch.cuda.ExternalStream``, which need them until the stream is done.
 """
 from __future__ import annotations
 
@@ -146,7 +147,12 @@ def _made_on(stream):
 
 
 def _used(stream, *tensors):
-    """Tensors of a call on `stream`: the caller may drop them behind the call, so the allocator is told who still uses them."""
+    """Tensors of a call on `stream`: the caller may drop them behind the call, so the allocator is told who still uses them.
+    Not of a stream that torch does not own: the allocator would ask it for an event when a tensor is freed, which may be after
+    the stream's end."""
+    import torch
+    if isinstance(stream, torch.cuda.ExternalStream):
+        return
     for t in tensors:
         if t is not None:
             t.record_stream(stream)
