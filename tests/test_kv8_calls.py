@@ -24,6 +24,11 @@ class FakeStream:
     cuda_stream = 0
 
 
+class ForeignStream:
+    """In the place of torch.cuda.ExternalStream, which takes a device to make."""
+    cuda_stream = 0
+
+
 @pytest.fixture
 def current(monkeypatch):
     """The stream that is current when a workspace is made, for each one made."""
@@ -73,6 +78,7 @@ def test_tensors_of_a_call_on_another_stream_are_recorded_on_it(monkeypatch):
     monkeypatch.setattr(Q, "_check", lambda status: None)                      # host tensors: refused by the library
     monkeypatch.setattr(A, "_check", lambda status, ctx=None: None)
     monkeypatch.setattr(Q, "_stream", lambda cache, stream: 0)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", ForeignStream)
     c, st = cache(), FakeStream()
     s = Q.Kv8Step(ints(3, 4), 2, 1, 4, row_offsets=ints(0, 1, 2), next_position=ints(3, 4))
     x = [torch.zeros((2, n, 64), dtype=torch.bfloat16) for n in (2, 2, 4, 4)]
@@ -92,7 +98,7 @@ def test_tensors_of_a_call_on_another_stream_are_recorded_on_it(monkeypatch):
         call(st)
         assert sorted(used, key=lambda u: u[0]) == sorted(((t.data_ptr(), st) for t in tensors), key=lambda u: u[0])
     for call, _ in calls[:3]:                                                  # nothing on the current stream, or on one that
-        for stream in (None, object.__new__(torch.cuda.ExternalStream)):       # may end before the tensors do
+        for stream in (None, ForeignStream()):                                 # may end before the tensors do
             used.clear()
             call(stream)
             assert not used
