@@ -24,10 +24,8 @@ def build(force: bool = True, verbose: bool = False) -> str:
     """Compile every source and link the shared library.  ``force`` recompiles everything."""
     os.makedirs(OBJ_DIR, exist_ok=True)
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    headers = [os.path.join(CSRC, "kernels.h"), os.path.join(CSRC, "attn_kernels.h"),
-               os.path.join(CSRC, "attn_ranges.h"), os.path.join(CSRC, "tile_rules.h"),
-               os.path.join(CSRC, "kv8_kernels.h"),
-               *(os.path.join(HERE, "..", "include", h) for h in ("moe.h", "moe_attn.h", "moe_kv8.h"))]
+    headers = [os.path.join(d, h) for d in (CSRC, os.path.join(HERE, "..", "include"))
+               for h in sorted(os.listdir(d)) if h.endswith(".h")]
     jobs = []
     for name in SOURCES:
         src = os.path.join(CSRC, name)

@@ -1,67 +1,19 @@
 // C ABI of the 8-bit key-value cache (include/moe_kv8.h): argument checks, then the launches.  No state but the
 // error text of each thread.
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 
+#include "call_checks.h"
 #include "kv8_kernels.h"
 
 using namespace kkv8;
+using namespace kcall;
 
 namespace {
 
-thread_local char g_error[256];
+thread_local CallError g_error;
 constexpr double kLog2e = 1.4426950408889634;
 
-moe_status fail(moe_status s, const char* fmt, ...) {
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_error, sizeof g_error, fmt, ap);
-    va_end(ap);
-    return s;
-}
-
-#define TRY(expr)                          \
-    do {                                   \
-        const moe_status s_ = (expr);      \
-        if (s_ != MOE_OK) return s_;       \
-    } while (0)
-
-// Device of the tensors of a call: the first one sets it, the others have to be there too.
-struct Where {
-    int device = -1;
-    moe_status on(const void* p, const char* name, unsigned align) {
-        if (!p) return fail(MOE_ERR_INVALID_ARG, "%s is null", name);
-        if (((uintptr_t)p & (align - 1)) != 0) return fail(MOE_ERR_INVALID_ARG, "%s is not aligned to %u bytes", name, align);
-        hipPointerAttribute_t at;
-        if (hipPointerGetAttributes(&at, p) != hipSuccess) {
-            (void)hipGetLastError();
-            return fail(MOE_ERR_INVALID_ARG, "%s is not device memory", name);
-        }
-        if (at.type != hipMemoryTypeDevice) return fail(MOE_ERR_INVALID_ARG, "%s is not device memory", name);
-        if (device >= 0 && at.device != device) return fail(MOE_ERR_INVALID_ARG, "%s is on device %d, other tensors on %d", name, at.device, device);
-        device = at.device;
-        return MOE_OK;
-    }
-};
-
-// The tensors' device for the time of the launches, where it is not the current one.
-class OnDevice {
-public:
-    explicit OnDevice(int device) {
-        if (hipGetDevice(&before_) != hipSuccess) before_ = device;
-        if (before_ != device) failed_ = hipSetDevice(device) != hipSuccess;
-        moved_ = before_ != device && !failed_;
-    }
-    ~OnDevice() {
-        if (moved_) (void)hipSetDevice(before_);
-    }
-    bool failed() const { return failed_; }
-
-private:
-    int before_ = 0;
-    bool moved_ = false, failed_ = false;
-};
+#define fail g_error.fail  // the text goes to this thread's buffer
 
 moe_status check_sizes(const moe_kv8_cache* c) {
     if (!c) return fail(MOE_ERR_INVALID_ARG, "cache is null");
@@ -115,22 +67,6 @@ moe_status check_rows(const void* p, const char* name, int64_t row, int64_t head
     return MOE_OK;
 }
 
-// Whether two of rows x heads pieces of `width` elements, at these strides, share an element.
-bool pieces_overlap(int64_t rows, int64_t heads, int64_t row, int64_t head, int64_t width) {
-    if ((heads > 1 && head < width) || (rows > 1 && row < width)) return true;
-    if (rows <= 1 || heads <= 1) return false;
-    typedef __int128 wide;  // any stride times any number of rows
-    if (row >= (wide)(heads - 1) * head + width || head >= (wide)(rows - 1) * row + width) return false;  // one inside the other
-    // `down` rows on and `back` heads back there is another piece, |down * row - back * head| away
-    for (int64_t back = 1; back < heads; ++back) {
-        const wide to = (wide)back * head;
-        const int64_t down = (int64_t)(to / row);
-        if (down >= 1 && down < rows && to - (wide)down * row < width) return true;
-        if (down + 1 < rows && (wide)(down + 1) * row - to < width) return true;
-    }
-    return false;
-}
-
 moe_status check_workspace(const void* ws, int64_t bytes, int64_t need, Where* w) {
     if (need == 0) return MOE_OK;
     if (bytes < need) return fail(MOE_ERR_OOM, "workspace of %lld bytes, need %lld", (long long)bytes, (long long)need);
@@ -162,7 +98,7 @@ moe_status check_append(const moe_kv8_cache* cache, const moe_kv8_step* step, co
                         int64_t row_stride, int64_t head_stride, int* device) {
     TRY(check_sizes(cache));
     TRY(check_step_sizes(cache, step));
-    Where w;
+    Where w{&g_error};
     TRY(check_cache(cache, &w));
     TRY(check_step(step, &w));
     *device = w.device;
@@ -184,7 +120,7 @@ moe_status check_attend(const moe_kv8_cache* cache, const moe_kv8_step* step, in
         return fail(MOE_ERR_INVALID_ARG, "softmax_scale must be finite, times log2(e) too, and not negative");
     if (step->n_rows > 0 && pieces_overlap(step->n_rows, n_q_heads, out_row_stride, out_head_stride, cache->head_dim))
         return fail(MOE_ERR_INVALID_ARG, "rows or heads of out overlap");
-    Where w;
+    Where w{&g_error};
     TRY(check_cache(cache, &w));
     TRY(check_step(step, &w));
     *device = w.device;
@@ -227,7 +163,7 @@ Step step_of_call(const moe_kv8_step* s) { return step_of(s); }
 
 extern "C" {
 
-const char* moe_kv8_last_error(void) { return g_error; }
+const char* moe_kv8_last_error(void) { return g_error.text; }
 
 moe_status moe_kv8_append(void* stream, const moe_kv8_cache* cache, const moe_kv8_step* step, const void* k_new,
                           const void* v_new, int64_t row_stride, int64_t head_stride) {
@@ -298,7 +234,7 @@ moe_status moe_kv8_evict(void* stream, const moe_kv8_cache* cache, const int32_t
     if (recent < 0 || recent > keep) return fail(MOE_ERR_INVALID_ARG, "recent %d outside 0..keep", recent);
     if (max_held < 0 || max_held > cache->max_len) return fail(MOE_ERR_INVALID_ARG, "max_held %d outside 0..max_len", max_held);
     if (!cache->position) return fail(MOE_ERR_INVALID_ARG, "eviction needs cache.position");
-    Where w;
+    Where w{&g_error};
     TRY(check_cache(cache, &w));
     TRY(w.on(held, "held", 4));
     if (next_position) TRY(w.on(next_position, "next_position", 4));

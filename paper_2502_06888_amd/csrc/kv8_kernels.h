@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include "../../include/moe_kv8.h"
+#include "attn_device.h"
 
 namespace kkv8 {
 
@@ -67,18 +68,13 @@ Step step_of_call(const moe_kv8_step* s);
 
 // ---- device helpers shared by the kernels -------------------------------------------------------
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-
-__device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
+using namespace kattn;
 
 // What a sequence brings and holds, every number brought into its bounds.
 struct Seq {
     int row0, n_new, cached;
 };
-__device__ __forceinline__ Seq sequence(const Cache& c, const Step& s, int seq) {
+__device__ __forceinline__ Seq sequence(int max_len, const Step& s, int seq) {
     Seq q;
     if (s.row_offsets != nullptr) {
         q.row0 = clampi(s.row_offsets[seq], 0, s.n_rows);
@@ -88,9 +84,10 @@ __device__ __forceinline__ Seq sequence(const Cache& c, const Step& s, int seq) 
         q.n_new = s.max_new;
     }
     q.cached = clampi(s.cached[seq], 0, s.max_cached);
-    q.n_new = min(q.n_new, c.max_len - q.cached);
+    q.n_new = min(q.n_new, max_len - q.cached);
     return q;
 }
+__device__ __forceinline__ Seq sequence(const Cache& c, const Step& s, int seq) { return sequence(c.max_len, s, seq); }
 
 // Sequence whose rows include `row`, and the token's place in it; -1 where there is none.
 __device__ __forceinline__ int seq_of_row(const Cache& c, const Step& s, int row, int* token, Seq* q) {
@@ -120,12 +117,6 @@ __device__ __forceinline__ float fit(float x) { return x != x ? x : __builtin_am
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(fit(a), fit(b), 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(fit(c), fit(d), w, true);
-}
-__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {  // to nearest even
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
 }
 // Four codes rounded again to another scale: `by` = old scale / new scale, a power of two of at most 1.
 __device__ __forceinline__ uint32_t rescale4(uint32_t w, float by) {
