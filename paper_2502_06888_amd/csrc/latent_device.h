@@ -1,0 +1,35 @@
+// Shared by the kernels of the latent cache: transposed reads of LDS, the parts of a row's sums.
+#pragma once
+#include "latent_kernels.h"
+
+namespace klat {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <class T>
+__device__ __forceinline__ uint32_t lds_address(T* p) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) T*)p;
+}
+__device__ __forceinline__ u32x4 read_lds(uint32_t at) { return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)at; }
+__device__ __forceinline__ void write_lds(uint32_t at, const u32x4 v) { *(__attribute__((address_space(3))) u32x4*)(uintptr_t)at = v; }
+// Four rows of 16 elements of 16 bits, transposed: lane l of 16 points at four elements of row l / 4, 4 * (l % 4) on, and gets element l
+// of the four rows.
+__device__ __forceinline__ u32x2 read_transposed(uint32_t at) {
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)at));
+}
+__device__ __forceinline__ u32x4 join(const u32x2 a, const u32x2 b) { return u32x4{a.x, a.y, b.x, b.y}; }
+
+// Sums of the absorbed form, cut into parts: a row's slots into ranges of `per`, the prefix into ranges of its own, behind them.
+struct Parts {
+    int per, pre_per;  // slots of a range: of a sequence, of the prefix
+    int own, all;      // parts of a row at most: of its sequence, with the prefix's
+    float* acc;        // [row, head, part, latent] sums of weight * latent
+    float2* ml;        // [row, head, part] reference, sum of weights
+};
+
+int64_t absorb_groups(const Cache& c, const Heads& h, int n_rows);
+void launch_absorb(hipStream_t st, const Cache& c, const Heads& h, const Rows& q, int n_rows, uint16_t* out);
+int64_t finish_groups(const Heads& h, int n_rows);
+void launch_finish(hipStream_t st, const Cache& c, const Step& s, const Heads& h, const RowsOut& out, const Parts& parts);
+
+}  // namespace klat
