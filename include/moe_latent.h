@@ -74,7 +74,7 @@ typedef enum { MOE_LATENT_AUTO = 0, MOE_LATENT_ABSORBED = 1, MOE_LATENT_EXPANDED
  *     no two (row, head) of out share an element, and q and out share none.
  *   softmax_scale: 0 stands for 1 / sqrt(nope_dim + rope_dim).
  * Rows of no sequence are left as they were.  Scores, the softmax's statistics and sums are kept in 32 bits.  Rounded to bf16
- * on the way: the softmax weights, in the absorbed form a and (as two of them, with 16 bits together) u, in the expanded one keys and values,
+ * on the way: the softmax weights, in the absorbed form a and u (each as two of them, with 16 bits together), in the expanded one keys and values,
  * finite ones to finite ones.  A latent that is not finite reaches the rows that see it, all their elements, and no others.
  * The result of a sequence does not depend on what the others hold; how its sums are split follows from the numbers in the structs and
  * its own length.

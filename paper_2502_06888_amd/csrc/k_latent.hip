@@ -49,18 +49,19 @@ __global__ __launch_bounds__(256) void append_kernel(Cache c, Step s, Append a) 
     if (lane < c.rope) to[c.latent + lane] = (uint16_t)e;
 }
 
-// a[row][head] = w_k[head]^T n, then the part that carries the position: rows of latent + rope elements in bf16, in the
-// caller's order of rows and heads.
+// a[row][head] = w_k[head]^T n in bf16, then the part that carries the position, then what rounding a left over, in bf16, too:
+// rows of 2 * latent + rope elements, in the caller's order of rows and heads.  (a counts with 16 bits: rounded to 8 it would move
+// the scores, and with them the outputs, by more than the outputs' own rounding: 2.8e-3 over 3000 slots, where that is 1.7e-3.)
 //
 // One wavefront per (head, 128 latents, `each` tiles of 32 rows): its piece of w_k lies in LDS (nope_dim x 256 bytes) and is read
 // transposed by the LDS, four latents of four rows at a time, as the first operand: a^T = w_k^T n^T, so that a lane has one row and
 // four latents side by side.  The result goes through LDS to leave in pieces of 256 bytes.
 template <int NOPE>
 __global__ __launch_bounds__(64) void absorb_kernel(Cache c, Heads h, Rows q, int n_rows, int each, uint16_t* out) {
-    __shared__ u32x4 w[NOPE * 16], o[32 * 16];
+    __shared__ u32x4 w[NOPE * 16], o[2][32 * 16];
     const int lane = threadIdx.x, col = lane & 31, grp = lane >> 5;
     const int chunks = c.latent / 128, head = blockIdx.x % h.n, rest = blockIdx.x / h.n, chunk = rest % chunks;
-    const int tile0 = rest / chunks * each, tiles = (n_rows + 31) / 32, width = c.latent + c.rope;
+    const int tile0 = rest / chunks * each, tiles = (n_rows + 31) / 32, width = 2 * c.latent + c.rope;
     // rows of w_k four at a time; 16-byte units of a row lie at an xor of its number, which spreads the transposed reads over the banks
     const uint16_t* from = h.w_k + head * h.w_k_head + chunk * 128 + (lane >> 4) * c.latent + ((lane & 15) ^ (lane >> 4 & 3) << 2) * 8;
     const uint32_t w_at = lds_address(w);
@@ -99,17 +100,26 @@ __global__ __launch_bounds__(64) void absorb_kernel(Cache c, Heads h, Rows q, in
         for (int b = 0; b < 4; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                u32x2 x;
-                x.x = pack_bf16(acc[b][4 * i], acc[b][4 * i + 1]);
-                x.y = pack_bf16(acc[b][4 * i + 2], acc[b][4 * i + 3]);
-                ((u32x2*)&o[col * 16 + ((b * 4 + i) ^ (col & 15))])[grp] = x;
+                u32x2 x, y;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float e = acc[b][4 * i + 2 * j], e2 = acc[b][4 * i + 2 * j + 1];
+                    x[j] = pack_bf16(e, e2);
+                    y[j] = pack_bf16(e - bf_lo(x[j]), e2 - bf_hi(x[j]));
+                }
+                const int at = col * 16 + ((b * 4 + i) ^ (col & 15));
+                ((u32x2*)&o[0][at])[grp] = x;
+                ((u32x2*)&o[1][at])[grp] = y;
             }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int in = i * 4 + (lane >> 4), row = row0 + in;
-            if (row < n_rows)
-                *(u32x4*)(out + ((int64_t)row * h.n + head) * width + chunk * 128 + (lane & 15) * 8) = o[in * 16 + ((lane & 15) ^ (in & 15))];
+            if (row < n_rows) {
+                uint16_t* to = out + ((int64_t)row * h.n + head) * width + chunk * 128 + (lane & 15) * 8;
+                *(u32x4*)to = o[0][in * 16 + ((lane & 15) ^ (in & 15))];
+                *(u32x4*)(to + c.latent + c.rope) = o[1][in * 16 + ((lane & 15) ^ (in & 15))];
+            }
         }
         if (chunk == 0) {
             const int units = c.rope / 8;

@@ -9,7 +9,7 @@ namespace klat {
 namespace {
 
 // How C lies in LDS: tiles of 32 slots, cut into groups of 64 elements (128 bytes), a group being 32 slots x 8 units of 16 bytes.
-// Unit u of slot r is at place u ^ twist(r): then neither the reads by slots (32 lanes, one unit each; keys) nor the transposed ones
+// Unit u of slot r is at place u ^ twist(r): then neither the reads by slots (16 lanes, one unit each; keys) nor the transposed ones
 // (8 slots, 64 bytes each; values) meet in a bank.  Rows whose width is half a group more than whole groups fill the last one twice.
 template <int DC, int DR>
 struct Tile {
@@ -19,29 +19,38 @@ struct Tile {
 __device__ __forceinline__ int twist(int slot) { return (slot >> 1 & 1) << 2 | (slot >> 2 & 3); }
 
 struct Run {  // one launch
-    int H, row_tiles;  // tiles of MW * 32 rows of a sequence (of the prefix: of all)
+    int H, row_tiles;  // tiles of 32 * MT rows of a sequence (of the prefix: of all)
     int per, ranges;   // slots of a range, ranges at most
     int part0;         // where the launch's parts are among a row's
     float qscale;
-    const uint16_t* a;  // [row, head, latent + rope]
+    const uint16_t* a;  // [row, head, 2 * latent + rope], see absorb_kernel
     Parts parts;
 };
 
-// A workgroup of four wavefronts takes MW * 32 rows of A and a range of slots: MW wavefronts side by side with 32 rows each
-// (in registers), and 4 / MW such teams that take the tiles of the range in turn and add up at the end.  Scores are formed
-// transposed, z^T = C A^T, so that a lane has one row of A: its softmax needs no exchange but one between two lanes, and the weights
-// are the second operand of u^T = C^T w as they stand.  LDS holds four tiles; a team's tiles come in a ring of MW, copied without
-// registers.  With MW = 1 nothing is shared: every wavefront copies, waits and computes by itself, the other three cover its waits.
-template <int DC, int DR, int MW, bool PREFIX>
-__global__ __launch_bounds__(256, 1) void absorbed_kernel(Cache c, Step s, Run run) {
+// A workgroup of 4 * MT wavefronts takes 32 * MT rows of A and a range of slots, SUB tiles at a time (a step; the next one comes
+// meanwhile, without registers):
+//   scores  z^T = C A^T, 16 slots x 16 rows, 16x16x32: a wavefront has 16 rows of A (in registers, as two bf16: see absorb_kernel; the
+//           second halves double the work of this product) and one half of every tile.  A lane has one row and four slots.
+//   sums    u^T = C^T w, 32 latents x 32 rows, 32x32x16: a wavefront has some blocks of 32 latents for all rows.  The weights go through LDS,
+//           the values are read from it transposed.
+// So a tile is read once from memory for all rows, its keys by the wavefronts of half the rows each and its values once; the sums take
+// 64 registers and the rows 136, which leaves two wavefronts to a SIMD.
+// References of the softmax are whole numbers, so that bringing sums or weights from one to another is exact.  The two wavefronts of a row
+// set theirs by their own halves; behind the barrier everybody sees both and goes on with the larger one.
+template <int DC, int DR, int MT, bool PREFIX>
+__global__ __launch_bounds__(256 * MT, 2) void absorbed_kernel(Cache c, Step s, Run run) {
     typedef Tile<DC, DR> T;
-    constexpr int KW = 4 / MW, STEPS = T::kWidth / 16, BLOCKS = DC / 32;
-    constexpr int AT_ONCE = BLOCKS > 8 ? 8 : 4;          // blocks of 32 elements that meet in LDS at a time
-    constexpr int RING = 4 * T::kBytes, SUMS = AT_ONCE * 4 * 4096;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[RING > SUMS || KW == 1 ? RING : SUMS];
-    __shared__ float2 sm_ml[4][32];
-    const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, grp = lane >> 5;
-    const int mw = wave % MW, team = wave / MW;
+    constexpr int WAVES = 4 * MT, GROUPS = 2 * MT, SUB = MT, M = 32 * MT;
+    constexpr int KEYS = T::kWidth / 32, LOW = DC / 32;               // products of a score: first halves, second ones
+    constexpr int BLOCKS = DC / 32 * MT / WAVES;                      // (block of latents, 32 rows) of a wavefront
+    constexpr int ROW_TILES = BLOCKS >= MT ? MT : 1;                  // of them 32-row tiles
+    constexpr int COLS = BLOCKS / ROW_TILES;                          // and blocks of latents
+    constexpr int STEP = SUB * T::kBytes, RING = 2 * STEP, SUMS = M * DC * 4;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[RING > SUMS ? RING : SUMS];
+    __shared__ __attribute__((aligned(16))) uint8_t weights[SUB * M * 64];  // [tile][row][32 slots] bf16
+    __shared__ float sm_ref[2][M], sm_sum[2][M];
+    const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, grp = lane >> 5, c16 = lane & 15, g16 = lane >> 4;
+    const int rows16 = wave % GROUPS, half = wave / GROUPS;
     int seq = 0, rest = blockIdx.x;
     if (!PREFIX) {
         seq = blockIdx.x % c.n_seq;
@@ -51,241 +60,235 @@ __global__ __launch_bounds__(256, 1) void absorbed_kernel(Cache c, Step s, Run r
     Seq q;
     if (PREFIX) q = Seq{0, s.n_rows, 0};
     else q = kkv8::sequence(c.max_len, s, seq);
-    const int rows = q.n_new * run.H, row0 = tile * MW * 32;
+    const int rows = q.n_new * run.H, row0 = tile * M;
     if (row0 >= rows) return;
-    const int last_row = min(row0 + MW * 32, rows) - 1;
     const int first = range * run.per;
-    const int sees = PREFIX ? c.prefix_len : q.cached + last_row / run.H + 1;  // slots that the last row sees
+    const int sees = PREFIX ? c.prefix_len : q.cached + (min(row0 + M, rows) - 1) / run.H + 1;  // slots that the last row sees
     const int end = min(first + run.per, sees);
     if (first >= end) return;
     const uint16_t* C = PREFIX ? c.prefix : c.rows + (int64_t)seq * c.max_len * T::kWidth;
-    const int r = row0 + mw * 32 + col, mine = min(r, rows - 1);
-    const int limit = PREFIX ? c.prefix_len : q.cached + mine / run.H + 1;  // slots that the lane's row sees
-    const int wave_least = PREFIX ? c.prefix_len : q.cached + min(row0 + mw * 32, rows - 1) / run.H + 1;  // that all its rows see
-    const int64_t row_head = (int64_t)q.row0 * run.H;
+    const int mine = min(row0 + rows16 * 16 + c16, rows - 1);                    // the lane's row, for the scores
+    const int limit = min(PREFIX ? c.prefix_len : q.cached + mine / run.H + 1, end);  // slots of the range that it sees end here
+    const int all_see = PREFIX ? c.prefix_len : q.cached + row0 / run.H + 1;     // slots that every row sees
+    const int64_t row_head = (int64_t)q.row0 * run.H + row0;
 
-    // copies: a wavefront brings 8 slots x 8 units at a time, of 4 / MW of the tile's four quarters
+    // copies: a wavefront brings 8 slots x 8 units at a time, one quarter of a tile
     const uint32_t lds_at = lds_address(lds);
-    const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_at + team * MW * T::kBytes);
-    const int in8 = lane >> 3;
-    uint32_t unit_at[2];  // byte of the row that the lane brings, in even and odd quarters
-#pragma unroll
-    for (int odd = 0; odd < 2; ++odd) unit_at[odd] = (uint32_t)(((lane & 7) ^ twist(odd * 8 + in8)) * 16);
+    const int in8 = lane >> 3, quarter = wave & 3, sub = wave >> 2;
+    const uint32_t unit_at = (uint32_t)(((lane & 7) ^ twist(quarter * 8 + in8)) * 16);
+    const uint32_t copy_at = __builtin_amdgcn_readfirstlane(lds_at + sub * T::kBytes + quarter * 1024);
     auto copy = [&](int buf, int j0) {
+        const uint32_t slot = (uint32_t)min(j0 + sub * 32 + quarter * 8 + in8, end - 1);  // past the end the last one again
+        const uint32_t at = slot * (T::kWidth * 2) + unit_at;
 #pragma unroll
-        for (int i = 0; i < KW; ++i) {
-            const int quarter = mw * KW + i;
-            const uint32_t slot = (uint32_t)min(j0 + quarter * 8 + in8, end - 1);  // past the end the last one again
-            const uint32_t at = slot * (T::kWidth * 2) + (quarter & 1 ? unit_at[1] : unit_at[0]);
-            const uint32_t to = ring_at + buf * T::kBytes + quarter * 1024;
-#pragma unroll
-            for (int g = 0; g < T::kGroups; ++g) {
-                if (T::kHalf && g == T::kGroups - 1) {  // the row ends within the group
-                    const uint32_t u = (quarter & 1 ? unit_at[1] : unit_at[0]) & 63;
-                    copy_to_lds((const uint8_t*)C + g * 128, slot * (T::kWidth * 2) + u, __builtin_amdgcn_readfirstlane(to + g * 4096));
-                } else {
-                    copy_to_lds((const uint8_t*)C + g * 128, at, __builtin_amdgcn_readfirstlane(to + g * 4096));
-                }
-            }
+        for (int g = 0; g < T::kGroups; ++g) {
+            const bool cut = T::kHalf && g == T::kGroups - 1;  // the row ends within the group
+            copy_to_lds((const uint8_t*)C + g * 128, cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, copy_at + buf * STEP + g * 4096);
         }
     };
-    constexpr int COPIES = KW * T::kGroups;  // of a wavefront for a tile
+    copy(0, first);
 
-    u32x4 af[STEPS];
+    u32x4 hi[KEYS], lo[LOW];
     {
-        const uint16_t* p = run.a + (row_head + mine) * T::kWidth + grp * 8;
+        const uint16_t* p = run.a + (row_head + (mine - row0)) * (T::kWidth + DC) + g16 * 8;
 #pragma unroll
-        for (int f = 0; f < STEPS; ++f) af[f] = *(const u32x4*)(p + f * 16);
+        for (int f = 0; f < KEYS; ++f) hi[f] = *(const u32x4*)(p + f * 32);
 #pragma unroll
-        for (int f = 0; f < STEPS; ++f) asm volatile("" : "+v"(af[f]));  // waited for here, not in the loop
+        for (int f = 0; f < LOW; ++f) lo[f] = *(const u32x4*)(p + T::kWidth + f * 32);
+#pragma unroll
+        for (int f = 0; f < KEYS; ++f) asm volatile("" : "+v"(hi[f]));  // waited for here, not in the loop
+#pragma unroll
+        for (int f = 0; f < LOW; ++f) asm volatile("" : "+v"(lo[f]));
     }
-    f32x16 acc[BLOCKS];
+    f32x16 acc[COLS][ROW_TILES];
 #pragma unroll
-    for (int b = 0; b < BLOCKS; ++b)
+    for (int b = 0; b < COLS; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
-    float ref = kEmpty, sum = 0.f;
+        for (int r = 0; r < ROW_TILES; ++r)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[b][r][i] = 0.f;
+    const int block0 = (MT > 1 && ROW_TILES == 1 ? wave & 3 : wave) * COLS, tile32 = MT > 1 && ROW_TILES == 1 ? wave >> 2 : 0;
+    float ref = kEmpty, sum = 0.f, sums_ref[ROW_TILES];
+#pragma unroll
+    for (int r = 0; r < ROW_TILES; ++r) sums_ref[r] = kEmpty;
 
-    // the lane's places in a tile: units 2 * (f % 4) + grp of its slot; four slots of 16 elements for the transposed reads
-    uint32_t key_at[4], value_at[2][2];
+    // the lane's places in a tile: units 4 * (f % 2) + g16 of its slot; four slots of 16 elements for the transposed reads
+    const int key_slot = half * 16 + c16;
+    uint32_t key_at[2], value_at[2][2];
 #pragma unroll
-    for (int f = 0; f < 4; ++f) key_at[f] = (uint32_t)(col * 128 + ((2 * f + grp) ^ twist(col)) * 16);
+    for (int f = 0; f < 2; ++f) key_at[f] = lds_at + (uint32_t)(key_slot * 128 + ((4 * f + g16) ^ twist(key_slot)) * 16);
 #pragma unroll
     for (int odd = 0; odd < 2; ++odd)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int slot = 8 * j + 4 * grp + ((lane & 15) >> 2), unit = odd * 4 + (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
-            value_at[odd][j] = (uint32_t)(slot * 128 + (unit ^ twist(slot)) * 16 + (lane & 1) * 8);
+            const int slot = 8 * grp + 4 * j + (c16 >> 2), unit = odd * 4 + (g16 & 1) * 2 + (lane >> 1 & 1);
+            value_at[odd][j] = lds_at + (uint32_t)(slot * 128 + (unit ^ twist(slot)) * 16 + (lane & 1) * 8);
         }
+    // weights: 64 bytes a row, its four units at an xor of the row
+    const uint32_t weights_at = lds_address(weights);
+    const int my_row = rows16 * 16 + c16;
+    const uint32_t put_at = weights_at + (uint32_t)(my_row * 64 + ((half * 2 + (g16 >> 1)) ^ (my_row >> 2 & 3)) * 16 + (g16 & 1) * 8);
+    const uint32_t get_at = weights_at + (uint32_t)((tile32 * 32 + col) * 64), get_xor = (uint32_t)(col >> 2 & 3);
 
-    // The sums stay in the accumulation registers: 256 of the lane's 512 with 512 latents, the rows of A 144 of the others.
-    auto pin = [&](int b) { asm volatile("" : "+a"(acc[b])); };
-    auto compute = [&](uint32_t at, int j0) {
-        f32x16 z;
+    const int steps = (end - first + SUB * 32 - 1) / (SUB * 32);
+    for (int t = 0; t < steps; ++t) {
+        const int j0 = first + t * SUB * 32, buf = t & 1;
+        wait_copies<0>();
+        __syncthreads();  // the step's tiles are there, and nobody reads the ones before it any more
+        if (t + 1 < steps) copy(buf ^ 1, j0 + SUB * 32);
+        // A latent that is not finite, in a slot that some row of the workgroup does not see, would reach that row as 0 times it.
+        // In tiles where that can be, such slots give up their latents and get NaN in the part that only the scores read:
+        // the rows that see them become NaN, as they have to, and no others.  Done by the wavefront that brought the slots.
+        if (!PREFIX && all_see < sees && j0 + SUB * 32 > all_see) {
+            const uint32_t at = lds_at + buf * STEP + sub * T::kBytes;
+            for (int i = 0; i < 8; ++i) {
+                const int slot = quarter * 8 + i;
+                const uint32_t to = at + (lane >> 3) * 4096 + slot * 128 + ((lane & 7) ^ twist(slot)) * 16;
+                bool bad = false;
+                if (lane * 8 < DC) {
+                    const u32x4 x = read_lds(to);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) z[i] = 0.f;
-#pragma unroll
-        for (int f = 0; f < STEPS; ++f) z = mfma32(read_lds(at + key_at[f & 3] + (f >> 2) * 4096), af[f], z);
-        if (j0 + 32 > wave_least || j0 + 32 > end) {
-            const int within = min(limit, end) - j0 - 4 * grp;
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (row_of(i, 0) >= within) z[i] = -__builtin_inff();
+                    for (int e = 0; e < 4; ++e) bad |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
+                }
+                if (__any(bad)) {
+                    if (lane * 8 < DC) write_lds(to, u32x4{0u, 0u, 0u, 0u});
+                    if (lane == 0)
+                        write_lds(at + (DC / 64) * 4096 + slot * 128 + twist(slot) * 16, u32x4{0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu});
+                }
+            }
+            __syncthreads();
         }
-        float top = z[0];
+        f32x4 z[SUB], y[SUB];  // two chains of products a tile, which do not wait for one another
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, z[i]);
+        for (int u = 0; u < SUB; ++u) {
+            z[u] = y[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int f = 0; f < KEYS; ++f) {
+                const u32x4 k = read_lds(key_at[f & 1] + buf * STEP + u * T::kBytes + (f >> 1) * 4096);
+                z[u] = mfma16(k, hi[f], z[u]);
+                if (f < LOW) y[u] = mfma16(k, lo[f], y[u]);
+            }
+        }
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            z[u] += y[u];
+            const int within = limit - j0 - u * 32 - half * 16 - 4 * g16;
+            if (j0 + SUB * 32 > all_see || j0 + SUB * 32 > end) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i >= within) z[u][i] = -__builtin_inff();
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, z[u][i]);
+        }
         top *= run.qscale;
         if (__any(top > ref + kRise)) {
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
             top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float now = top > ref + kRise ? reference_of(top) : ref;
-            const float f = __builtin_amdgcn_exp2f(ref - now);
+            const float now = top > ref + kRise ? ceilf(top) : ref;
+            sum *= __builtin_amdgcn_exp2f(ref - now);
             ref = now;
-            sum *= f;
-#pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) {
-                pin(b);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[b][i] *= f;
-                pin(b);
-            }
         }
         exponents(ref, kAbove, run.qscale, [&](auto&& of) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] = of(z[i]);
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[u][i] = of(z[u][i]);
         });
-        u32x4 w[2];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            float p[8];
+        for (int u = 0; u < SUB; ++u) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                p[i] = __builtin_amdgcn_exp2f(z[t * 8 + i]);
-                sum += p[i];
+            for (int i = 0; i < 4; ++i) {
+                z[u][i] = __builtin_amdgcn_exp2f(z[u][i]);
+                sum += z[u][i];
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[t][i] = pack_bf16(p[2 * i], p[2 * i + 1]);
+            write_lds2(put_at + u * M * 64, u32x2{pack_bf16(z[u][0], z[u][1]), pack_bf16(z[u][2], z[u][3])});
         }
+        if (g16 == 0) sm_ref[half][my_row] = ref;
+        __syncthreads();
+        float ref0[ROW_TILES], ref1[ROW_TILES];
+        bool moved = false;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int r = 0; r < ROW_TILES; ++r) {
+            ref0[r] = sm_ref[0][(tile32 + r) * 32 + col];
+            ref1[r] = sm_ref[1][(tile32 + r) * 32 + col];
+            moved |= ref0[r] != sums_ref[r] || ref1[r] != sums_ref[r];
+        }
+        const float other = sm_ref[half ^ 1][my_row];
+        if (other > ref) {
+            sum *= __builtin_amdgcn_exp2f(ref - other);
+            ref = other;
+        }
+        const bool any_moved = __any(moved);
+        if (any_moved) {
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) {
-                const uint32_t v = at + (b >> 1) * 4096 + t * 2048;
-                acc[b] = mfma32(join(read_transposed(v + value_at[b & 1][0]), read_transposed(v + value_at[b & 1][1])), w[t], acc[b]);
-            }
-    };
-    // A latent that is not finite, in a slot that some row of the workgroup does not see, would reach that row as 0 times it.
-    // In tiles where that can be, such slots give up their latents and get NaN in the part that only the scores read:
-    // the rows that see them become NaN, as they have to, and no others.  Done by the wavefront that brought the slots.
-    const int all_see = PREFIX ? c.prefix_len : q.cached + row0 / run.H + 1;
-    auto mend = [&](uint32_t at) {
-        for (int i = 0; i < KW * 8; ++i) {
-            const int slot = mw * KW * 8 + i;
-            const uint32_t to = at + (lane >> 3) * 4096 + slot * 128 + ((lane & 7) ^ twist(slot)) * 16;
-            bool bad = false;
-            if (lane * 8 < DC) {
-                const u32x4 x = read_lds(to);
+            for (int r = 0; r < ROW_TILES; ++r) {
+                const float now = fmaxf(ref0[r], ref1[r]), f = __builtin_amdgcn_exp2f(sums_ref[r] - now);
+                sums_ref[r] = now;
+                ref0[r] = __builtin_amdgcn_exp2f(ref0[r] - now);  // from here on factors of the halves' weights
+                ref1[r] = __builtin_amdgcn_exp2f(ref1[r] - now);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) bad |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
-            }
-            if (__any(bad)) {
-                if (lane * 8 < DC) write_lds(to, u32x4{0u, 0u, 0u, 0u});
-                if (lane == 0)
-                    write_lds(at + (DC / 64) * 4096 + slot * 128 + twist(slot) * 16, u32x4{0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu});
+                for (int b = 0; b < COLS; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[b][r][i] *= f;
             }
         }
-    };
-
-    const int tiles = (end - first + 31) / 32;
-    if constexpr (MW == 1) {
-        for (int t = team; t < tiles; t += KW) {
-            const int j0 = first + t * 32;
-            copy(0, j0);
-            wait_copies<0>();
-            if (!PREFIX && all_see < sees && j0 + 32 > all_see) mend(ring_at);
-            compute(ring_at, j0);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile has been read
-        }
-    } else {
-        const int steps = (tiles + KW - 1) / KW;  // the same for both teams, which wait for one another
-        auto slot_at = [&](int step) { return first + min(step * KW + team, tiles - 1) * 32; };
 #pragma unroll
-        for (int i = 0; i < MW - 1; ++i)
-            if (i < steps) copy(i, slot_at(i));
-        int buf = 0;
-        for (int t = 0; t < steps; ++t) {
-            if (t + MW - 2 < steps) wait_copies<(MW - 2) * COPIES>();  // all but the youngest MW - 2 tiles
-            else wait_copies<0>();
-            __syncthreads();  // the tile is there, and nobody reads the one before it any more
-            if (t + MW - 1 < steps) copy(buf == 0 ? MW - 1 : buf - 1, slot_at(t + MW - 1));
-            // Every wavefront takes every tile, though some see nothing of it: a branch around the products would have the sums
-            // copied between registers.  A team's tile past the last one is the last one again, and its slots count as hidden.
-            if (!PREFIX && all_see < sees && first + (t + 1) * KW * 32 > all_see) {  // the same for both teams
-                mend(ring_at + buf * T::kBytes);
-                __syncthreads();
-            }
-            compute(ring_at + buf * T::kBytes, first + (t * KW + team) * 32);
-            buf = buf == MW - 1 ? 0 : buf + 1;
-        }
-    }
-    sum += __shfl_xor(sum, 32, 64);
-
-    const int64_t item = (row_head + r) * run.parts.all + run.part0 + range;
-    float* to = run.parts.acc + item * DC;
-    if constexpr (KW == 1) {
-        if (r < rows) {
+        for (int u = 0; u < SUB; ++u)
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b)
+            for (int h = 0; h < 2; ++h) {
+                u32x4 w[ROW_TILES];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    *(f32x4*)(to + b * 32 + row_of(4 * i, grp)) = f32x4{acc[b][4 * i], acc[b][4 * i + 1], acc[b][4 * i + 2], acc[b][4 * i + 3]};
-            if (grp == 0) run.parts.ml[item] = make_float2(ref, sum);
-        }
-    } else {
-        // the teams' sums meet in LDS, AT_ONCE blocks at a time, each team adding its share of them
-        if (grp == 0) sm_ml[wave][col] = make_float2(ref, sum);
-        __syncthreads();  // the tiles are done with, too
-        float most = kEmpty, all = 0.f;
+                for (int r = 0; r < ROW_TILES; ++r) {
+                    w[r] = read_lds(get_at + u * M * 64 + r * 2048 + ((h * 2 + grp) ^ get_xor) * 16);
+                    if (any_moved) {
+                        const float f = h == 0 ? ref0[r] : ref1[r];
 #pragma unroll
-        for (int k = 0; k < KW; ++k) most = fmaxf(most, sm_ml[k * MW + mw][col].x);
+                        for (int i = 0; i < 4; ++i) w[r][i] = pack_bf16(bf_lo(w[r][i]) * f, bf_hi(w[r][i]) * f);
+                    }
+                }
 #pragma unroll
-        for (int k = 0; k < KW; ++k) {
-            const float2 ml = sm_ml[k * MW + mw][col];
-            all = __builtin_fmaf(ml.y, __builtin_amdgcn_exp2f(ml.x - most), all);
-        }
-        const float f = __builtin_amdgcn_exp2f(ref - most);
-        constexpr int SHARE = AT_ONCE / KW;
-        f32x4* sums = (f32x4*)lds;
+                for (int b = 0; b < COLS; ++b) {
+                    // block0 is even wherever there is more than one block
+                    const int odd = COLS > 1 ? b & 1 : block0 & 1;
+                    const uint32_t at = buf * STEP + u * T::kBytes + ((block0 + b) >> 1) * 4096 + h * 2048;
+                    const u32x4 v = join(read_transposed((odd ? value_at[1][0] : value_at[0][0]) + at), read_transposed((odd ? value_at[1][1] : value_at[0][1]) + at));
 #pragma unroll
-        for (int b0 = 0; b0 < BLOCKS; b0 += AT_ONCE) {
-            if (b0 > 0) __syncthreads();
-#pragma unroll
-            for (int b = 0; b < AT_ONCE; ++b)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    sums[((wave * AT_ONCE + b) * 4 + i) * 64 + lane] =
-                        f32x4{acc[b0 + b][4 * i] * f, acc[b0 + b][4 * i + 1] * f, acc[b0 + b][4 * i + 2] * f, acc[b0 + b][4 * i + 3] * f};
-            __syncthreads();
-#pragma unroll
-            for (int b = 0; b < SHARE; ++b) {
-                const int block = team * SHARE + b;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    f32x4 x = sums[((mw * AT_ONCE + block) * 4 + i) * 64 + lane];
-#pragma unroll
-                    for (int k = 1; k < KW; ++k) x += sums[(((k * MW + mw) * AT_ONCE + block) * 4 + i) * 64 + lane];
-                    if (r < rows) *(f32x4*)(to + (b0 + block) * 32 + row_of(4 * i, grp)) = x;
+                    for (int r = 0; r < ROW_TILES; ++r) acc[b][r] = mfma32(v, w[r], acc[b][r]);
                 }
             }
-        }
-        if (r < rows && team == 0 && grp == 0) run.parts.ml[item] = make_float2(most, all);
     }
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if (g16 == 0) sm_sum[half][my_row] = sum;
+    __syncthreads();  // the tiles are done with, too
+
+    // The sums go through LDS, so that a row leaves in one piece; its 16-byte units lie at an xor of the row.
+    constexpr int UNITS = DC / 4;
+#pragma unroll
+    for (int b = 0; b < COLS; ++b)
+#pragma unroll
+        for (int r = 0; r < ROW_TILES; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = (tile32 + r) * 32 + col, unit = (block0 + b) * 8 + 2 * i + grp;
+                ((f32x4*)lds)[row * UNITS + (unit ^ (row & 31))] = f32x4{acc[b][r][4 * i], acc[b][r][4 * i + 1], acc[b][r][4 * i + 2], acc[b][r][4 * i + 3]};
+            }
+    __syncthreads();
+    const int64_t item = row_head * run.parts.all + run.part0 + range;
+    for (int i = threadIdx.x; i < M * UNITS; i += WAVES * 64) {
+        const int row = i / UNITS, unit = i % UNITS;
+        if (row0 + row < rows) ((f32x4*)(run.parts.acc + (item + (int64_t)row * run.parts.all) * DC))[unit] = ((const f32x4*)lds)[row * UNITS + (unit ^ (row & 31))];
+    }
+    if (threadIdx.x < M && row0 + (int)threadIdx.x < rows)
+        run.parts.ml[item + (int64_t)threadIdx.x * run.parts.all] = make_float2(fmaxf(sm_ref[0][threadIdx.x], sm_ref[1][threadIdx.x]), sm_sum[0][threadIdx.x] + sm_sum[1][threadIdx.x]);
 }
 
 int64_t up256(int64_t v) { return (v + 255) & ~(int64_t)255; }
 
-// Wavefronts side by side over `rows` rows.
-int wide(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
+// Tiles of 32 rows of a workgroup that has `rows` of them to share.
+int wide(int64_t rows) { return rows <= 32 ? 1 : 2; }
 
 // Ranges of `most` slots for `groups` workgroups each.
 void split(int64_t most, int64_t groups, int* per, int* ranges) {
@@ -303,7 +306,7 @@ void split(int64_t most, int64_t groups, int* per, int* ranges) {
 
 // How a step is run, from its sizes and bounds.
 struct Plan {
-    int own_mw, own_tiles, pre_mw, pre_tiles;  // wavefronts side by side, row tiles: of a sequence, of all rows over the prefix
+    int own_mt, own_tiles, pre_mt, pre_tiles;  // 32-row tiles of a workgroup, workgroups' tiles: of a sequence, of all rows over the prefix
     int own_ranges, pre_ranges;
     Parts parts;
     int64_t own_groups, pre_groups;
@@ -317,15 +320,15 @@ Plan plan(const Cache& c, const Step& s, const Heads& h) {
     if (s.n_rows == 0) return p;
     const int64_t most = min((int64_t)s.max_cached + s.max_new, (int64_t)c.max_len);
     const int64_t rows = (int64_t)s.max_new * h.n, all = (int64_t)s.n_rows * h.n;
-    p.own_mw = wide(rows);
-    p.own_tiles = (int)((rows + p.own_mw * 32 - 1) / (p.own_mw * 32));
+    p.own_mt = wide(rows);
+    p.own_tiles = (int)((rows + p.own_mt * 32 - 1) / (p.own_mt * 32));
     split(most, (int64_t)c.n_seq * p.own_tiles, &p.parts.per, &p.own_ranges);
     p.own_groups = (int64_t)c.n_seq * p.own_tiles * p.own_ranges;
     p.parts.own = p.parts.all = p.own_ranges;
     p.parts.pre_per = 1;
     if (c.prefix_len > 0) {
-        p.pre_mw = wide(all);
-        p.pre_tiles = (int)((all + p.pre_mw * 32 - 1) / (p.pre_mw * 32));
+        p.pre_mt = wide(all);
+        p.pre_tiles = (int)((all + p.pre_mt * 32 - 1) / (p.pre_mt * 32));
         split(c.prefix_len, p.pre_tiles, &p.parts.pre_per, &p.pre_ranges);
         p.pre_groups = (int64_t)p.pre_tiles * p.pre_ranges;
         p.parts.all += p.pre_ranges;
@@ -335,17 +338,16 @@ Plan plan(const Cache& c, const Step& s, const Heads& h) {
     p.o_ml = o;
     o += up256(items * 8);
     p.o_a = o;
-    o += up256(all * (c.latent + c.rope) * 2);
+    o += up256(all * (2 * c.latent + c.rope) * 2);
     p.bytes = o;
     return p;
 }
 
 template <int DC, int DR, bool PREFIX>
-void launch_run(hipStream_t st, const Cache& c, const Step& s, const Run& run, int mw, int64_t groups) {
-    const dim3 grid((unsigned)groups), block(256);
-    if (mw == 1) hipLaunchKernelGGL((absorbed_kernel<DC, DR, 1, PREFIX>), grid, block, 0, st, c, s, run);
-    if (mw == 2) hipLaunchKernelGGL((absorbed_kernel<DC, DR, 2, PREFIX>), grid, block, 0, st, c, s, run);
-    if (mw == 4) hipLaunchKernelGGL((absorbed_kernel<DC, DR, 4, PREFIX>), grid, block, 0, st, c, s, run);
+void launch_run(hipStream_t st, const Cache& c, const Step& s, const Run& run, int mt, int64_t groups) {
+    const dim3 grid((unsigned)groups);
+    if (mt == 1) hipLaunchKernelGGL((absorbed_kernel<DC, DR, 1, PREFIX>), grid, dim3(256), 0, st, c, s, run);
+    if (mt == 2) hipLaunchKernelGGL((absorbed_kernel<DC, DR, 2, PREFIX>), grid, dim3(512), 0, st, c, s, run);
 }
 
 template <int DC, int DR>
@@ -355,13 +357,13 @@ void launch_sizes(hipStream_t st, const Cache& c, const Step& s, const Plan& p, 
         run.per = p.parts.pre_per;
         run.ranges = p.pre_ranges;
         run.part0 = p.parts.own;
-        launch_run<DC, DR, true>(st, c, s, run, p.pre_mw, p.pre_groups);
+        launch_run<DC, DR, true>(st, c, s, run, p.pre_mt, p.pre_groups);
     }
     run.row_tiles = p.own_tiles;
     run.per = p.parts.per;
     run.ranges = p.own_ranges;
     run.part0 = 0;
-    launch_run<DC, DR, false>(st, c, s, run, p.own_mw, p.own_groups);
+    launch_run<DC, DR, false>(st, c, s, run, p.own_mt, p.own_groups);
 }
 
 }  // namespace

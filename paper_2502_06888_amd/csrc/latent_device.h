@@ -12,6 +12,7 @@ __device__ __forceinline__ uint32_t lds_address(T* p) {
 }
 __device__ __forceinline__ u32x4 read_lds(uint32_t at) { return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)at; }
 __device__ __forceinline__ void write_lds(uint32_t at, const u32x4 v) { *(__attribute__((address_space(3))) u32x4*)(uintptr_t)at = v; }
+__device__ __forceinline__ void write_lds2(uint32_t at, const u32x2 v) { *(__attribute__((address_space(3))) u32x2*)(uintptr_t)at = v; }
 // Four rows of 16 elements of 16 bits, transposed: lane l of 16 points at four elements of row l / 4, 4 * (l % 4) on, and gets element l
 // of the four rows.
 __device__ __forceinline__ u32x2 read_transposed(uint32_t at) {
