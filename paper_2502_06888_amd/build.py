@@ -12,7 +12,8 @@ LIB = os.path.join(HERE, "libklotski_moe.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["moe_api.hip", "k_router.hip", "k_plan.hip", "k_misc.hip", "k_ffn_f32.hip",
            "k_ffn_bf16.hip", "attn_api.hip", "k_attn.hip", "kv8_api.hip", "k_kv8.hip", "k_kv8_attn.hip",
-           "rope_api.hip", "k_rope.hip", "latent_api.hip", "k_latent.hip", "k_latent_attn.hip"]
+           "rope_api.hip", "k_rope.hip", "latent_api.hip", "k_latent.hip", "k_latent_attn.hip",
+           "k_latent_expand.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

@@ -16,7 +16,6 @@ struct Tile {
     static constexpr int kWidth = DC + DR, kGroups = (kWidth + 63) / 64, kBytes = kGroups * 4096;
     static constexpr bool kHalf = kWidth % 64 != 0;
 };
-__device__ __forceinline__ int twist(int slot) { return (slot >> 1 & 1) << 2 | (slot >> 2 & 3); }
 
 struct Run {  // one launch
     int H, row_tiles;  // tiles of 32 * MT rows of a sequence (of the prefix: of all)
@@ -198,12 +197,11 @@ __global__ __launch_bounds__(256 * MT, 2) void absorbed_kernel(Cache c, Step s, 
         });
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                z[u][i] = __builtin_amdgcn_exp2f(z[u][i]);
-                sum += z[u][i];
-            }
-            write_lds2(put_at + u * M * 64, u32x2{pack_bf16(z[u][0], z[u][1]), pack_bf16(z[u][2], z[u][3])});
+            u32x2 w;  // the sum is that of the weights as rounded: then one slot that has nearly all of it counts nearly exactly
+            w.x = pack_bf16(__builtin_amdgcn_exp2f(z[u][0]), __builtin_amdgcn_exp2f(z[u][1]));
+            w.y = pack_bf16(__builtin_amdgcn_exp2f(z[u][2]), __builtin_amdgcn_exp2f(z[u][3]));
+            sum += (bf_lo(w.x) + bf_hi(w.x)) + (bf_lo(w.y) + bf_hi(w.y));
+            write_lds2(put_at + u * M * 64, w);
         }
         if (g16 == 0) sm_ref[half][my_row] = ref;
         __syncthreads();
@@ -302,8 +300,6 @@ void split(int64_t most, int64_t groups, int* per, int* ranges) {
     *ranges = (int)(most > p ? (most + p - 1) / p : 1);
 }
 
-}  // namespace
-
 // How a step is run, from its sizes and bounds.
 struct Plan {
     int own_mt, own_tiles, pre_mt, pre_tiles;  // 32-row tiles of a workgroup, workgroups' tiles: of a sequence, of all rows over the prefix
@@ -312,8 +308,6 @@ struct Plan {
     int64_t own_groups, pre_groups;
     int64_t o_ml, o_a, bytes;
 };
-
-namespace {
 
 Plan plan(const Cache& c, const Step& s, const Heads& h) {
     Plan p{};
@@ -368,17 +362,15 @@ void launch_sizes(hipStream_t st, const Cache& c, const Step& s, const Plan& p, 
 
 }  // namespace
 
-int choose_form(const Cache&, const Step&, const Heads&, int) { return MOE_LATENT_ABSORBED; }
-
-bool attend_fits(const Cache& c, const Step& s, const Heads& h, int) {
+bool absorbed_fits(const Cache& c, const Step& s, const Heads& h) {
     const Plan p = plan(c, s, h);
     return p.own_groups <= kMostGroups && p.pre_groups <= kMostGroups && absorb_groups(c, h, s.n_rows) <= kMostGroups &&
            finish_groups(h, s.n_rows) <= kMostGroups;
 }
 
-int64_t attend_workspace(const Cache& c, const Step& s, const Heads& h, int) { return plan(c, s, h).bytes; }
+int64_t absorbed_workspace(const Cache& c, const Step& s, const Heads& h) { return plan(c, s, h).bytes; }
 
-void launch_attend(hipStream_t st, const Cache& c, const Step& s, const Heads& h, const Attend& a, int) {
+void launch_absorbed(hipStream_t st, const Cache& c, const Step& s, const Heads& h, const Attend& a) {
     Plan p = plan(c, s, h);
     p.parts.acc = (float*)a.ws;
     p.parts.ml = (float2*)(a.ws + p.o_ml);

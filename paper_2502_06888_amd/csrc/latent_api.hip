@@ -89,6 +89,15 @@ Heads heads_of(const moe_latent_cache* c, const moe_latent_heads* h) {
                  h->w_k_head ? h->w_k_head : (int64_t)h->nope_dim * c->latent_dim, h->w_v_head ? h->w_v_head : (int64_t)h->v_dim * c->latent_dim};
 }
 
+// Whether a step is better run expanded: by operations, with what a slot or a row costs on the way.
+bool expands(const Cache& c, const Step& s, const Heads& h, int form) {
+    if (form != MOE_LATENT_AUTO) return form == MOE_LATENT_EXPANDED;
+    return s.max_new > 128;
+}
+
+bool fits(const Cache& c, const Step& s, const Heads& h, bool expanded) { return expanded ? expanded_fits(c, s, h) : absorbed_fits(c, s, h); }
+int64_t workspace_of(const Cache& c, const Step& s, const Heads& h, bool expanded) { return expanded ? expanded_workspace(c, s, h) : absorbed_workspace(c, s, h); }
+
 moe_status launched() {
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? MOE_OK : fail(MOE_ERR_HIP, "launch failed: %s", hipGetErrorString(e));
@@ -142,9 +151,9 @@ moe_status moe_latent_attend_workspace_bytes(const moe_latent_cache* cache, cons
     const Cache c = cache_of(cache);
     const Step s = step_of(step);
     const Heads h = heads_of(cache, heads);
-    const int how = choose_form(c, s, h, form);
-    if (!attend_fits(c, s, h, how)) return fail(MOE_ERR_SHAPE, "too many workgroups: bring fewer sequences or tokens at once");
-    *bytes_out = attend_workspace(c, s, h, how);
+    const bool expanded = expands(c, s, h, form);
+    if (!fits(c, s, h, expanded)) return fail(MOE_ERR_SHAPE, "too many workgroups: bring fewer sequences or tokens at once");
+    *bytes_out = workspace_of(c, s, h, expanded);
     return MOE_OK;
 }
 
@@ -170,9 +179,9 @@ moe_status moe_latent_attend(void* stream, const moe_latent_cache* cache, const 
     TRY(check_rows(out, "out", out_row_stride, out_head_stride, &w));
     if (pieces_overlap(s.n_rows, h.n, out_row_stride, out_head_stride, h.v)) return fail(MOE_ERR_INVALID_ARG, "rows or heads of out overlap");
     if (q == out) return fail(MOE_ERR_INVALID_ARG, "out must not be q");
-    const int how = choose_form(c, s, h, form);
-    if (!attend_fits(c, s, h, how)) return fail(MOE_ERR_SHAPE, "too many workgroups: bring fewer sequences or tokens at once");
-    const int64_t need = attend_workspace(c, s, h, how);
+    const bool expanded = expands(c, s, h, form);
+    if (!fits(c, s, h, expanded)) return fail(MOE_ERR_SHAPE, "too many workgroups: bring fewer sequences or tokens at once");
+    const int64_t need = workspace_of(c, s, h, expanded);
     if (workspace_bytes < need) return fail(MOE_ERR_OOM, "workspace of %lld bytes, need %lld", (long long)workspace_bytes, (long long)need);
     TRY(w.on(workspace, "workspace", 256));
     OnDevice on(w.device);
@@ -182,7 +191,8 @@ moe_status moe_latent_attend(void* stream, const moe_latent_cache* cache, const 
     a.q = Rows{(const uint16_t*)q, q_row_stride, q_head_stride};
     a.out = RowsOut{(uint16_t*)out, out_row_stride, out_head_stride};
     a.ws = (uint8_t*)workspace;
-    launch_attend((hipStream_t)stream, c, s, h, a, how);
+    if (expanded) launch_expanded((hipStream_t)stream, c, s, h, a);
+    else launch_absorbed((hipStream_t)stream, c, s, h, a);
     return launched();
 }
 

@@ -20,11 +20,15 @@ __device__ __forceinline__ u32x2 read_transposed(uint32_t at) {
 }
 __device__ __forceinline__ u32x4 join(const u32x2 a, const u32x2 b) { return u32x4{a.x, a.y, b.x, b.y}; }
 
-// Sums of the absorbed form, cut into parts: a row's slots into ranges of `per`, the prefix into ranges of its own, behind them.
+// Where the eight 16-byte units of a slot's 128 bytes lie in LDS: unit u at place u ^ twist(slot).  Slots side by side then differ in
+// their bank for reads of one unit each, and for transposed ones of four units each.
+__device__ __forceinline__ int twist(int slot) { return (slot >> 1 & 1) << 2 | (slot >> 2 & 3); }
+
+// Sums, cut into parts: a row's slots into ranges of `per`, the prefix into ranges of its own, behind them.
 struct Parts {
     int per, pre_per;  // slots of a range: of a sequence, of the prefix
     int own, all;      // parts of a row at most: of its sequence, with the prefix's
-    float* acc;        // [row, head, part, latent] sums of weight * latent
+    float* acc;        // [row, head, part, element] sums of weight * latent, or * value
     float2* ml;        // [row, head, part] reference, sum of weights
 };
 

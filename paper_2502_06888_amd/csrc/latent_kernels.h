@@ -49,12 +49,13 @@ using kkv8::kMostGroups;
 
 void launch_append(hipStream_t st, const Cache& c, const Step& s, const Append& a);
 
-// Which form a step takes, what it needs, whether its launches stay within kMostGroups.
-struct Plan;
-int choose_form(const Cache& c, const Step& s, const Heads& h, int asked);
-bool attend_fits(const Cache& c, const Step& s, const Heads& h, int form);
-int64_t attend_workspace(const Cache& c, const Step& s, const Heads& h, int form);
-void launch_attend(hipStream_t st, const Cache& c, const Step& s, const Heads& h, const Attend& a, int form);
+// The two forms: whether their launches stay within kMostGroups, what they need.
+bool absorbed_fits(const Cache& c, const Step& s, const Heads& h);
+int64_t absorbed_workspace(const Cache& c, const Step& s, const Heads& h);
+void launch_absorbed(hipStream_t st, const Cache& c, const Step& s, const Heads& h, const Attend& a);
+bool expanded_fits(const Cache& c, const Step& s, const Heads& h);
+int64_t expanded_workspace(const Cache& c, const Step& s, const Heads& h);
+void launch_expanded(hipStream_t st, const Cache& c, const Step& s, const Heads& h, const Attend& a);
 
 // Sequence whose rows include `row` (the same for the whole wavefront), and the token's place in it; -1 where there is none.
 // The wavefront looks at 64 offsets at a time: two reads one behind the other for up to 4096 sequences, where halving takes twelve.
