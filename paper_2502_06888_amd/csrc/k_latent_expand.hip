@@ -37,6 +37,7 @@ struct Made {
     u32x4* kv;                // [sequence, head, tile]: keys, then values, in the order of the matrix instructions
     u32x4* pe;                // [sequence, tile]: the part that carries the position
     int2* shift;              // [sequence, head, tile] exponents taken off the keys and the values
+    const u32x4* w;           // w_k and w_v of all heads, see order_kernel
     int per, ranges, row_tiles, part0;
 };
 
@@ -55,18 +56,39 @@ __device__ __forceinline__ int slots_of(const Cache& c, const Step& s, int seq) 
     return q.n_new > 0 ? q.cached + q.n_new : 0;
 }
 
-// Keys and values of 128 slots for some heads, one after the other: the latents lie in LDS (up to 128 KiB) for all of them, rows
-// of w_k and w_v come from L2 into registers, one step of 64 latents ahead.  A wavefront makes 32 elements of the keys (w_k c^T: a lane has one
+// w_k and w_v in the order in which expand_kernel's matrix instructions take them: [head][32 rows][16 latents][lane], 16 bytes a lane.  Read
+// where they lie, a wavefront's rows are 32 lines of which it uses 32 bytes at a time: expand_kernel then waits for L2 (8192 slots of 32
+// heads 120 us, with this copy and its 4 us LATER).  One workgroup per 32 rows.
+__global__ __launch_bounds__(256) void order_kernel(Heads h, int latent, u32x4* out) {
+    const int lane = threadIdx.x & 63, blocks = (h.nope + h.v) / 32, head = blockIdx.x / blocks, block = blockIdx.x % blocks;
+    const bool key = block < h.nope / 32;
+    const int row = (key ? block : block - h.nope / 32) * 32 + (lane & 31);
+    const uint16_t* from = (key ? h.w_k + head * h.w_k_head : h.w_v + head * h.w_v_head) + (int64_t)row * latent + (lane >> 5) * 8;
+    u32x4* to = out + (int64_t)blockIdx.x * (latent / 16) * 64 + lane;
+    for (int f = wave_number() * 4; f < latent / 16; f += 16) {
+        u32x4 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = *(const u32x4*)(from + (f + i) * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[(f + i) * 64] = x[i];
+    }
+}
+
+// Keys and values of 128 slots for some heads, one after the other: the latents lie in LDS (up to 128 KiB) for all of them, w_k
+// and w_v come from L2 into registers, 64 latents ahead.  A wavefront makes 32 elements of the keys (w_k c^T: a lane has one
 // slot and four elements side by side) and 32 of the values (c w_v^T: one element and eight slots, in the order in which the weights of the
 // softmax come out of the scores), which is how the attention's matrix instructions take them.
-// The contraction runs over 64 latents at a time with lane half g taking the g-th 64 bytes, so that lines are read whole.
+constexpr int expand_waves(int nope, int v) { return (nope > v ? nope : v) / 32; }  // of 64 slots
+// Wavefronts of a SIMD: as many workgroups as the LDS holds.
+constexpr int expand_occupancy(int latent, int waves) { return waves * 2 * (latent == 512 ? 1 : latent == 256 ? 2 : 4) >= 8 ? 2 : 1; }
 template <int DC, int NOPE, int DV, bool PREFIX>
-__global__ __launch_bounds__(256, 1) void expand_kernel(Cache c, Step s, Heads h, Made m, int each) {
-    constexpr int G = DC / 64, KEYS = NOPE / 32, VALUES = DV / 32, TILE = kSlots * (NOPE + DV) / 8;
+__global__ __launch_bounds__(128 * expand_waves(NOPE, DV), expand_occupancy(DC, expand_waves(NOPE, DV))) void expand_kernel(Cache c, Step s, Heads h, Made m, int each) {
+    constexpr int G = DC / 64, KEYS = NOPE / 32, VALUES = DV / 32, WAVES = expand_waves(NOPE, DV), TILE = kSlots * (NOPE + DV) / 8;
     __shared__ u32x4 lds[G * 128 * 8];
+    __shared__ uint32_t seen[2][2][WAVES];  // [odd and even heads][tile of 64][wavefront]
     __shared__ uint32_t largest[2][2];  // [keys, values][tile of 64]
     __shared__ int bad[128];
-    const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, grp = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = wave_number() % WAVES, half = wave_number() / WAVES, col = lane & 31, grp = lane >> 5;
     const int pairs_of = (m.tiles + 1) / 2;
     const int pair = blockIdx.x % pairs_of, rest = blockIdx.x / pairs_of;
     const int seq = PREFIX ? 0 : rest % c.n_seq, first = (PREFIX ? rest : rest / c.n_seq) * each;
@@ -77,7 +99,7 @@ __global__ __launch_bounds__(256, 1) void expand_kernel(Cache c, Step s, Heads h
     {
         const uint32_t at = lds_address(lds);
         const int in8 = lane >> 3;
-        for (int i = wave; i < 16; i += 4) {
+        for (int i = wave_number(); i < 16; i += 2 * WAVES) {
             const int slot = i * 8 + in8;
             const uint32_t from = (uint32_t)min(j0 + slot, total - 1) * (uint32_t)(width * 2) + ((lane & 7) ^ twist(slot)) * 16;
 #pragma unroll
@@ -86,7 +108,7 @@ __global__ __launch_bounds__(256, 1) void expand_kernel(Cache c, Step s, Heads h
     }
     if (first == 0) {  // the part that carries the position, once
         const int units = c.rope / 8;
-        for (int i = threadIdx.x; i < 128 * units; i += 256) {
+        for (int i = threadIdx.x; i < 128 * units; i += 128 * WAVES) {
             const int l = i & 63, unit = i >> 6;  // [tile][32 slots][16 elements][lane]
             const int f = unit % (units / 2), slot = unit / (units / 2) * 32 + (l & 31);
             if (j0 + slot / 64 * 64 < total) {
@@ -97,28 +119,27 @@ __global__ __launch_bounds__(256, 1) void expand_kernel(Cache c, Step s, Heads h
     }
     const bool keys = wave < KEYS, values = wave < VALUES;
     // past the last head the last one is asked for again, and not used
-    const auto row_k = [&](int head) { return h.w_k + (int64_t)(m.head0 + min(head, m.heads - 1)) * h.w_k_head + (int64_t)((keys ? wave : 0) * 32 + col) * DC + grp * 32; };
-    const auto row_v = [&](int head) { return h.w_v + (int64_t)(m.head0 + min(head, m.heads - 1)) * h.w_v_head + (int64_t)((values ? wave : 0) * 32 + col) * DC + grp * 32; };
+    constexpr int BLOCK = DC / 16 * 64;
+    const auto from = [&](int head) { return m.w + (int64_t)(m.head0 + min(head, m.heads - 1)) * (KEYS + VALUES) * BLOCK + lane; };
+    const int block_k = (keys ? wave : 0) * BLOCK, block_v = (KEYS + (values ? wave : 0)) * BLOCK;
     u32x4 wk[4], wv[4];
-    auto load = [&](const uint16_t* pk, const uint16_t* pv) {
+    auto load = [&](const u32x4* p, int g) {
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
-            wk[f] = *(const u32x4*)(pk + f * 8);
-            wv[f] = *(const u32x4*)(pv + f * 8);
+            wk[f] = p[block_k + (g * 4 + f) * 64];
+            wv[f] = p[block_v + (g * 4 + f) * 64];
         }
     };
-    load(row_k(first), row_v(first));
-    uint32_t at[4];  // unit 4 * grp + f of the lane's slot
+    load(from(first), 0);
+    uint32_t at[4];  // unit 2 * f + grp of the lane's slot
 #pragma unroll
-    for (int f = 0; f < 4; ++f) at[f] = lds_address(lds) + (uint32_t)(col * 128 + ((4 * grp + f) ^ twist(col)) * 16);
+    for (int f = 0; f < 4; ++f) at[f] = lds_address(lds) + (uint32_t)((half * 64 + col) * 128 + ((2 * f + grp) ^ twist(col)) * 16);
     wait_copies<0>();
     __syncthreads();
     for (int head = first; head < min(first + each, m.heads); ++head) {
-        if (threadIdx.x < 4) largest[threadIdx.x >> 1][threadIdx.x & 1] = 0;
-        if (threadIdx.x < 128) bad[threadIdx.x] = 0;
-        f32x16 k[4], v[4];
+        f32x16 k[2], v[2];
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) k[t][i] = v[t][i] = 0.f;
 #pragma unroll
@@ -129,73 +150,91 @@ __global__ __launch_bounds__(256, 1) void expand_kernel(Cache c, Step s, Heads h
                 a[f] = wk[f];
                 b[f] = wv[f];
             }
-            if (g + 1 < G) load(row_k(head) + (g + 1) * 64, row_v(head) + (g + 1) * 64);
-            else load(row_k(head + 1), row_v(head + 1));
+            if (g + 1 < G) load(from(head), g + 1);
+            else load(from(head + 1), 0);
 #pragma unroll
             for (int f = 0; f < 4; ++f)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
+                for (int t = 0; t < 2; ++t) {
                     const u32x4 x = read_lds(at[f] + g * 16384 + t * 4096);
                     k[t] = mfma32(a[f], x, k[t]);
                     v[t] = mfma32(x, b[f], v[t]);
                 }
         }
-        __syncthreads();
-        // the largest of each tile, and the slots with something that is not finite
-        uint32_t top[2][2] = {{0, 0}, {0, 0}};
+        // Whether every tile is within the range of fp16 as it is: nothing from 2^15 on (infinities and NaN among that), something from 2^-6 on.
+        uint32_t a = 0, b = 0;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            bool odd = false;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const uint32_t x = __float_as_uint(k[t][i]) & 0x7fffffffu, y = __float_as_uint(v[t][i]) & 0x7fffffffu;
-                if (x >= 0x7f800000u) odd = true;
-                else top[0][t >> 1] = max(top[0][t >> 1], x);
-                if (y >= 0x7f800000u) {
-                    if (values) bad[t * 32 + row_of(i, grp)] = 1;
-                    v[t][i] = 0.f;
-                } else {
-                    top[1][t >> 1] = max(top[1][t >> 1], y);
-                }
-            }
-            if (odd && keys) bad[t * 32 + col] = 1;
+        for (int i = 0; i < 32; ++i) {
+            a = max(a, __float_as_uint(k[i >> 4][i & 15]) & 0x7fffffffu);
+            b = max(b, __float_as_uint(v[i >> 4][i & 15]) & 0x7fffffffu);
         }
+        constexpr uint32_t kBig = (127u + 15) << 23, kSome = (127u - 6) << 23;
+        const uint32_t mine = (keys ? (__any(a >= kBig) ? 1u : 0u) | (__any(a >= kSome) ? 2u : 0u) : 0u) |
+                              (values ? (__any(b >= kBig) ? 4u : 0u) | (__any(b >= kSome) ? 8u : 0u) : 0u);
+        if (lane == 0) seen[head & 1][half][wave] = mine;
+        __syncthreads();
+        uint32_t all[2] = {0, 0};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            all[0] |= seen[head & 1][0][w];
+            all[1] |= seen[head & 1][1][w];
+        }
+        const bool plain = all[0] == 10u && all[1] == 10u;
+        if (!plain) {  // the exponents of the largest, and the slots with something that is not finite
+            if (threadIdx.x < 4) largest[threadIdx.x >> 1][threadIdx.x & 1] = 0;
+            if (threadIdx.x < 128) bad[threadIdx.x] = 0;  // (a workgroup has at least 128 threads)
+            __syncthreads();
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                uint32_t a = 0, b = 0;
+                bool odd = false;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t x = __float_as_uint(k[t][i]) & 0x7fffffffu, y = __float_as_uint(v[t][i]) & 0x7fffffffu;
+                    odd |= x >= 0x7f800000u;
+                    a = max(a, x >= 0x7f800000u ? 0u : x);
+                    if (y >= 0x7f800000u) {
+                        if (values) bad[half * 64 + t * 32 + row_of(i, grp)] = 1;
+                        v[t][i] = 0.f;
+                    } else {
+                        b = max(b, y);
+                    }
+                }
+                if (odd && keys) bad[half * 64 + t * 32 + col] = 1;
+                if (keys) atomicMax(&largest[0][half], a);
+                if (values) atomicMax(&largest[1][half], b);
+            }
+            __syncthreads();
+        }
+        const int64_t tile = ((int64_t)seq * m.heads + head) * m.tiles + pair * 2 + half;
+        const bool there = j0 + half * 64 < total;
+        u32x4* to = m.kv + tile * TILE;
+        const int down[2] = {plain ? 0 : shift_of(largest[0][half]), plain ? 0 : shift_of(largest[1][half])};
+        if (there && wave == 0 && lane == 0) m.shift[tile] = make_int2(down[0], down[1]);
+        const float fk = power(-down[0]), fv = power(-down[1]);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            if (keys) atomicMax(&largest[0][t], top[0][t]);
-            if (values) atomicMax(&largest[1][t], top[1][t]);
-        }
-        __syncthreads();
-        const int64_t tile = ((int64_t)seq * m.heads + head) * m.tiles + pair * 2;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            if (j0 + (t >> 1) * 64 >= total) continue;
-            u32x4* to = m.kv + (tile + (t >> 1)) * TILE;
-            const int down[2] = {shift_of(largest[0][t >> 1]), shift_of(largest[1][t >> 1])};
-            if (threadIdx.x == 0 && (t & 1) == 0) m.shift[tile + (t >> 1)] = make_int2(down[0], down[1]);
-            if (keys) {
-                const float f = power(-down[0]);
-                const bool out = bad[t * 32 + col] != 0;  // then no row that sees the slot stays finite
+            if (there && keys) {
+                const bool out = !plain && bad[half * 64 + t * 32 + col] != 0;  // then no row that sees the slot stays finite
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     u32x2 x;
-                    x.x = out ? 0x7e007e00u : pack_f16(k[t][4 * i] * f, k[t][4 * i + 1] * f);
-                    x.y = out ? 0x7e007e00u : pack_f16(k[t][4 * i + 2] * f, k[t][4 * i + 3] * f);
-                    ((u32x2*)(to + ((t & 1) * (NOPE / 16) + wave * 2 + (i >> 1)) * 64 + col + 32 * (i & 1)))[grp] = x;
+                    x.x = out ? 0x7e007e00u : pack_f16(k[t][4 * i] * fk, k[t][4 * i + 1] * fk);
+                    x.y = out ? 0x7e007e00u : pack_f16(k[t][4 * i + 2] * fk, k[t][4 * i + 3] * fk);
+                    ((u32x2*)(to + (t * (NOPE / 16) + wave * 2 + (i >> 1)) * 64 + col + 32 * (i & 1)))[grp] = x;
                 }
             }
-            if (values) {
-                const float f = power(-down[1]);
+            if (there && values) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     u32x4 x;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = pack_f16(v[t][8 * u + 2 * i] * f, v[t][8 * u + 2 * i + 1] * f);
-                    to[kSlots * NOPE / 8 + (((t & 1) * 2 + u) * VALUES + wave) * 64 + lane] = x;
+                    for (int i = 0; i < 4; ++i) x[i] = pack_f16(v[t][8 * u + 2 * i] * fv, v[t][8 * u + 2 * i + 1] * fv);
+                    to[kSlots * NOPE / 8 + ((t * 2 + u) * VALUES + wave) * 64 + lane] = x;
                 }
             }
         }
-        __syncthreads();
+        if (!plain) __syncthreads();  // `largest` and `bad` may be set anew
     }
 }
 
@@ -441,25 +480,36 @@ struct Plan {
     Made own, pre;
     Parts parts;
     int heads;  // at a time
-    int64_t o_ml, o_own_kv, o_own_pe, o_own_shift, o_pre_kv, o_pre_pe, o_pre_shift, bytes;
+    int64_t o_ml, o_w, o_own_kv, o_own_pe, o_own_shift, o_pre_kv, o_pre_pe, o_pre_shift, bytes;
     int64_t own_groups, pre_groups, own_expand, pre_expand, merges;  // workgroups of the launches of a set of heads
     int own_each, pre_each;
 };
 
 int64_t up256(int64_t v) { return (v + 255) & ~(int64_t)255; }
 
-// Slots of a range: about 512 workgroups, each of 512 slots and more.
-int range_of(int64_t most, int64_t groups) {
-    int64_t n = groups > 0 ? 512 / groups : 1;
+// Slots of a range, so that about `aim` workgroups get 512 slots and more.  Sequences: 1024, since tiles late in a long one see the most slots and
+// would be left alone at the end (3 chunks of 267 to 800 tokens behind up to 6001 slots, 240 workgroups whole: 140 us, in four ranges 83 and 7 to
+// merge).  The prefix, of which all tiles see the same: 512 (5 prompts of 97 to 300 tokens over 8001 slots, in two ranges 140 and 9, in four 140 and 14).
+int range_of(int64_t most, int64_t groups, int64_t aim) {
+    int64_t n = groups > 0 ? aim / groups : 1;
     n = min(n, most / 512);
     if (n < 1) n = 1;
     return (int)(((most + n - 1) / n + kSlots - 1) / kSlots * kSlots);
 }
 
-// Heads that one workgroup of expand_kernel makes, so that 512 remain.
+// Heads that one workgroup of expand_kernel makes: the fewest rounds of a workgroup per compute unit, each of its heads and, about as
+// long as one of them, its latents' way into LDS.
 int heads_each(int64_t tiles, int heads) {
-    const int64_t n = tiles * heads / 512;
-    return n < 1 ? 1 : n > 16 ? 16 : (int)n;
+    int best = 1;
+    int64_t least = INT64_MAX;
+    for (int n = 1; n <= heads && n <= 32; ++n) {
+        const int64_t rounds = (tiles * ((heads + n - 1) / n) + 255) / 256, cost = rounds * (n + 1);
+        if (cost < least) {
+            least = cost;
+            best = n;
+        }
+    }
+    return best;
 }
 
 Plan plan(const Cache& c, const Step& s, const Heads& h) {
@@ -476,7 +526,7 @@ Plan plan(const Cache& c, const Step& s, const Heads& h) {
     const int64_t about = min(c.n_seq * own_rows, (int64_t)s.n_rows / kRows + (c.n_seq + 1) / 2 + 1);
     p.own.tiles = (int)tiles;
     p.own.row_tiles = (int)own_rows;
-    p.own.per = range_of(most, about * p.heads);
+    p.own.per = range_of(most, about * p.heads, 1024);
     p.own.ranges = (int)((most + p.own.per - 1) / p.own.per);
     p.parts.per = p.own.per;
     p.parts.own = p.parts.all = p.own.ranges;
@@ -487,7 +537,7 @@ Plan plan(const Cache& c, const Step& s, const Heads& h) {
     if (c.prefix_len > 0) {
         p.pre.tiles = (int)pre_tiles;
         p.pre.row_tiles = (int)pre_rows;
-        p.pre.per = range_of(c.prefix_len, pre_rows * p.heads);
+        p.pre.per = range_of(c.prefix_len, pre_rows * p.heads, 512);
         p.pre.ranges = (int)((c.prefix_len + p.pre.per - 1) / p.pre.per);
         p.pre.part0 = p.parts.own;
         p.parts.pre_per = p.pre.per;
@@ -507,6 +557,7 @@ Plan plan(const Cache& c, const Step& s, const Heads& h) {
         return at;
     };
     p.o_ml = take(items * 8);
+    p.o_w = take((int64_t)h.n * (h.nope + h.v) * c.latent * 2);
     p.o_own_kv = take(c.n_seq * p.heads * tiles * tile);
     p.o_own_pe = take(c.n_seq * tiles * pe);
     p.o_own_shift = take(c.n_seq * p.heads * tiles * 8);
@@ -528,7 +579,7 @@ struct Call {
 
 template <int DC, int NOPE, int DV>
 void launch_expand(const Call& k, const Made& m, int64_t groups, int each, bool prefix) {
-    const dim3 grid((unsigned)groups), block(256);
+    const dim3 grid((unsigned)groups), block(128 * expand_waves(NOPE, DV));
     if (prefix) hipLaunchKernelGGL((expand_kernel<DC, NOPE, DV, true>), grid, block, 0, k.st, k.c, k.s, k.h, m, each);
     else hipLaunchKernelGGL((expand_kernel<DC, NOPE, DV, false>), grid, block, 0, k.st, k.c, k.s, k.h, m, each);
 }
@@ -574,6 +625,7 @@ void launch_expanded(hipStream_t st, const Cache& c, const Step& s, const Heads&
     p.parts.acc = (float*)a.ws;
     p.parts.ml = (float2*)(a.ws + p.o_ml);
     const Call k{st, c, s, h, a, p.parts};
+    hipLaunchKernelGGL(order_kernel, dim3((unsigned)(h.n * (h.nope + h.v) / 32)), dim3(256), 0, st, h, c.latent, (u32x4*)(a.ws + p.o_w));
     for (int head = 0; head < h.n; head += p.heads) {
         const int heads = min(p.heads, h.n - head);
         auto made = [&](Made m, int64_t kv, int64_t pe, int64_t shift) {
@@ -582,6 +634,7 @@ void launch_expanded(hipStream_t st, const Cache& c, const Step& s, const Heads&
             m.kv = (u32x4*)(a.ws + kv);
             m.pe = (u32x4*)(a.ws + pe);
             m.shift = (int2*)(a.ws + shift);
+            m.w = (const u32x4*)(a.ws + p.o_w);
             return m;
         };
         // the last set of heads may be smaller: its launches have the workgroups of its own heads
