@@ -53,20 +53,25 @@ __global__ __launch_bounds__(256) void append_kernel(Cache c, Step s, Append a) 
 // rows of 2 * latent + rope elements, in the caller's order of rows and heads.  (a counts with 16 bits: rounded to 8 it would move
 // the scores, and with them the outputs, by more than the outputs' own rounding: 2.8e-3 over 3000 slots, where that is 1.7e-3.)
 //
-// One wavefront per (head, 128 latents, `each` tiles of 32 rows): its piece of w_k lies in LDS (nope_dim x 256 bytes) and is read
-// transposed by the LDS, four latents of four rows at a time, as the first operand: a^T = w_k^T n^T, so that a lane has one row and
-// four latents side by side.  The result goes through LDS to leave in pieces of 256 bytes.
-template <int NOPE>
-__global__ __launch_bounds__(64) void absorb_kernel(Cache c, Heads h, Rows q, int n_rows, int each, uint16_t* out) {
-    __shared__ u32x4 w[NOPE * 16], o[2][32 * 16];
-    const int lane = threadIdx.x, col = lane & 31, grp = lane >> 5;
+// A workgroup of WAVES wavefronts per (head, 128 latents, `each` tiles of 32 rows for each of them): its piece of w_k lies in LDS (nope_dim x
+// 256 bytes) and is read transposed by the LDS, four latents of four rows at a time, as the first operand: a^T = w_k^T n^T, so that a lane
+// has one row and four latents side by side.  The result goes through LDS to leave in pieces of 256 bytes.  Bound by the bytes written (four
+// for every latent) where there are many rows, by latency where there are few: then one wavefront a workgroup.
+template <int NOPE, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void absorb_kernel(Cache c, Heads h, Rows q, int n_rows, int each, uint16_t* out) {
+    __shared__ u32x4 w[NOPE * 16], stage[WAVES][32 * 16];
+    const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, grp = lane >> 5;
     const int chunks = c.latent / 128, head = blockIdx.x % h.n, rest = blockIdx.x / h.n, chunk = rest % chunks;
-    const int tile0 = rest / chunks * each, tiles = (n_rows + 31) / 32, width = 2 * c.latent + c.rope;
+    const int tile0 = rest / chunks * each * WAVES + wave, tiles = (n_rows + 31) / 32, width = 2 * c.latent + c.rope;
+    u32x4* o = stage[wave];
     // rows of w_k four at a time; 16-byte units of a row lie at an xor of its number, which spreads the transposed reads over the banks
     const uint16_t* from = h.w_k + head * h.w_k_head + chunk * 128 + (lane >> 4) * c.latent + ((lane & 15) ^ (lane >> 4 & 3) << 2) * 8;
     const uint32_t w_at = lds_address(w);
 #pragma unroll
-    for (int i = 0; i < NOPE / 4; ++i) copy_to_lds(from + (int64_t)i * 4 * c.latent, __builtin_amdgcn_readfirstlane(w_at + i * 1024));
+    for (int i = 0; i < NOPE / 4 / WAVES; ++i) {
+        const int four = i * WAVES + wave;
+        copy_to_lds(from + (int64_t)four * 4 * c.latent, __builtin_amdgcn_readfirstlane(w_at + four * 1024));
+    }
     u32x4 n[NOPE / 16];
     const uint16_t* rows = q.p + (int64_t)head * q.head + grp * 8;
     auto load = [&](int tile) {
@@ -81,7 +86,9 @@ __global__ __launch_bounds__(64) void absorb_kernel(Cache c, Heads h, Rows q, in
     const int rr = (lane & 15) >> 2;
     const uint32_t at = w_at + (8 * grp + rr) * 256 + (lane & 1) * 8;
     const int unit = (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
-    for (int t = 0; t < each && tile0 + t < tiles; ++t) {
+    for (int t = 0; t < each; ++t) {
+        const int tile = tile0 + t * WAVES;
+        if (tile >= tiles) break;
         f32x16 acc[4];
 #pragma unroll
         for (int b = 0; b < 4; ++b)
@@ -94,32 +101,33 @@ __global__ __launch_bounds__(64) void absorb_kernel(Cache c, Heads h, Rows q, in
                 const uint32_t p = at + f * 4096 + ((b * 4 + unit) ^ rr << 2) * 16;
                 acc[b] = mfma32(join(read_transposed(p), read_transposed(p + 1024)), n[f], acc[b]);
             }
-        const int row0 = (tile0 + t) * 32;
-        if (t + 1 < each && tile0 + t + 1 < tiles) load(tile0 + t + 1);
+        const int row0 = tile * 32;
+        if (t + 1 < each) load(tile + WAVES);
+        uint16_t* to = out + ((int64_t)row0 * h.n + head) * width + chunk * 128 + (lane & 15) * 8;
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+        for (int second = 0; second < 2; ++second) {  // what is left over goes where the values themselves went before: only this wavefront's
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                u32x2 x, y;
+            for (int b = 0; b < 4; ++b)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float e = acc[b][4 * i + 2 * j], e2 = acc[b][4 * i + 2 * j + 1];
-                    x[j] = pack_bf16(e, e2);
-                    y[j] = pack_bf16(e - bf_lo(x[j]), e2 - bf_hi(x[j]));
+                for (int i = 0; i < 4; ++i) {
+                    u32x2 x;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int e = 4 * i + 2 * j;
+                        x[j] = pack_bf16(acc[b][e], acc[b][e + 1]);
+                        acc[b][e] -= bf_lo(x[j]);
+                        acc[b][e + 1] -= bf_hi(x[j]);
+                    }
+                    ((u32x2*)&o[col * 16 + ((b * 4 + i) ^ (col & 15))])[grp] = x;
                 }
-                const int at = col * 16 + ((b * 4 + i) ^ (col & 15));
-                ((u32x2*)&o[0][at])[grp] = x;
-                ((u32x2*)&o[1][at])[grp] = y;
-            }
-        __syncthreads();
+            wave_sync();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int in = i * 4 + (lane >> 4), row = row0 + in;
-            if (row < n_rows) {
-                uint16_t* to = out + ((int64_t)row * h.n + head) * width + chunk * 128 + (lane & 15) * 8;
-                *(u32x4*)to = o[0][in * 16 + ((lane & 15) ^ (in & 15))];
-                *(u32x4*)(to + c.latent + c.rope) = o[1][in * 16 + ((lane & 15) ^ (in & 15))];
+            for (int i = 0; i < 8; ++i) {
+                const int in = i * 4 + (lane >> 4);
+                if (row0 + in < n_rows)
+                    *(u32x4*)(to + (int64_t)in * h.n * width + second * (c.latent + c.rope)) = o[in * 16 + ((lane & 15) ^ (in & 15))];
             }
+            wave_sync();
         }
         if (chunk == 0) {
             const int units = c.rope / 8;
@@ -130,91 +138,170 @@ __global__ __launch_bounds__(64) void absorb_kernel(Cache c, Heads h, Rows q, in
                         *(const u32x4*)(q.p + (int64_t)row * q.row + (int64_t)head * q.head + NOPE + u * 8);
             }
         }
-        __syncthreads();
     }
 }
 
-// o = w_v u / sum for 32 rows of one head: the parts of a row's sums are brought to the largest reference and added,
-// the result goes into LDS as two bf16 (value and what rounding it left over) in the order of the matrix instructions, and every
-// wavefront takes 32 of the value's elements.  w_v is asked for before the parts are read.
-template <int DC>
-__global__ __launch_bounds__(256) void finish_kernel(Cache c, Step s, Heads h, RowsOut out, Parts parts) {
-    constexpr int F = DC / 16;
+// o = w_v u / sum for 32 rows of one head: the parts of a row's sums are brought to the largest reference and added (a wavefront
+// per row; FEW: all eight share a row), the result goes into LDS as two bf16 (value and what rounding it left over) in the
+// order of the matrix instructions, and the wavefronts take 32 of the value's elements and a share of the latents each, which then meet
+// in LDS.  w_v is asked for before the parts are read.  Bound by latency where there are few rows, then by the parts' bytes.
+template <int DC, int DV, bool FEW>
+__global__ __launch_bounds__(512, FEW ? 2 : 4) void finish_kernel(Cache c, Step s, Heads h, RowsOut out, Parts parts) {
+    constexpr int BLOCKS = DV / 32, SHARES = 8 / BLOCKS, F = DC / 16 / SHARES, Q = DC / 4 > 64 ? DC / 256 : 1;  // pieces of four elements that a lane has
     __shared__ u32x4 u[2][DC / 8 * 32];
-    __shared__ int there[32];
+    __shared__ int own_parts[32];                    // of a row's slots; 0: no row
+    __shared__ f32x4 shared_sums[FEW ? 8 : 1][FEW ? (DC / 4 < 64 ? 64 : DC / 4) : 1];
+    constexpr bool FITS = sizeof u >= 8 * 4096 + 32 * DV * 2;  // the shares of the product and the rows that leave
+    __shared__ f32x4 shares_apart[FITS ? 1 : 8 * 256 + 32 * DV / 8];
     const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, grp = lane >> 5;
-    const int head = blockIdx.x % h.n, row0 = blockIdx.x / h.n * 32;
-    const bool busy = wave * 32 < h.v;
+    const int head = blockIdx.x % h.n, row0 = blockIdx.x / h.n * 32, rows = min(32, s.n_rows - row0);
+    if (threadIdx.x < 32) {
+        int own = 0;
+        if ((int)threadIdx.x < rows) {
+            Seq q;
+            int token;
+            if (lane_seq_of_row(c, s, row0 + threadIdx.x, &token, &q) >= 0) own = (q.cached + token + parts.per) / parts.per;
+        }
+        own_parts[threadIdx.x] = own;
+    }
+    const int block = wave % BLOCKS, share = wave / BLOCKS;
     u32x4 wf[F];
-    if (busy) {
-        const uint16_t* p = h.w_v + head * h.w_v_head + (int64_t)(wave * 32 + col) * DC + grp * 8;
+    {
+        const uint16_t* p = h.w_v + head * h.w_v_head + (int64_t)(block * 32 + col) * DC + share * F * 16 + grp * 8;
 #pragma unroll
         for (int f = 0; f < F; ++f) wf[f] = *(const u32x4*)(p + f * 16);
     }
-    for (int i = wave * 8; i < wave * 8 + 8; ++i) {
-        const int row = row0 + i;
-        Seq q;
-        int token = 0;
-        const int seq = row < s.n_rows ? seq_of_row(c, s, row, &token, &q) : -1;
-        float x[8];
+    __syncthreads();
+    // FEW: one row after the other; else the wavefront's four rows two by two, so that their reads are on the way together
+    constexpr int R = FEW ? 1 : 2;
+    for (int i0 = 0; i0 < (FEW ? rows : 4 / R); ++i0) {
+        const auto row_of_wave = [&](int r) { return FEW ? i0 : wave + 8 * (R * i0 + r); };
+        int own[R], n[R], most = 0;
+        int64_t item[R];
+        float ref[R], sum[R];
+        f32x4 x[R][Q];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = 0.f;
-        if (seq >= 0) {
-            const int own = (q.cached + token + parts.per) / parts.per;  // parts of the slots that the row sees
-            const int64_t item = ((int64_t)row * h.n + head) * parts.all;
-            const int n = own + parts.all - parts.own;
-            float ref = kEmpty, sum = 0.f;
-            for (int k = 0; k < n; ++k) ref = fmaxf(ref, parts.ml[item + (k < own ? k : parts.own + k - own)].x);
-            for (int k = 0; k < n; ++k) {
-                const int64_t at = item + (k < own ? k : parts.own + k - own);
-                const float2 ml = parts.ml[at];
-                const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-                sum = __builtin_fmaf(ml.y, f, sum);
-                if (lane * 8 < DC) {
-                    const f32x4* p = (const f32x4*)(parts.acc + at * DC + lane * 8);
-                    const f32x4 a = p[0], b = p[1];
+        for (int r = 0; r < R; ++r) {
+            own[r] = __builtin_amdgcn_readfirstlane(own_parts[row_of_wave(r)]);
+            n[r] = own[r] > 0 ? own[r] + parts.all - parts.own : 0;
+            most = max(most, n[r]);
+            item[r] = ((int64_t)(row0 + row_of_wave(r)) * h.n + head) * parts.all;
+            ref[r] = kEmpty;
+            sum[r] = 0.f;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        x[j] = __builtin_fmaf(a[j], f, x[j]);
-                        x[4 + j] = __builtin_fmaf(b[j], f, x[4 + j]);
-                    }
+            for (int j = 0; j < Q; ++j) x[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        const auto at = [&](int r, int k) { return item[r] + (k < own[r] ? k : parts.own + k - own[r]); };
+        for (int k = lane; k < (most + 63 & ~63); k += 64)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (k < n[r]) ref[r] = fmaxf(ref[r], parts.ml[at(r, k)].x);
+#pragma unroll
+        for (int m = 32; m > 0; m /= 2)
+#pragma unroll
+            for (int r = 0; r < R; ++r) ref[r] = fmaxf(ref[r], __shfl_xor(ref[r], m, 64));
+        for (int k0 = 0; k0 < most; k0 += 64) {
+            float f[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                f[r] = 0.f;
+                if (k0 + lane < n[r]) {
+                    const float2 ml = parts.ml[at(r, k0 + lane)];
+                    f[r] = __builtin_amdgcn_exp2f(ml.x - ref[r]);
+                    sum[r] = __builtin_fmaf(ml.y, f[r], sum[r]);
                 }
             }
-            const float inv = 1.f / sum;
+            for (int k = FEW ? wave : 0; k < min(64, most - k0); k += FEW ? 8 : 1) {
+                f32x4 y[R][Q];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] *= inv;
-        }
-        if (lane == 0) there[i] = seq >= 0;
-        if (lane * 8 < DC) {
-            u32x4 hi, lo;
+                for (int r = 0; r < R; ++r) {
+                    // past a row's last part the last one again, which then counts 0 times
+                    const f32x4* p = (const f32x4*)(parts.acc + at(r, max(0, min(k0 + k, n[r] - 1))) * DC) + lane;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                hi[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
-                lo[j] = pack_bf16(x[2 * j] - bf_lo(hi[j]), x[2 * j + 1] - bf_hi(hi[j]));
+                    for (int j = 0; j < Q; ++j) y[r][j] = n[r] > 0 && (DC / 4 >= 64 || lane < DC / 4) ? p[j * 64] : f32x4{0.f, 0.f, 0.f, 0.f};
+                }
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    if (k0 + k >= n[r]) continue;
+                    const float by = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f[r]), k));
+#pragma unroll
+                    for (int j = 0; j < Q; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[r][j][e] = __builtin_fmaf(y[r][j][e], by, x[r][j][e]);
+                }
             }
-            u[0][lane * 32 + (i ^ (lane & 31))] = hi;
-            u[1][lane * 32 + (i ^ (lane & 31))] = lo;
         }
+#pragma unroll
+        for (int m = 32; m > 0; m /= 2)
+#pragma unroll
+            for (int r = 0; r < R; ++r) sum[r] += __shfl_xor(sum[r], m, 64);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float inv = n[r] > 0 ? 1.f / sum[r] : 0.f;
+#pragma unroll
+            for (int j = 0; j < Q; ++j) x[r][j] *= inv;
+        }
+        if constexpr (FEW) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < Q; ++j) shared_sums[wave][j * 64 + lane] = x[0][j];
+            __syncthreads();
+            if (wave != 0) continue;
+#pragma unroll
+            for (int j = 0; j < Q; ++j)
+#pragma unroll
+                for (int w = 1; w < 8; ++w) x[0][j] += shared_sums[w][j * 64 + lane];
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = 0; j < Q; ++j) {
+                const int piece = j * 64 + lane, unit = piece >> 1;  // of four elements, of eight
+                if (piece * 4 >= DC) continue;
+                u32x2 hi, lo;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    hi[e] = pack_bf16(x[r][j][2 * e], x[r][j][2 * e + 1]);
+                    lo[e] = pack_bf16(x[r][j][2 * e] - bf_lo(hi[e]), x[r][j][2 * e + 1] - bf_hi(hi[e]));
+                }
+                ((u32x2*)&u[0][unit * 32 + (row_of_wave(r) ^ (unit & 31))])[piece & 1] = hi;
+                ((u32x2*)&u[1][unit * 32 + (row_of_wave(r) ^ (unit & 31))])[piece & 1] = lo;
+            }
     }
     __syncthreads();
-    if (!busy) return;
     f32x16 acc;
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[i] = 0.f;
 #pragma unroll
     for (int f = 0; f < F; ++f) {
-        const int unit = 2 * f + grp;
+        const int unit = 2 * (share * F + f) + grp;
         acc = mfma32(wf[f], u[0][unit * 32 + (col ^ (unit & 31))], acc);
         acc = mfma32(wf[f], u[1][unit * 32 + (col ^ (unit & 31))], acc);
     }
-    if (!there[col]) return;
-    uint16_t* o = out.p + (int64_t)(row0 + col) * out.row + (int64_t)head * out.head + wave * 32 + 4 * grp;
+    f32x4* shares = FITS ? (f32x4*)&u[0][0] : shares_apart;
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 4; ++i) shares[(wave * 4 + i) * 64 + lane] = f32x4{acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]};
+    __syncthreads();
+    // four elements of a row a piece: wavefront w takes pieces w, w + 8 ... of BLOCKS * 4; through LDS, so that a row leaves in one piece
+    u32x2* rows_out = (u32x2*)(shares + 8 * 256);
+#pragma unroll
+    for (int n = 0; n < (BLOCKS * 4 + 7) / 8; ++n) {
+        const int piece = n * 8 + wave;
+        if (piece >= BLOCKS * 4) break;
+        f32x4 y = shares[piece * 64 + lane];  // share 0 of block piece / 4
+#pragma unroll
+        for (int k = 1; k < SHARES; ++k) y += shares[(k * BLOCKS * 4 + piece) * 64 + lane];
         u32x2 x;
-        x.x = pack_bf16(acc[4 * i], acc[4 * i + 1]);
-        x.y = pack_bf16(acc[4 * i + 2], acc[4 * i + 3]);
-        *(u32x2*)(o + 8 * i) = x;
+        x.x = pack_bf16(y[0], y[1]);
+        x.y = pack_bf16(y[2], y[3]);
+        rows_out[(col * (DV / 8) + (piece ^ (col & (DV / 8 - 1)))) * 2 + grp] = x;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * (DV / 8); i += 512) {
+        const int row = i / (DV / 8), piece = i % (DV / 8);
+        if (own_parts[row] != 0)
+            *(u32x4*)(out.p + (int64_t)(row0 + row) * out.row + (int64_t)head * out.head + piece * 8) = ((const u32x4*)rows_out)[row * (DV / 8) + (piece ^ (row & (DV / 8 - 1)))];
     }
 }
 
@@ -224,32 +311,53 @@ void launch_append(hipStream_t st, const Cache& c, const Step& s, const Append& 
     hipLaunchKernelGGL(append_kernel, dim3((unsigned)((s.n_rows + 3) / 4)), dim3(256), 0, st, c, s, a);
 }
 
-// Tiles of 32 rows of a wavefront: about 2048 wavefronts, which are eight per compute unit.
+// Wavefronts of a workgroup, and tiles of 32 rows of each: about 2048 wavefronts, which are eight per compute unit.
+static int absorb_waves(int n_rows) { return n_rows > 64 ? 4 : 1; }
 static int absorb_each(const Cache& c, const Heads& h, int n_rows) {
     const int64_t all = (int64_t)h.n * (c.latent / 128) * ((n_rows + 31) / 32);
     return all > 2048 ? (int)((all + 2047) / 2048) : 1;
 }
 
 int64_t absorb_groups(const Cache& c, const Heads& h, int n_rows) {
-    const int64_t tiles = (n_rows + 31) / 32, each = absorb_each(c, h, n_rows);
-    return h.n * (c.latent / 128) * ((tiles + each - 1) / each);
+    const int64_t tiles = (n_rows + 31) / 32, of = absorb_each(c, h, n_rows) * absorb_waves(n_rows);
+    return h.n * (c.latent / 128) * ((tiles + of - 1) / of);
+}
+
+template <int NOPE>
+static void launch_absorb_nope(hipStream_t st, const Cache& c, const Heads& h, const Rows& q, int n_rows, uint16_t* out) {
+    const dim3 grid((unsigned)absorb_groups(c, h, n_rows));
+    const int each = absorb_each(c, h, n_rows);
+    if (absorb_waves(n_rows) == 4) hipLaunchKernelGGL((absorb_kernel<NOPE, 4>), grid, dim3(256), 0, st, c, h, q, n_rows, each, out);
+    else hipLaunchKernelGGL((absorb_kernel<NOPE, 1>), grid, dim3(64), 0, st, c, h, q, n_rows, each, out);
 }
 
 void launch_absorb(hipStream_t st, const Cache& c, const Heads& h, const Rows& q, int n_rows, uint16_t* out) {
-    const dim3 grid((unsigned)absorb_groups(c, h, n_rows)), block(64);
-    const int each = absorb_each(c, h, n_rows);
-    if (h.nope == 32) hipLaunchKernelGGL(absorb_kernel<32>, grid, block, 0, st, c, h, q, n_rows, each, out);
-    if (h.nope == 64) hipLaunchKernelGGL(absorb_kernel<64>, grid, block, 0, st, c, h, q, n_rows, each, out);
-    if (h.nope == 128) hipLaunchKernelGGL(absorb_kernel<128>, grid, block, 0, st, c, h, q, n_rows, each, out);
+    if (h.nope == 32) launch_absorb_nope<32>(st, c, h, q, n_rows, out);
+    if (h.nope == 64) launch_absorb_nope<64>(st, c, h, q, n_rows, out);
+    if (h.nope == 128) launch_absorb_nope<128>(st, c, h, q, n_rows, out);
 }
 
 int64_t finish_groups(const Heads& h, int n_rows) { return (int64_t)h.n * ((n_rows + 31) / 32); }
 
+namespace {
+template <int DC, int DV>
+void launch_finish_sizes(hipStream_t st, const Cache& c, const Step& s, const Heads& h, const RowsOut& out, const Parts& parts) {
+    const dim3 grid((unsigned)finish_groups(h, s.n_rows)), block(512);
+    if (s.n_rows <= 4) hipLaunchKernelGGL((finish_kernel<DC, DV, true>), grid, block, 0, st, c, s, h, out, parts);
+    else hipLaunchKernelGGL((finish_kernel<DC, DV, false>), grid, block, 0, st, c, s, h, out, parts);
+}
+template <int DC>
+void launch_finish_latent(hipStream_t st, const Cache& c, const Step& s, const Heads& h, const RowsOut& out, const Parts& parts) {
+    if (h.v == 32) launch_finish_sizes<DC, 32>(st, c, s, h, out, parts);
+    if (h.v == 64) launch_finish_sizes<DC, 64>(st, c, s, h, out, parts);
+    if (h.v == 128) launch_finish_sizes<DC, 128>(st, c, s, h, out, parts);
+}
+}  // namespace
+
 void launch_finish(hipStream_t st, const Cache& c, const Step& s, const Heads& h, const RowsOut& out, const Parts& parts) {
-    const dim3 grid((unsigned)finish_groups(h, s.n_rows)), block(256);
-    if (c.latent == 128) hipLaunchKernelGGL(finish_kernel<128>, grid, block, 0, st, c, s, h, out, parts);
-    if (c.latent == 256) hipLaunchKernelGGL(finish_kernel<256>, grid, block, 0, st, c, s, h, out, parts);
-    if (c.latent == 512) hipLaunchKernelGGL(finish_kernel<512>, grid, block, 0, st, c, s, h, out, parts);
+    if (c.latent == 128) launch_finish_latent<128>(st, c, s, h, out, parts);
+    if (c.latent == 256) launch_finish_latent<256>(st, c, s, h, out, parts);
+    if (c.latent == 512) launch_finish_latent<512>(st, c, s, h, out, parts);
 }
 
 }  // namespace klat

@@ -36,7 +36,7 @@ struct Run {  // one launch
 // 64 registers and the rows 136, which leaves two wavefronts to a SIMD.
 // References of the softmax are whole numbers, so that bringing sums or weights from one to another is exact.  The two wavefronts of a row
 // set theirs by their own halves; behind the barrier everybody sees both and goes on with the larger one.
-template <int DC, int DR, int MT, bool PREFIX>
+template <int DC, int DR, int MT, bool PREFIX, bool STREAM>
 __global__ __launch_bounds__(256 * MT, 2) void absorbed_kernel(Cache c, Step s, Run run) {
     typedef Tile<DC, DR> T;
     constexpr int WAVES = 4 * MT, GROUPS = 2 * MT, SUB = MT, M = 32 * MT;
@@ -50,12 +50,14 @@ __global__ __launch_bounds__(256 * MT, 2) void absorbed_kernel(Cache c, Step s, 
     __shared__ float sm_ref[2][M], sm_sum[2][M];
     const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, grp = lane >> 5, c16 = lane & 15, g16 = lane >> 4;
     const int rows16 = wave % GROUPS, half = wave / GROUPS;
-    int seq = 0, rest = blockIdx.x;
+    // of a sequence the row tiles one behind the other, so that they read its slots together; of the prefix the ranges, each to its XCD
+    int seq = 0, range = blockIdx.x % run.ranges, tile = run.row_tiles - 1 - (int)blockIdx.x / run.ranges;
     if (!PREFIX) {
         seq = blockIdx.x % c.n_seq;
-        rest = blockIdx.x / c.n_seq;
+        const int rest = blockIdx.x / c.n_seq;
+        tile = run.row_tiles - 1 - rest % run.row_tiles;  // those that see the most slots first
+        range = rest / run.row_tiles;
     }
-    const int range = rest % run.ranges, tile = run.row_tiles - 1 - rest / run.ranges;  // those that see the most slots first
     Seq q;
     if (PREFIX) q = Seq{0, s.n_rows, 0};
     else q = kkv8::sequence(c.max_len, s, seq);
@@ -82,7 +84,9 @@ __global__ __launch_bounds__(256 * MT, 2) void absorbed_kernel(Cache c, Step s, 
 #pragma unroll
         for (int g = 0; g < T::kGroups; ++g) {
             const bool cut = T::kHalf && g == T::kGroups - 1;  // the row ends within the group
-            copy_to_lds((const uint8_t*)C + g * 128, cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, copy_at + buf * STEP + g * 4096);
+const uint32_t from = cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, to = copy_at + buf * STEP + g * 4096;
+            if constexpr (STREAM) stream_to_lds((const uint8_t*)C + g * 128, from, to);
+            else copy_to_lds((const uint8_t*)C + g * 128, from, to);
         }
     };
     copy(0, first);
@@ -140,38 +144,49 @@ __global__ __launch_bounds__(256 * MT, 2) void absorbed_kernel(Cache c, Step s, 
         // the rows that see them become NaN, as they have to, and no others.  Done by the wavefront that brought the slots.
         if (!PREFIX && all_see < sees && j0 + SUB * 32 > all_see) {
             const uint32_t at = lds_at + buf * STEP + sub * T::kBytes;
-            for (int i = 0; i < 8; ++i) {
-                const int slot = quarter * 8 + i;
+#pragma unroll 1
+            for (int slot = quarter * 8; slot < quarter * 8 + 8; ++slot) {
                 const uint32_t to = at + (lane >> 3) * 4096 + slot * 128 + ((lane & 7) ^ twist(slot)) * 16;
+                // word by word: registers are short here
                 bool bad = false;
-                if (lane * 8 < DC) {
-                    const u32x4 x = read_lds(to);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) bad |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
+#pragma unroll 1
+                for (int e = 0; e < 16 && lane * 8 < DC; e += 4) {
+                    const uint32_t x = read_lds_word(to + e);
+                    bad |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
                 }
                 if (__any(bad)) {
-                    if (lane * 8 < DC) write_lds(to, u32x4{0u, 0u, 0u, 0u});
-                    if (lane == 0)
-                        write_lds(at + (DC / 64) * 4096 + slot * 128 + twist(slot) * 16, u32x4{0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu});
+#pragma unroll 1
+                    for (int e = 0; e < 16; e += 4) {
+                        if (lane * 8 < DC) write_lds_word(to + e, 0u);
+                        if (lane == 0) write_lds_word(at + (DC / 64) * 4096 + slot * 128 + twist(slot) * 16 + e, 0x7fff7fffu);
+                    }
                 }
             }
             __syncthreads();
         }
-        f32x4 z[SUB], y[SUB];  // two chains of products a tile, which do not wait for one another
+        // two chains of products, which do not wait for one another: of the two tiles, or of one tile's first and second halves
+        f32x4 z[2];
+        z[0] = z[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-            z[u] = y[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int u = 0; u < SUB; ++u)
 #pragma unroll
             for (int f = 0; f < KEYS; ++f) {
                 const u32x4 k = read_lds(key_at[f & 1] + buf * STEP + u * T::kBytes + (f >> 1) * 4096);
                 z[u] = mfma16(k, hi[f], z[u]);
-                if (f < LOW) y[u] = mfma16(k, lo[f], y[u]);
+                if (f < LOW) z[SUB == 1 ? 1 : u] = mfma16(k, lo[f], z[SUB == 1 ? 1 : u]);
             }
+        // four keys on their way ahead of their products: left to itself the compiler, short of registers, waits for every one
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int i = 0; i < SUB * KEYS - 4; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(0x8, 8, 0);
+        if (SUB == 1) z[0] += z[1];
         float top = -__builtin_inff();
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
-            z[u] += y[u];
             const int within = limit - j0 - u * 32 - half * 16 - 4 * g16;
             if (j0 + SUB * 32 > all_see || j0 + SUB * 32 > end) {
 #pragma unroll
@@ -195,67 +210,70 @@ __global__ __launch_bounds__(256 * MT, 2) void absorbed_kernel(Cache c, Step s, 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) z[u][i] = of(z[u][i]);
         });
+        u32x2 w[SUB];
 #pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-            u32x2 w;  // the sum is that of the weights as rounded: then one slot that has nearly all of it counts nearly exactly
-            w.x = pack_bf16(__builtin_amdgcn_exp2f(z[u][0]), __builtin_amdgcn_exp2f(z[u][1]));
-            w.y = pack_bf16(__builtin_amdgcn_exp2f(z[u][2]), __builtin_amdgcn_exp2f(z[u][3]));
-            sum += (bf_lo(w.x) + bf_hi(w.x)) + (bf_lo(w.y) + bf_hi(w.y));
-            write_lds2(put_at + u * M * 64, w);
+        for (int u = 0; u < SUB; ++u) {  // the sum is that of the weights as rounded: then one slot that has nearly all of it counts nearly exactly
+            w[u].x = pack_bf16(__builtin_amdgcn_exp2f(z[u][0]), __builtin_amdgcn_exp2f(z[u][1]));
+            w[u].y = pack_bf16(__builtin_amdgcn_exp2f(z[u][2]), __builtin_amdgcn_exp2f(z[u][3]));
+            sum += (bf_lo(w[u].x) + bf_hi(w[u].x)) + (bf_lo(w[u].y) + bf_hi(w[u].y));
+            write_lds2(put_at + u * M * 64, w[u]);
         }
         if (g16 == 0) sm_ref[half][my_row] = ref;
         __syncthreads();
-        float ref0[ROW_TILES], ref1[ROW_TILES];
+        // the references of a wavefront's lanes: row `lane` of all (32 of them twice with MT = 1)
+        const float both0 = sm_ref[0][lane & (M - 1)], both1 = sm_ref[1][lane & (M - 1)];
+        if (__any(both0 != both1)) {  // the same for the whole workgroup: halves that are behind bring their weights up
+            const float now = fmaxf(ref, sm_ref[half ^ 1][my_row]), f = __builtin_amdgcn_exp2f(ref - now);
+            sum *= f;
+            ref = now;
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+                write_lds2(put_at + u * M * 64, u32x2{pack_bf16(bf_lo(w[u].x) * f, bf_hi(w[u].x) * f), pack_bf16(bf_lo(w[u].y) * f, bf_hi(w[u].y) * f)});
+            __syncthreads();
+        }
+        float now[ROW_TILES];
         bool moved = false;
 #pragma unroll
         for (int r = 0; r < ROW_TILES; ++r) {
-            ref0[r] = sm_ref[0][(tile32 + r) * 32 + col];
-            ref1[r] = sm_ref[1][(tile32 + r) * 32 + col];
-            moved |= ref0[r] != sums_ref[r] || ref1[r] != sums_ref[r];
+            const int row = (tile32 + r) * 32 + col;
+            now[r] = fmaxf(sm_ref[0][row], sm_ref[1][row]);
+            moved |= now[r] != sums_ref[r];
         }
-        const float other = sm_ref[half ^ 1][my_row];
-        if (other > ref) {
-            sum *= __builtin_amdgcn_exp2f(ref - other);
-            ref = other;
-        }
-        const bool any_moved = __any(moved);
-        if (any_moved) {
+        if (__any(moved)) {
 #pragma unroll
             for (int r = 0; r < ROW_TILES; ++r) {
-                const float now = fmaxf(ref0[r], ref1[r]), f = __builtin_amdgcn_exp2f(sums_ref[r] - now);
-                sums_ref[r] = now;
-                ref0[r] = __builtin_amdgcn_exp2f(ref0[r] - now);  // from here on factors of the halves' weights
-                ref1[r] = __builtin_amdgcn_exp2f(ref1[r] - now);
+                const float f = __builtin_amdgcn_exp2f(sums_ref[r] - now[r]);
+                sums_ref[r] = now[r];
 #pragma unroll
                 for (int b = 0; b < COLS; ++b)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) acc[b][r][i] *= f;
             }
         }
+        // Blocks of values AHEAD - 1 of their products, with the weights of half a tile: the order is laid down, since the compiler,
+        // short of registers, would wait for every read.
+        constexpr int AHEAD = MT == 2 ? 2 : 3, ITEMS = 2 * SUB * COLS;
+        u32x4 p[2][ROW_TILES], v[AHEAD];
+        auto fetch = [&](int n) {
+            const int u = n / COLS >> 1, h = n / COLS & 1, b = n % COLS;
+            if (b == 0) {
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                u32x4 w[ROW_TILES];
-#pragma unroll
-                for (int r = 0; r < ROW_TILES; ++r) {
-                    w[r] = read_lds(get_at + u * M * 64 + r * 2048 + ((h * 2 + grp) ^ get_xor) * 16);
-                    if (any_moved) {
-                        const float f = h == 0 ? ref0[r] : ref1[r];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) w[r][i] = pack_bf16(bf_lo(w[r][i]) * f, bf_hi(w[r][i]) * f);
-                    }
-                }
-#pragma unroll
-                for (int b = 0; b < COLS; ++b) {
-                    // block0 is even wherever there is more than one block
-                    const int odd = COLS > 1 ? b & 1 : block0 & 1;
-                    const uint32_t at = buf * STEP + u * T::kBytes + ((block0 + b) >> 1) * 4096 + h * 2048;
-                    const u32x4 v = join(read_transposed((odd ? value_at[1][0] : value_at[0][0]) + at), read_transposed((odd ? value_at[1][1] : value_at[0][1]) + at));
-#pragma unroll
-                    for (int r = 0; r < ROW_TILES; ++r) acc[b][r] = mfma32(v, w[r], acc[b][r]);
-                }
+                for (int r = 0; r < ROW_TILES; ++r) p[h][r] = read_lds(get_at + u * M * 64 + r * 2048 + ((h * 2 + grp) ^ get_xor) * 16);
             }
+            const int odd = COLS > 1 ? b & 1 : block0 & 1;  // block0 is even wherever there is more than one block
+            const uint32_t at = buf * STEP + u * T::kBytes + ((block0 + b) >> 1) * 4096 + h * 2048;
+            v[n % AHEAD] = join(read_transposed((odd ? value_at[1][0] : value_at[0][0]) + at), read_transposed((odd ? value_at[1][1] : value_at[0][1]) + at));
+        };
+#pragma unroll
+        for (int n = 0; n < AHEAD - 1; ++n) fetch(n);
+#pragma unroll
+        for (int n = 0; n < ITEMS; ++n) {
+            if (n + AHEAD - 1 < ITEMS) fetch(n + AHEAD - 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int r = 0; r < ROW_TILES; ++r) acc[n % COLS][r] = mfma32(v[n % AHEAD], p[n / COLS & 1][r], acc[n % COLS][r]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
@@ -288,14 +306,13 @@ int64_t up256(int64_t v) { return (v + 255) & ~(int64_t)255; }
 // Tiles of 32 rows of a workgroup that has `rows` of them to share.
 int wide(int64_t rows) { return rows <= 32 ? 1 : 2; }
 
-// Ranges of `most` slots for `groups` workgroups each.
-void split(int64_t most, int64_t groups, int* per, int* ranges) {
-    int64_t n = groups > 0 ? (512 + groups - 1) / groups : 1;
-    const int64_t least = 256;
-    if (n > (most + least - 1) / least) n = (most + least - 1) / least;
-    if (n < 1) n = 1;
-    int64_t p = ((most + n - 1) / n + 127) / 128 * 128;
-    if (p < 128) p = 128;
+// Ranges of `most` slots for `groups` workgroups each, of `mt` tiles of 32 rows.  About as many workgroups as run at once, 512 or 256, of 256 slots
+// and more, since each costs its start, its end and its sums written and read: 512 sequences of 513 slots in one range 74 us, in two 86;
+// 48 of up to 6001 with 128 heads in ranges of 2048 143, of 1024 162, of 512 184.  Compute units that would stand idle are worth ranges of
+// one step of two tiles, though: 1 sequence of 701 slots in ranges of 256 20 us, of 128 15, of 64 12.5.
+void split(int64_t most, int64_t groups, int mt, int* per, int* ranges) {
+    const int64_t busy = min(((mt == 1 ? 512 : 256) + groups - 1) / groups, (most + 255) / 256), idle = min(256 / groups, (most + 63) / 64);
+    const int64_t n = max(max(busy, idle), (int64_t)1), p = ((most + n - 1) / n + 63) / 64 * 64;
     *per = (int)p;
     *ranges = (int)(most > p ? (most + p - 1) / p : 1);
 }
@@ -316,14 +333,14 @@ Plan plan(const Cache& c, const Step& s, const Heads& h) {
     const int64_t rows = (int64_t)s.max_new * h.n, all = (int64_t)s.n_rows * h.n;
     p.own_mt = wide(rows);
     p.own_tiles = (int)((rows + p.own_mt * 32 - 1) / (p.own_mt * 32));
-    split(most, (int64_t)c.n_seq * p.own_tiles, &p.parts.per, &p.own_ranges);
+    split(most, (int64_t)c.n_seq * p.own_tiles, p.own_mt, &p.parts.per, &p.own_ranges);
     p.own_groups = (int64_t)c.n_seq * p.own_tiles * p.own_ranges;
     p.parts.own = p.parts.all = p.own_ranges;
     p.parts.pre_per = 1;
     if (c.prefix_len > 0) {
         p.pre_mt = wide(all);
         p.pre_tiles = (int)((all + p.pre_mt * 32 - 1) / (p.pre_mt * 32));
-        split(c.prefix_len, p.pre_tiles, &p.parts.pre_per, &p.pre_ranges);
+        split(c.prefix_len, p.pre_tiles, p.pre_mt, &p.parts.pre_per, &p.pre_ranges);
         p.pre_groups = (int64_t)p.pre_tiles * p.pre_ranges;
         p.parts.all += p.pre_ranges;
     }
@@ -340,8 +357,15 @@ Plan plan(const Cache& c, const Step& s, const Heads& h) {
 template <int DC, int DR, bool PREFIX>
 void launch_run(hipStream_t st, const Cache& c, const Step& s, const Run& run, int mt, int64_t groups) {
     const dim3 grid((unsigned)groups);
-    if (mt == 1) hipLaunchKernelGGL((absorbed_kernel<DC, DR, 1, PREFIX>), grid, dim3(256), 0, st, c, s, run);
-    if (mt == 2) hipLaunchKernelGGL((absorbed_kernel<DC, DR, 2, PREFIX>), grid, dim3(512), 0, st, c, s, run);
+    if (mt == 2) {
+        hipLaunchKernelGGL((absorbed_kernel<DC, DR, 2, PREFIX, false>), grid, dim3(512), 0, st, c, s, run);
+        return;
+    }
+    // Caches beyond the last-level cache of 256 MiB, read once by every call, are read past it: 512 sequences of 513 slots (302 MB) 74 us with ordinary
+    // copies, 66 so.
+    const int64_t bytes = (int64_t)c.n_seq * min((int64_t)s.max_cached + s.max_new, (int64_t)c.max_len) * (DC + DR) * 2;
+    if (!PREFIX && run.row_tiles == 1 && bytes > (int64_t)256 << 20) hipLaunchKernelGGL((absorbed_kernel<DC, DR, 1, false, true>), grid, dim3(256), 0, st, c, s, run);
+    else hipLaunchKernelGGL((absorbed_kernel<DC, DR, 1, PREFIX, false>), grid, dim3(256), 0, st, c, s, run);
 }
 
 template <int DC, int DR>

@@ -11,8 +11,11 @@ __device__ __forceinline__ uint32_t lds_address(T* p) {
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) T*)p;
 }
 __device__ __forceinline__ u32x4 read_lds(uint32_t at) { return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)at; }
-__device__ __forceinline__ void write_lds(uint32_t at, const u32x4 v) { *(__attribute__((address_space(3))) u32x4*)(uintptr_t)at = v; }
+__device__ __forceinline__ uint32_t read_lds_word(uint32_t at) { return *(__attribute__((address_space(3))) const uint32_t*)(uintptr_t)at; }
+__device__ __forceinline__ void write_lds_word(uint32_t at, uint32_t v) { *(__attribute__((address_space(3))) uint32_t*)(uintptr_t)at = v; }
 __device__ __forceinline__ void write_lds2(uint32_t at, const u32x2 v) { *(__attribute__((address_space(3))) u32x2*)(uintptr_t)at = v; }
+// LDS accesses of a wavefront before it are done before those behind it: they run in order, the compiler has to keep them so.
+__device__ __forceinline__ void wave_sync() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 // Four rows of 16 elements of 16 bits, transposed: lane l of 16 points at four elements of row l / 4, 4 * (l % 4) on, and gets element l
 // of the four rows.
 __device__ __forceinline__ u32x2 read_transposed(uint32_t at) {
@@ -20,9 +23,14 @@ __device__ __forceinline__ u32x2 read_transposed(uint32_t at) {
 }
 __device__ __forceinline__ u32x4 join(const u32x2 a, const u32x2 b) { return u32x4{a.x, a.y, b.x, b.y}; }
 
-// Where the eight 16-byte units of a slot's 128 bytes lie in LDS: unit u at place u ^ twist(slot).  Slots side by side then differ in
-// their bank for reads of one unit each, and for transposed ones of four units each.
-__device__ __forceinline__ int twist(int slot) { return (slot >> 1 & 1) << 2 | (slot >> 2 & 3); }
+// Where the eight 16-byte units of a slot's 128 bytes lie in LDS: unit u at place u ^ twist(slot).  A read of 16 bytes a lane takes lanes
+// 0-3, 12-15, 20-23 and 24-27 together, then the others of 32: by the slot's bits 0 and 1 (half of the banks, and their half) and the
+// permutation 0, 2, 3, 1 of bits 2 and 3 none of them meet, whether lanes 16-31 read the same unit of other slots or the next one of the
+// same; and neither do transposed reads, of four units of four slots each.
+__device__ __forceinline__ int twist(int slot) {
+    const int q = slot >> 2 & 3;
+    return (slot >> 1 & 1) << 2 | ((q ^ q >> 1) & 1) << 1 | q >> 1;
+}
 
 // Sums, cut into parts: a row's slots into ranges of `per`, the prefix into ranges of its own, behind them.
 struct Parts {

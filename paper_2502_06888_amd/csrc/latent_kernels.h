@@ -81,4 +81,22 @@ __device__ __forceinline__ int seq_of_row(const Cache& c, const Step& s, int row
     return *token >= 0 && *token < q->n_new ? lo : -1;
 }
 
+// The same for a row of every lane.
+__device__ __forceinline__ int lane_seq_of_row(const Cache& c, const Step& s, int row, int* token, Seq* q) {
+    int lo = 0;
+    if (s.row_offsets == nullptr) {
+        lo = row / s.max_new;
+    } else {
+        int hi = c.n_seq - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (s.row_offsets[mid] <= row) lo = mid;
+            else hi = mid - 1;
+        }
+    }
+    *q = kkv8::sequence(c.max_len, s, lo);
+    *token = row - q->row0;
+    return *token >= 0 && *token < q->n_new ? lo : -1;
+}
+
 }  // namespace klat
