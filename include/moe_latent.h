@@ -63,7 +63,7 @@ typedef struct {
 moe_status moe_latent_append(void* stream, const moe_latent_cache* cache, const moe_kv8_step* step, const void* x,
                              int64_t x_row_stride, const void* norm, float eps, const moe_rope_config* rope);
 
-/* How moe_latent_attend computes: MOE_LATENT_AUTO takes the form with fewer operations by the step's bounds. */
+/* How moe_latent_attend computes: MOE_LATENT_AUTO takes the form that should be the faster one by the step's bounds. */
 typedef enum { MOE_LATENT_AUTO = 0, MOE_LATENT_ABSORBED = 1, MOE_LATENT_EXPANDED = 2 } moe_latent_form;
 
 /*
@@ -73,9 +73,10 @@ typedef enum { MOE_LATENT_AUTO = 0, MOE_LATENT_ABSORBED = 1, MOE_LATENT_EXPANDED
  *     turned already (moe_rope_rotate with first = nope_dim); out: likewise, v_dim elements.  16-byte aligned, strides multiples of 8;
  *     no two (row, head) of out share an element, and q and out share none.
  *   softmax_scale: 0 stands for 1 / sqrt(nope_dim + rope_dim).
- * Rows of no sequence are left as they were.  Scores, the softmax's statistics and sums are kept in 32 bits.  Rounded to bf16
- * on the way: the softmax weights, in the absorbed form a and u (each as two of them, with 16 bits together), in the expanded one keys and values,
- * finite ones to finite ones.  A latent that is not finite reaches the rows that see it, all their elements, and no others.
+ * Rows of no sequence are left as they were.  Scores, the softmax's statistics and sums are kept in 32 bits.  Rounded on
+ * the way: in the absorbed form the softmax weights to bf16, a and u to two bf16 (16 bits together); in the expanded one the softmax
+ * weights, keys, values and the queries' nope_dim elements to fp16 times a power of two, finite ones to finite ones.  A latent that is
+ * not finite reaches the rows that see it, all their elements, and no others.
  * The result of a sequence does not depend on what the others hold; how its sums are split follows from the numbers in the structs and
  * its own length.
  * workspace: moe_latent_attend_workspace_bytes() of device memory, 256-byte aligned; it depends on sizes and bounds only.

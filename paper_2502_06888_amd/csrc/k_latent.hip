@@ -343,7 +343,7 @@ namespace {
 template <int DC, int DV>
 void launch_finish_sizes(hipStream_t st, const Cache& c, const Step& s, const Heads& h, const RowsOut& out, const Parts& parts) {
     const dim3 grid((unsigned)finish_groups(h, s.n_rows)), block(512);
-    if (s.n_rows <= 4) hipLaunchKernelGGL((finish_kernel<DC, DV, true>), grid, block, 0, st, c, s, h, out, parts);
+    if (s.n_rows <= kFewRows) hipLaunchKernelGGL((finish_kernel<DC, DV, true>), grid, block, 0, st, c, s, h, out, parts);
     else hipLaunchKernelGGL((finish_kernel<DC, DV, false>), grid, block, 0, st, c, s, h, out, parts);
 }
 template <int DC>

@@ -309,10 +309,15 @@ int wide(int64_t rows) { return rows <= 32 ? 1 : 2; }
 // Ranges of `most` slots for `groups` workgroups each, of `mt` tiles of 32 rows.  About as many workgroups as run at once, 512 or 256, of 256 slots
 // and more, since each costs its start, its end and its sums written and read: 512 sequences of 513 slots in one range 74 us, in two 86;
 // 48 of up to 6001 with 128 heads in ranges of 2048 143, of 1024 162, of 512 184.  Compute units that would stand idle are worth ranges of
-// one step of two tiles, though: 1 sequence of 701 slots in ranges of 256 20 us, of 128 15, of 64 12.5.
-void split(int64_t most, int64_t groups, int mt, int* per, int* ranges) {
+// one step of two tiles, though: 1 sequence of 701 slots in ranges of 256 20 us, of 128 15, of 64 12.5.  Where finish_kernel has a row's parts
+// added by one wavefront, a part costs it half as long as 32 slots cost here, so that together they are least at sqrt(slots / 16) parts: the whole
+// call for 5 sequences of 30000 slots and 8 heads, in 103 parts 83 us, in 43 68; of 2000, in 32 parts 35, in 11 32.
+void split(int64_t most, int64_t groups, int mt, bool few, int* per, int* ranges) {
     const int64_t busy = min(((mt == 1 ? 512 : 256) + groups - 1) / groups, (most + 255) / 256), idle = min(256 / groups, (most + 63) / 64);
-    const int64_t n = max(max(busy, idle), (int64_t)1), p = ((most + n - 1) / n + 63) / 64 * 64;
+    int64_t n = max(max(busy, idle), (int64_t)1);
+    if (!few)
+        while (n > 4 && n * n > most / 16) --n;
+    const int64_t p = ((most + n - 1) / n + 63) / 64 * 64;
     *per = (int)p;
     *ranges = (int)(most > p ? (most + p - 1) / p : 1);
 }
@@ -333,14 +338,14 @@ Plan plan(const Cache& c, const Step& s, const Heads& h) {
     const int64_t rows = (int64_t)s.max_new * h.n, all = (int64_t)s.n_rows * h.n;
     p.own_mt = wide(rows);
     p.own_tiles = (int)((rows + p.own_mt * 32 - 1) / (p.own_mt * 32));
-    split(most, (int64_t)c.n_seq * p.own_tiles, p.own_mt, &p.parts.per, &p.own_ranges);
+    split(most, (int64_t)c.n_seq * p.own_tiles, p.own_mt, s.n_rows <= kFewRows, &p.parts.per, &p.own_ranges);
     p.own_groups = (int64_t)c.n_seq * p.own_tiles * p.own_ranges;
     p.parts.own = p.parts.all = p.own_ranges;
     p.parts.pre_per = 1;
     if (c.prefix_len > 0) {
         p.pre_mt = wide(all);
         p.pre_tiles = (int)((all + p.pre_mt * 32 - 1) / (p.pre_mt * 32));
-        split(c.prefix_len, p.pre_tiles, p.pre_mt, &p.parts.pre_per, &p.pre_ranges);
+        split(c.prefix_len, p.pre_tiles, p.pre_mt, s.n_rows <= kFewRows, &p.parts.pre_per, &p.pre_ranges);
         p.pre_groups = (int64_t)p.pre_tiles * p.pre_ranges;
         p.parts.all += p.pre_ranges;
     }

@@ -115,6 +115,8 @@ def append(cache: LatentCache, step: Kv8Step, x, norm=None, eps: float = 1e-6, r
 
 
 def attend_workspace_bytes(cache: LatentCache, step: Kv8Step, heads: LatentHeads, form: str = "auto") -> int:
+    if form not in FORMS:
+        _refuse(f"form must be one of {', '.join(FORMS)}")
     n = C.c_int64(0)
     _check(load_library().moe_latent_attend_workspace_bytes(cache.ref, step.ref, heads.ref, FORMS[form], C.byref(n)))
     return int(n.value)

@@ -475,5 +475,9 @@ def test_a_run_of_rotation_append_and_attention_as_a_model_makes_it():
 
 
 def used(cache, step, heads, form):
-    """The form that a call takes, as far as its bounds are concerned: the wider ones for auto."""
-    return ABSORBED if form == "auto" else form
+    """The form that a call takes, by what it asks of memory."""
+    if form != "auto":
+        return form
+    need = {f: L.attend_workspace_bytes(cache, step, heads, f) for f in ("auto", ABSORBED, EXPANDED)}
+    assert need[ABSORBED] != need[EXPANDED]
+    return ABSORBED if need["auto"] == need[ABSORBED] else EXPANDED
