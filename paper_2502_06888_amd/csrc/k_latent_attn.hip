@@ -21,10 +21,57 @@ struct Run {  // one launch
     int H, row_tiles;  // tiles of 32 * MT rows of a sequence (of the prefix: of all)
     int per, ranges;   // slots of a range, ranges at most
     int part0;         // where the launch's parts are among a row's
+    bool packed;       // see place_of
     float qscale;
     const uint16_t* a;  // [row, head, 2 * latent + rope], see absorb_kernel
     Parts parts;
 };
+
+struct Place {
+    int seq, tile, range;
+};
+
+// Work of a workgroup among what the sequences have of it: whole ranges, then last ones of half a range and more, then the shorter ones, so that the
+// long ones start first and every XCD gets as many.  Laid out by the bounds, where a workgroup of a short sequence finds nothing to do, one XCD has
+// more than its compute units take at once and another none: 48 sequences of 80 to 6001 slots, 128 heads 143 us so
+// (and in three ranges, see split), 121 packed.
+template <int M>
+__device__ __forceinline__ bool place_of(const Cache& c, const Step& s, const Run& run, Place* at) {
+    const int lane = threadIdx.x & 63;
+    int left = blockIdx.x;
+    // two tiles of a range to one XCD, which then reads its slots once
+    if (run.row_tiles > 1 && (left | 15) < (int)gridDim.x) left = (left & ~15) + (left & 7) * 2 + (left >> 3 & 1);
+    for (int kind = 0; kind < 3; ++kind)
+        for (int first = 0; first < c.n_seq; first += 64) {
+            int tiles = 0, full = 0, here = 0;
+            if (first + lane < c.n_seq) {
+                const Seq q = kkv8::sequence(c.max_len, s, first + lane);
+                if (q.n_new > 0) {
+                    tiles = (q.n_new * run.H + M - 1) / M;
+                    full = (q.cached + q.n_new) / run.per;
+                    const int rest = q.cached + q.n_new - full * run.per;
+                    here = kind == 0 ? tiles * full : rest > 0 && (2 * rest >= run.per) == (kind == 1) ? tiles : 0;
+                }
+            }
+            int upto = here;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int y = __shfl_up(upto, d, 64);
+                if (lane >= d) upto += y;
+            }
+            const uint64_t has = __ballot(upto > left);
+            if (has != 0) {
+                const int who = __builtin_ctzll(has);
+                const int in = left - __builtin_amdgcn_readlane(upto - here, who), n = __builtin_amdgcn_readlane(tiles, who);
+                at->seq = first + who;
+                at->tile = n - 1 - in % n;  // those that see the most slots first
+                at->range = kind == 0 ? in / n : __builtin_amdgcn_readlane(full, who);
+                return true;
+            }
+            left -= __builtin_amdgcn_readlane(upto, 63);
+        }
+    return false;
+}
 
 // A workgroup of 4 * MT wavefronts takes 32 * MT rows of A and a range of slots, SUB tiles at a time (a step; the next one comes
 // meanwhile, without registers):
@@ -50,14 +97,17 @@ __global__ __launch_bounds__(256 * MT, 2) void absorbed_kernel(Cache c, Step s, 
     __shared__ float sm_ref[2][M], sm_sum[2][M];
     const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, grp = lane >> 5, c16 = lane & 15, g16 = lane >> 4;
     const int rows16 = wave % GROUPS, half = wave / GROUPS;
-    // of a sequence the row tiles one behind the other, so that they read its slots together; of the prefix the ranges, each to its XCD
-    int seq = 0, range = blockIdx.x % run.ranges, tile = run.row_tiles - 1 - (int)blockIdx.x / run.ranges;
+    // of the prefix the ranges, each to its XCD; of a sequence the row tiles one behind the other, so that they read its slots together
+    Place at{0, run.row_tiles - 1 - (int)blockIdx.x / run.ranges, (int)blockIdx.x % run.ranges};
     if (!PREFIX) {
-        seq = blockIdx.x % c.n_seq;
-        const int rest = blockIdx.x / c.n_seq;
-        tile = run.row_tiles - 1 - rest % run.row_tiles;  // those that see the most slots first
-        range = rest / run.row_tiles;
+        if (run.packed) {
+            if (!place_of<M>(c, s, run, &at)) return;
+        } else {
+            const int rest = blockIdx.x / c.n_seq;
+            at = Place{(int)blockIdx.x % c.n_seq, run.row_tiles - 1 - rest % run.row_tiles, rest / run.row_tiles};
+        }
     }
+    const int seq = __builtin_amdgcn_readfirstlane(at.seq), tile = __builtin_amdgcn_readfirstlane(at.tile), range = __builtin_amdgcn_readfirstlane(at.range);
     Seq q;
     if (PREFIX) q = Seq{0, s.n_rows, 0};
     else q = kkv8::sequence(c.max_len, s, seq);
@@ -306,20 +356,30 @@ int64_t up256(int64_t v) { return (v + 255) & ~(int64_t)255; }
 // Tiles of 32 rows of a workgroup that has `rows` of them to share.
 int wide(int64_t rows) { return rows <= 32 ? 1 : 2; }
 
-// Ranges of `most` slots for `groups` workgroups each, of `mt` tiles of 32 rows.  About as many workgroups as run at once, 512 or 256, of 256 slots
-// and more, since each costs its start, its end and its sums written and read: 512 sequences of 513 slots in one range 74 us, in two 86;
-// 48 of up to 6001 with 128 heads in ranges of 2048 143, of 1024 162, of 512 184.  Compute units that would stand idle are worth ranges of
-// one step of two tiles, though: 1 sequence of 701 slots in ranges of 256 20 us, of 128 15, of 64 12.5.  Where finish_kernel has a row's parts
-// added by one wavefront, a part costs it half as long as 32 slots cost here, so that together they are least at sqrt(slots / 16) parts: the whole
-// call for 5 sequences of 30000 slots and 8 heads, in 103 parts 83 us, in 43 68; of 2000, in 32 parts 35, in 11 32.
+// Ranges of `most` slots for `groups` workgroups each, of `mt` tiles of 32 rows: as many as take least, in slots of one workgroup alone: a round of
+// workgroups takes its range and 150 slots for its start and its end, a third more where two share a compute unit; a part costs finish_kernel
+// 16 where one wavefront adds a row's, 2 where eight do.  Whole calls with every sequence as long as its bound: 48 of 8000 slots, 128 heads, in three
+// ranges (288 workgroups for 256 compute units) 329 us, in eight 262; of 30000, 8 heads, in 11 (528 for 512 places) 365, in ten 275; 5 of 30000 in 103 83, in 43
+// 68; 1 of 701 in three ranges 20 us of attention, in eleven 12.5.
 void split(int64_t most, int64_t groups, int mt, bool few, int* per, int* ranges) {
-    const int64_t busy = min(((mt == 1 ? 512 : 256) + groups - 1) / groups, (most + 255) / 256), idle = min(256 / groups, (most + 63) / 64);
-    int64_t n = max(max(busy, idle), (int64_t)1);
-    if (!few)
-        while (n > 4 && n * n > most / 16) --n;
-    const int64_t p = ((most + n - 1) / n + 63) / 64 * 64;
-    *per = (int)p;
-    *ranges = (int)(most > p ? (most + p - 1) / p : 1);
+    const int64_t limit = min((most + 63) / 64, (int64_t)256);
+    float least = 0.f;
+    *per = (int)((most + 63) / 64 * 64);
+    *ranges = 1;
+    for (int64_t n = 1; n <= limit; ++n) {
+        const float parts = (few ? 2.f : 16.f) * (float)n;
+        if (n > 1 && parts >= least) break;
+        const int64_t p = ((most + n - 1) / n + 63) / 64 * 64, r = (most + p - 1) / p;
+        if (r != n) continue;
+        const int64_t wgs = groups * n;
+        const float rounds = mt == 2 || wgs <= 256 ? (float)((wgs + 255) / 256) : 1.33f * (float)((wgs + 511) / 512);
+        const float cost = rounds * ((float)p + 150.f) + parts;
+        if (n == 1 || cost < least) {
+            least = cost;
+            *per = (int)p;
+            *ranges = (int)n;
+        }
+    }
 }
 
 // How a step is run, from its sizes and bounds.
@@ -386,6 +446,7 @@ void launch_sizes(hipStream_t st, const Cache& c, const Step& s, const Plan& p, 
     run.per = p.parts.per;
     run.ranges = p.own_ranges;
     run.part0 = 0;
+    run.packed = p.own_ranges > 1 && c.n_seq <= 256;
     launch_run<DC, DR, false>(st, c, s, run, p.own_mt, p.own_groups);
 }
 
