@@ -141,12 +141,12 @@ __global__ __launch_bounds__(64 * WAVES) void absorb_kernel(Cache c, Heads h, Ro
     }
 }
 
-// o = w_v u / sum for 32 rows of one head: the parts of a row's sums are brought to the largest reference and added (a wavefront
-// per row; FEW: all eight share a row), the result goes into LDS as two bf16 (value and what rounding it left over) in the
+// o = w_v u / sum for up to 32 rows of one head: the parts of a row's sums are brought to the largest reference and added (a wavefront
+// per row; FEW: one row, which all eight share), the result goes into LDS as two bf16 (value and what rounding it left over) in the
 // order of the matrix instructions, and the wavefronts take 32 of the value's elements and a share of the latents each, which then meet
 // in LDS.  w_v is asked for before the parts are read.  Bound by latency where there are few rows, then by the parts' bytes.
 template <int DC, int DV, bool FEW>
-__global__ __launch_bounds__(512, FEW ? 2 : 4) void finish_kernel(Cache c, Step s, Heads h, RowsOut out, Parts parts) {
+__global__ __launch_bounds__(512, FEW ? 2 : 4) void finish_kernel(Cache c, Step s, Heads h, RowsOut out, Parts parts, int span) {
     constexpr int BLOCKS = DV / 32, SHARES = 8 / BLOCKS, F = DC / 16 / SHARES, Q = DC / 4 > 64 ? DC / 256 : 1;  // pieces of four elements that a lane has
     __shared__ u32x4 u[2][DC / 8 * 32];
     __shared__ int own_parts[32];                    // of a row's slots; 0: no row
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(512, FEW ? 2 : 4) void finish_kernel(Cache c, Step 
     constexpr bool FITS = sizeof u >= 8 * 4096 + 32 * DV * 2;  // the shares of the product and the rows that leave
     __shared__ f32x4 shares_apart[FITS ? 1 : 8 * 256 + 32 * DV / 8];
     const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, grp = lane >> 5;
-    const int head = blockIdx.x % h.n, row0 = blockIdx.x / h.n * 32, rows = min(32, s.n_rows - row0);
+    const int head = blockIdx.x % h.n, row0 = blockIdx.x / h.n * span, rows = min(span, s.n_rows - row0);
     if (threadIdx.x < 32) {
         int own = 0;
         if ((int)threadIdx.x < rows) {
@@ -172,10 +172,10 @@ __global__ __launch_bounds__(512, FEW ? 2 : 4) void finish_kernel(Cache c, Step 
         for (int f = 0; f < F; ++f) wf[f] = *(const u32x4*)(p + f * 16);
     }
     __syncthreads();
-    // FEW: one row after the other; else the wavefront's four rows two by two, so that their reads are on the way together
+    // the wavefront's rows two by two, so that their reads are on the way together
     constexpr int R = FEW ? 1 : 2;
-    for (int i0 = 0; i0 < (FEW ? rows : 4 / R); ++i0) {
-        const auto row_of_wave = [&](int r) { return FEW ? i0 : wave + 8 * (R * i0 + r); };
+    for (int i0 = 0; i0 < (FEW ? 1 : (span + 8 * R - 1) / (8 * R)); ++i0) {
+        const auto row_of_wave = [&](int r) { return FEW ? 0 : wave + 8 * (R * i0 + r); };
         int own[R], n[R], most = 0;
         int64_t item[R];
         float ref[R], sum[R];
@@ -337,14 +337,31 @@ void launch_absorb(hipStream_t st, const Cache& c, const Heads& h, const Rows& q
     if (h.nope == 128) launch_absorb_nope<128>(st, c, h, q, n_rows, out);
 }
 
-int64_t finish_groups(const Heads& h, int n_rows) { return (int64_t)h.n * ((n_rows + 31) / 32); }
+// Up to one row and head per compute unit.  1 sequence of 30000 slots with 8 heads, whole call: a wavefront for a row 64 us, all eight 37; 8 of 4000 with
+// 32 heads 42 and 34; with 512 rows and heads they are slower, 16 of 700 with 32 heads 33 and 40.
+bool finish_few(const Heads& h, int n_rows) { return (int64_t)h.n * n_rows <= 256; }
+
+// Rows of a workgroup: 32 of them share w_v, fewer where compute units would be left alone (64 rows of 32 heads in 9 to 16 parts: 64 workgroups 24
+// us, 256 of eight rows 15; 48 rows of 128 heads: 256 workgroups 17 us, 768 of eight rows 24).
+static int finish_span(const Heads& h, int n_rows) {
+    if (finish_few(h, n_rows)) return 1;
+    int span = 32;
+    while (span > 8 && (int64_t)h.n * ((n_rows + span - 1) / span) < 256) span /= 2;
+    return span;
+}
+
+int64_t finish_groups(const Heads& h, int n_rows) {
+    const int span = finish_span(h, n_rows);
+    return (int64_t)h.n * ((n_rows + span - 1) / span);
+}
 
 namespace {
 template <int DC, int DV>
 void launch_finish_sizes(hipStream_t st, const Cache& c, const Step& s, const Heads& h, const RowsOut& out, const Parts& parts) {
+    const int span = finish_span(h, s.n_rows);
     const dim3 grid((unsigned)finish_groups(h, s.n_rows)), block(512);
-    if (s.n_rows <= kFewRows) hipLaunchKernelGGL((finish_kernel<DC, DV, true>), grid, block, 0, st, c, s, h, out, parts);
-    else hipLaunchKernelGGL((finish_kernel<DC, DV, false>), grid, block, 0, st, c, s, h, out, parts);
+    if (finish_few(h, s.n_rows)) hipLaunchKernelGGL((finish_kernel<DC, DV, true>), grid, block, 0, st, c, s, h, out, parts, span);
+    else hipLaunchKernelGGL((finish_kernel<DC, DV, false>), grid, block, 0, st, c, s, h, out, parts, span);
 }
 template <int DC>
 void launch_finish_latent(hipStream_t st, const Cache& c, const Step& s, const Heads& h, const RowsOut& out, const Parts& parts) {

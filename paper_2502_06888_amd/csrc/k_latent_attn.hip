@@ -398,14 +398,14 @@ Plan plan(const Cache& c, const Step& s, const Heads& h) {
     const int64_t rows = (int64_t)s.max_new * h.n, all = (int64_t)s.n_rows * h.n;
     p.own_mt = wide(rows);
     p.own_tiles = (int)((rows + p.own_mt * 32 - 1) / (p.own_mt * 32));
-    split(most, (int64_t)c.n_seq * p.own_tiles, p.own_mt, s.n_rows <= kFewRows, &p.parts.per, &p.own_ranges);
+    split(most, (int64_t)c.n_seq * p.own_tiles, p.own_mt, finish_few(h, s.n_rows), &p.parts.per, &p.own_ranges);
     p.own_groups = (int64_t)c.n_seq * p.own_tiles * p.own_ranges;
     p.parts.own = p.parts.all = p.own_ranges;
     p.parts.pre_per = 1;
     if (c.prefix_len > 0) {
         p.pre_mt = wide(all);
         p.pre_tiles = (int)((all + p.pre_mt * 32 - 1) / (p.pre_mt * 32));
-        split(c.prefix_len, p.pre_tiles, p.pre_mt, s.n_rows <= kFewRows, &p.parts.pre_per, &p.pre_ranges);
+        split(c.prefix_len, p.pre_tiles, p.pre_mt, finish_few(h, s.n_rows), &p.parts.pre_per, &p.pre_ranges);
         p.pre_groups = (int64_t)p.pre_tiles * p.pre_ranges;
         p.parts.all += p.pre_ranges;
     }

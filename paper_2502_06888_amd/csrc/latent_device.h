@@ -40,9 +40,8 @@ struct Parts {
     float2* ml;        // [row, head, part] reference, sum of weights
 };
 
-// Rows of a step up to which finish_kernel has all wavefronts of a workgroup share a row's parts.
-constexpr int kFewRows = 4;
-
+// Whether finish_kernel has all wavefronts of a workgroup share a row's parts.
+bool finish_few(const Heads& h, int n_rows);
 int64_t absorb_groups(const Cache& c, const Heads& h, int n_rows);
 void launch_absorb(hipStream_t st, const Cache& c, const Heads& h, const Rows& q, int n_rows, uint16_t* out);
 int64_t finish_groups(const Heads& h, int n_rows);

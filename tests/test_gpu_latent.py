@@ -145,6 +145,19 @@ def test_bounds_wider_than_the_lengths_and_strides(case, form):
 
 
 @pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("heads,dims,n_seq,longest,every", [(8, (128, 32, 32, 32), 70, 900, 3), (40, SMALL, 131, 700, 4), (128, WIDE, 9, 1500, 2),
+                                                            (4, (128, 32, 32, 32), 300, 1990, 60)])
+def test_many_sequences_of_uneven_lengths(heads, dims, n_seq, longest, every, form):
+    """Work of sequences with none, one or many ranges, whole or not, with none to three tokens."""
+    g = torch.Generator().manual_seed(n_seq)
+    cached = [int(torch.randint(0, longest if i % every == 1 else 60, (1,), generator=g)) for i in range(n_seq)]
+    cached[every + 1], cached[-1] = longest, 0
+    new = [i % 4 if every < 10 else 1 for i in range(n_seq)]
+    x = Layer(90 + n_seq, cached, new, heads, dims)
+    check(x.run(form), form, x.reference())
+
+
+@pytest.mark.parametrize("form", FORMS)
 def test_steps_without_offsets_scales_and_heads_of_one_matrix(form):
     x = Layer(50, [40, 7, 300], [2, 2, 2], 20, WIDE, prefix=33, uniform=True, tail=0)
     both = torch.cat((x.w_k, x.w_v), 1).to(DEV)                               # [heads, nope + value, latent]
