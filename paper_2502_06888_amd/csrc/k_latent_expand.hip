@@ -48,7 +48,7 @@ struct Sizes {
     static constexpr int kBytes = (kTile + kPe) * 16;
 };
 
-// Slots that the step's tokens see, and which tile of 128 of them: the launch's sequences, or the prefix.
+// Slots that the step's tokens see: of a sequence, or of the prefix.
 template <bool PREFIX>
 __device__ __forceinline__ int slots_of(const Cache& c, const Step& s, int seq) {
     if (PREFIX) return c.prefix_len;
@@ -58,7 +58,7 @@ __device__ __forceinline__ int slots_of(const Cache& c, const Step& s, int seq) 
 
 // w_k and w_v in the order in which expand_kernel's matrix instructions take them: [head][32 rows][16 latents][lane], 16 bytes a lane.  Read
 // where they lie, a wavefront's rows are 32 lines of which it uses 32 bytes at a time: expand_kernel then waits for L2 (8192 slots of 32
-// heads 120 us, with this copy and its 4 us LATER).  One workgroup per 32 rows.
+// heads 152 us, from this copy 87 and 5 for the copy).  One workgroup per 32 rows.
 __global__ __launch_bounds__(256) void order_kernel(Heads h, int latent, u32x4* out) {
     const int lane = threadIdx.x & 63, blocks = (h.nope + h.v) / 32, head = blockIdx.x / blocks, block = blockIdx.x % blocks;
     const bool key = block < h.nope / 32;
