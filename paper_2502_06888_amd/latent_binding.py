@@ -81,6 +81,8 @@ def _weights(w, name: str, latent: int):
     import torch
     if w.dtype != torch.bfloat16 or w.dim() != 3 or w.shape[2] != latent or w.stride(2) != 1 or w.stride(1) != latent:
         _refuse(f"{name} must be a bf16 tensor [n_heads, rows, latent] whose heads are contiguous")
+    if w.shape[0] > 1 and w.stride(0) == 0:
+        _refuse(f"the heads of {name} must be there one by one")
     return w.stride(0) if w.shape[0] > 1 else 0
 
 

@@ -147,6 +147,12 @@ def test_shapes_the_binding_refuses():
         L.append(c, s, torch.zeros((2, 576), dtype=torch.bfloat16), norm=torch.zeros(256, dtype=torch.bfloat16))
     with pytest.raises(B.MoeError):
         L.LatentHeads(torch.zeros((8, 128, 512), dtype=torch.bfloat16), torch.zeros((4, 128, 512), dtype=torch.bfloat16))
+    one = torch.zeros((1, 128, 512), dtype=torch.bfloat16)                    # a stride of 0 would stand for heads one behind the other
+    for w_k, w_v in ((one.expand(8, 128, 512), one.repeat(8, 1, 1)), (one.repeat(8, 1, 1), one.expand(8, 128, 512))):
+        with pytest.raises(B.MoeError):
+            L.LatentHeads(w_k, w_v)
+    with pytest.raises(B.MoeError):
+        L.attend_workspace_bytes(c, s, h, "none")
     with pytest.raises(B.MoeError):
         L.LatentCache(torch.zeros((2, 8, 576), dtype=torch.bfloat16), 64, prefix=torch.zeros((3, 512), dtype=torch.bfloat16))
     both = torch.zeros((8, 256, 512), dtype=torch.bfloat16)                   # w_k and w_v as parts of one matrix
