@@ -352,6 +352,36 @@ def test_another_stream_and_tensors_dropped_behind_the_call(form):
     assert torch.equal(out.cpu(), want)
 
 
+@pytest.mark.parametrize("form", FORMS)
+def test_graphs_that_share_a_workspace_and_calls_at_once(form):
+    """Two captured steps of other sizes over one workspace, replayed in turn; then both at once with a workspace each, guards behind."""
+    a, b = Layer(97, [700, 3, 90], [1, 1, 1], 128, WIDE), Layer(98, [40, 500], [30, 2], 8, SMALL, prefix=200)
+    want = [x.run(form) for x in (a, b)]
+    need = [L.attend_workspace_bytes(x.cache, x.step, x.h, form) for x in (a, b)]
+    shared = torch.full((max(need),), 0xff, dtype=torch.uint8, device=DEV)
+    q, out = [x.q.to(DEV) for x in (a, b)], [torch.full(w.shape, -7.0, dtype=torch.bfloat16, device=DEV) for w in want]
+    graphs = []
+    for i, x in enumerate((a, b)):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i]):
+            L.attend(x.cache, x.step, x.h, q[i], out[i], form=form, workspace=shared)
+    for i in (0, 1, 1, 0, 1, 0):
+        out[i].fill_(-7.0)
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[i].cpu(), want[i])
+        shared.fill_(0xff)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    own = [torch.full((n + 4096,), 0xa5, dtype=torch.uint8, device=DEV) for n in need]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for i, x in enumerate((a, b)):
+            L.attend(x.cache, x.step, x.h, q[i], out[i], form=form, workspace=own[i][:need[i]], stream=streams[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert torch.equal(out[i].cpu(), want[i]) and (own[i][need[i]:] == 0xa5).all()
+
+
 def test_refused_on_the_device():
     x = Layer(95, [5], [1], 8, SMALL, tail=0)
     q, out = x.q.to(DEV), torch.zeros((1, 8, 64), dtype=torch.bfloat16, device=DEV)
