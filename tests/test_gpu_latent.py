@@ -294,6 +294,13 @@ def test_many_slots_in_ranges_and_a_long_prefix(form):
     check(x.run(form), form, x.reference())
 
 
+@pytest.mark.parametrize("heads,prefix", [(130, 150), (251, 0)])
+def test_heads_in_sets_whose_last_one_is_smaller(heads, prefix):
+    """Bounds under which the keys and values of all heads do not fit the last-level cache."""
+    x = Layer(96, [100, 3, 700], [3, 1, 40], heads, WIDE, prefix=prefix, slack=(0, 1300), max_len=2100)
+    check(x.run(EXPANDED), EXPANDED, x.reference())
+
+
 @pytest.mark.parametrize("form", FORMS)
 def test_offsets_beyond_32_bits(form):
     """The last sequence of a cache of more than 2^32 elements."""
