@@ -31,14 +31,21 @@ __device__ __forceinline__ int shift_of(uint32_t largest) {
     return largest == 0 || (e >= -6 && e < 15) ? 0 : e - 8;
 }
 
-// One launch's view: heads head0 .. head0 + heads - 1 of the sequences, or of the prefix.
+// Keys and values of heads head0 .. head0 + heads - 1 of the sequences, or of the prefix.
 struct Made {
     int head0, heads, tiles;  // tiles of a sequence at most
+    int each;                 // heads that a workgroup makes
     u32x4* kv;                // [sequence, head, tile]: keys, then values, in the order of the matrix instructions
     u32x4* pe;                // [sequence, tile]: the part that carries the position
     int2* shift;              // [sequence, head, tile] exponents taken off the keys and the values
     const u32x4* w;           // w_k and w_v of all heads, see order_kernel
     int per, ranges, row_tiles, part0;
+};
+// One launch: the first `before` workgroups have the prefix, the others the sequences.  (One behind the other, the smaller launch leaves most
+// compute units alone: 5 prompts over a prefix of 8001 slots, 57 and 24 us of expand_kernel, 146 and 18 of expanded_kernel; in one 78 and 154.)
+struct Both {
+    Made pre, own;
+    int before;
 };
 
 template <int NOPE, int DV, int DR>
@@ -49,9 +56,8 @@ struct Sizes {
 };
 
 // Slots that the step's tokens see: of a sequence, or of the prefix.
-template <bool PREFIX>
-__device__ __forceinline__ int slots_of(const Cache& c, const Step& s, int seq) {
-    if (PREFIX) return c.prefix_len;
+__device__ __forceinline__ int slots_of(const Cache& c, const Step& s, bool prefix, int seq) {
+    if (prefix) return c.prefix_len;
     const Seq q = kkv8::sequence(c.max_len, s, seq);
     return q.n_new > 0 ? q.cached + q.n_new : 0;
 }
@@ -82,21 +88,23 @@ __global__ __launch_bounds__(256) void order_kernel(Heads h, int latent, u32x4* 
 constexpr int expand_waves(int nope, int v) { return (nope > v ? nope : v) / 32; }  // of 64 slots
 // Wavefronts of a SIMD: as many workgroups as the LDS holds.
 constexpr int expand_occupancy(int latent, int waves) { return waves * 2 * (latent == 512 ? 1 : latent == 256 ? 2 : 4) >= 8 ? 2 : 1; }
-template <int DC, int NOPE, int DV, bool PREFIX>
-__global__ __launch_bounds__(128 * expand_waves(NOPE, DV), expand_occupancy(DC, expand_waves(NOPE, DV))) void expand_kernel(Cache c, Step s, Heads h, Made m, int each) {
+template <int DC, int NOPE, int DV>
+__global__ __launch_bounds__(128 * expand_waves(NOPE, DV), expand_occupancy(DC, expand_waves(NOPE, DV))) void expand_kernel(Cache c, Step s, Heads h, Both both) {
     constexpr int G = DC / 64, KEYS = NOPE / 32, VALUES = DV / 32, WAVES = expand_waves(NOPE, DV), TILE = kSlots * (NOPE + DV) / 8;
     __shared__ u32x4 lds[G * 128 * 8];
     __shared__ uint32_t seen[2][2][WAVES];  // [odd and even heads][tile of 64][wavefront]
     __shared__ uint32_t largest[2][2];  // [keys, values][tile of 64]
     __shared__ int bad[128];
     const int lane = threadIdx.x & 63, wave = wave_number() % WAVES, half = wave_number() / WAVES, col = lane & 31, grp = lane >> 5;
-    const int pairs_of = (m.tiles + 1) / 2;
-    const int pair = blockIdx.x % pairs_of, rest = blockIdx.x / pairs_of;
-    const int seq = PREFIX ? 0 : rest % c.n_seq, first = (PREFIX ? rest : rest / c.n_seq) * each;
-    const int total = slots_of<PREFIX>(c, s, seq), j0 = pair * 128;
+    const bool prefix = (int)blockIdx.x < both.before;
+    const Made& m = prefix ? both.pre : both.own;
+    const int block = prefix ? blockIdx.x : blockIdx.x - both.before, pairs_of = (m.tiles + 1) / 2;
+    const int pair = block % pairs_of, rest = block / pairs_of;
+    const int seq = prefix ? 0 : rest % c.n_seq, first = (prefix ? rest : rest / c.n_seq) * m.each;
+    const int total = slots_of(c, s, prefix, seq), j0 = pair * 128;
     if (j0 >= total) return;
     const int width = c.latent + c.rope;
-    const uint16_t* C = PREFIX ? c.prefix : c.rows + (int64_t)seq * c.max_len * width;
+    const uint16_t* C = prefix ? c.prefix : c.rows + (int64_t)seq * c.max_len * width;
     {
         const uint32_t at = lds_address(lds);
         const int in8 = lane >> 3;
@@ -137,7 +145,7 @@ __global__ __launch_bounds__(128 * expand_waves(NOPE, DV), expand_occupancy(DC, 
     for (int f = 0; f < 4; ++f) at[f] = lds_address(lds) + (uint32_t)((half * 64 + col) * 128 + ((2 * f + grp) ^ twist(col)) * 16);
     wait_copies<0>();
     __syncthreads();
-    for (int head = first; head < min(first + each, m.heads); ++head) {
+    for (int head = first; head < min(first + m.each, m.heads); ++head) {
         f32x16 k[2], v[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -243,26 +251,29 @@ __global__ __launch_bounds__(128 * expand_waves(NOPE, DV), expand_occupancy(DC, 
 // exchange but one between two lanes, and the weights are the second operand of the sums as they stand.  Tiles come in turn into two
 // buffers, without registers.  2 prompts of about 4000 tokens, 32 heads: 335 GFLOP in 356 us, 0.94 PFLOP/s, 76 % of what a large library product reaches;
 // matrix cores half busy, the clock at the card's power limit.
-template <int NOPE, int DV, int DR, bool PREFIX>
-__global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads h, Attend a, Made m, Parts parts) {
+template <int NOPE, int DV, int DR>
+__global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads h, Attend a, Both both, Parts parts) {
     typedef Sizes<NOPE, DV, DR> Z;
     constexpr int KF = NOPE / 16, PF = DR / 16, VB = DV / 32;
     __shared__ u32x4 lds[2][Z::kBytes / 16];
     const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, grp = lane >> 5;
-    const int seqs = PREFIX ? 1 : c.n_seq, pairs = seqs * m.heads;
-    const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
+    const bool prefix = (int)blockIdx.x < both.before;
+    const Made& m = prefix ? both.pre : both.own;
+    const int block = prefix ? blockIdx.x : blockIdx.x - both.before, pairs = (prefix ? 1 : c.n_seq) * m.heads;
+    const int pair = block % pairs, rest = block / pairs;
     const int seq = pair / m.heads, head = pair % m.heads;
     const int range = rest % m.ranges, tile = m.row_tiles - 1 - rest / m.ranges;  // those that see the most slots first
-    const Seq q = PREFIX ? Seq{0, s.n_rows, 0} : kkv8::sequence(c.max_len, s, seq);
+    Seq q{0, s.n_rows, 0};
+    if (!prefix) q = kkv8::sequence(c.max_len, s, seq);
     const int rows = q.n_new, row0 = tile * kRows, first = range * m.per;
     if (row0 >= rows) return;
-    const int sees = PREFIX ? c.prefix_len : q.cached + min(row0 + kRows, rows);  // slots that the last row sees
+    const int sees = prefix ? c.prefix_len : q.cached + min(row0 + kRows, rows);  // slots that the last row sees
     const int end = min(first + m.per, sees);
     if (first >= end) return;
     const int r = row0 + wave * 32 + col, mine = min(r, rows - 1);
-    const int limit = PREFIX ? c.prefix_len : q.cached + mine + 1;
-    const int wave_least = PREFIX ? c.prefix_len : q.cached + min(row0 + wave * 32, rows - 1) + 1;
-    const int wave_most = PREFIX ? c.prefix_len : q.cached + min(row0 + wave * 32 + 31, rows - 1) + 1;
+    const int limit = prefix ? c.prefix_len : q.cached + mine + 1;
+    const int wave_least = prefix ? c.prefix_len : q.cached + min(row0 + wave * 32, rows - 1) + 1;
+    const int wave_most = prefix ? c.prefix_len : q.cached + min(row0 + wave * 32 + 31, rows - 1) + 1;
     const bool active = row0 + wave * 32 < rows;
     const uint8_t* kv = (const uint8_t*)(m.kv + (int64_t)pair * m.tiles * Z::kTile);
     const uint8_t* pe = (const uint8_t*)(m.pe + (int64_t)seq * m.tiles * Z::kPe);
@@ -484,7 +495,6 @@ struct Plan {
     int heads;  // at a time
     int64_t o_ml, o_w, o_own_kv, o_own_pe, o_own_shift, o_pre_kv, o_pre_pe, o_pre_shift, bytes;
     int64_t own_groups, pre_groups, own_expand, pre_expand, merges;  // workgroups of the launches of a set of heads
-    int own_each, pre_each;
 };
 
 int64_t up256(int64_t v) { return (v + 255) & ~(int64_t)255; }
@@ -532,8 +542,8 @@ Plan plan(const Cache& c, const Step& s, const Heads& h) {
     p.own.ranges = (int)((most + p.own.per - 1) / p.own.per);
     p.parts.per = p.own.per;
     p.parts.own = p.parts.all = p.own.ranges;
-    p.own_each = heads_each(c.n_seq * ((tiles + 1) / 2), p.heads);
-    p.own_expand = c.n_seq * ((tiles + 1) / 2) * ((p.heads + p.own_each - 1) / p.own_each);
+    p.own.each = heads_each(c.n_seq * ((tiles + 1) / 2), p.heads);
+    p.own_expand = c.n_seq * ((tiles + 1) / 2) * ((p.heads + p.own.each - 1) / p.own.each);
     p.own_groups = (int64_t)c.n_seq * p.heads * own_rows * p.own.ranges;
     p.parts.pre_per = 1;
     if (c.prefix_len > 0) {
@@ -544,8 +554,8 @@ Plan plan(const Cache& c, const Step& s, const Heads& h) {
         p.pre.part0 = p.parts.own;
         p.parts.pre_per = p.pre.per;
         p.parts.all += p.pre.ranges;
-        p.pre_each = heads_each((pre_tiles + 1) / 2, p.heads);
-        p.pre_expand = ((pre_tiles + 1) / 2) * ((p.heads + p.pre_each - 1) / p.pre_each);
+        p.pre.each = heads_each((pre_tiles + 1) / 2, p.heads);
+        p.pre_expand = ((pre_tiles + 1) / 2) * ((p.heads + p.pre.each - 1) / p.pre.each);
         p.pre_groups = (int64_t)p.heads * pre_rows * p.pre.ranges;
     }
     const int64_t items = p.parts.all > 1 ? (int64_t)s.n_rows * h.n * p.parts.all : 0;
@@ -580,35 +590,33 @@ struct Call {
 };
 
 template <int DC, int NOPE, int DV>
-void launch_expand(const Call& k, const Made& m, int64_t groups, int each, bool prefix) {
-    const dim3 grid((unsigned)groups), block(128 * expand_waves(NOPE, DV));
-    if (prefix) hipLaunchKernelGGL((expand_kernel<DC, NOPE, DV, true>), grid, block, 0, k.st, k.c, k.s, k.h, m, each);
-    else hipLaunchKernelGGL((expand_kernel<DC, NOPE, DV, false>), grid, block, 0, k.st, k.c, k.s, k.h, m, each);
-}
-template <int NOPE, int DV, int DR>
-void launch_attention(const Call& k, const Made& m, int64_t groups, bool prefix) {
-    const dim3 grid((unsigned)groups), block(256);
-    if (prefix) hipLaunchKernelGGL((expanded_kernel<NOPE, DV, DR, true>), grid, block, 0, k.st, k.c, k.s, k.h, k.a, m, k.parts);
-    else hipLaunchKernelGGL((expanded_kernel<NOPE, DV, DR, false>), grid, block, 0, k.st, k.c, k.s, k.h, k.a, m, k.parts);
+void launch_expand(const Call& k, const Both& m, int64_t groups) {
+    hipLaunchKernelGGL((expand_kernel<DC, NOPE, DV>), dim3((unsigned)groups), dim3(128 * expand_waves(NOPE, DV)), 0, k.st, k.c, k.s, k.h, m);
 }
 template <int NOPE, int DV>
-void launch_pair(const Call& k, const Made& m, int64_t expand, int each, int64_t groups, bool prefix) {
-    if (k.c.latent == 128) launch_expand<128, NOPE, DV>(k, m, expand, each, prefix);
-    if (k.c.latent == 256) launch_expand<256, NOPE, DV>(k, m, expand, each, prefix);
-    if (k.c.latent == 512) launch_expand<512, NOPE, DV>(k, m, expand, each, prefix);
-    if (k.c.rope == 32) launch_attention<NOPE, DV, 32>(k, m, groups, prefix);
-    if (k.c.rope == 64) launch_attention<NOPE, DV, 64>(k, m, groups, prefix);
+void launch_expand_sizes(const Call& k, const Both& m, int64_t groups) {
+    if (k.c.latent == 128) launch_expand<128, NOPE, DV>(k, m, groups);
+    if (k.c.latent == 256) launch_expand<256, NOPE, DV>(k, m, groups);
+    if (k.c.latent == 512) launch_expand<512, NOPE, DV>(k, m, groups);
+}
+template <int NOPE, int DV>
+void launch_attention(const Call& k, const Both& m, int64_t groups) {
+    const dim3 grid((unsigned)groups), block(256);
+    if (k.c.rope == 32) hipLaunchKernelGGL((expanded_kernel<NOPE, DV, 32>), grid, block, 0, k.st, k.c, k.s, k.h, k.a, m, k.parts);
+    if (k.c.rope == 64) hipLaunchKernelGGL((expanded_kernel<NOPE, DV, 64>), grid, block, 0, k.st, k.c, k.s, k.h, k.a, m, k.parts);
+}
+template <int NOPE, int DV>
+void launch_set(const Call& k, Both m, int64_t pre_expand, int64_t own_expand, int64_t pre_groups, int64_t own_groups) {
+    m.before = (int)pre_expand;
+    launch_expand_sizes<NOPE, DV>(k, m, pre_expand + own_expand);
+    m.before = (int)pre_groups;
+    launch_attention<NOPE, DV>(k, m, pre_groups + own_groups);
 }
 template <int NOPE>
-void launch_nope(const Call& k, const Made& m, int64_t expand, int each, int64_t groups, bool prefix) {
-    if (k.h.v == 32) launch_pair<NOPE, 32>(k, m, expand, each, groups, prefix);
-    if (k.h.v == 64) launch_pair<NOPE, 64>(k, m, expand, each, groups, prefix);
-    if (k.h.v == 128) launch_pair<NOPE, 128>(k, m, expand, each, groups, prefix);
-}
-void launch_set(const Call& k, const Made& m, int64_t expand, int each, int64_t groups, bool prefix) {
-    if (k.h.nope == 32) launch_nope<32>(k, m, expand, each, groups, prefix);
-    if (k.h.nope == 64) launch_nope<64>(k, m, expand, each, groups, prefix);
-    if (k.h.nope == 128) launch_nope<128>(k, m, expand, each, groups, prefix);
+void launch_nope(const Call& k, const Both& m, int64_t pre_expand, int64_t own_expand, int64_t pre_groups, int64_t own_groups) {
+    if (k.h.v == 32) launch_set<NOPE, 32>(k, m, pre_expand, own_expand, pre_groups, own_groups);
+    if (k.h.v == 64) launch_set<NOPE, 64>(k, m, pre_expand, own_expand, pre_groups, own_groups);
+    if (k.h.v == 128) launch_set<NOPE, 128>(k, m, pre_expand, own_expand, pre_groups, own_groups);
 }
 
 }  // namespace
@@ -617,7 +625,7 @@ int64_t expanded_workspace(const Cache& c, const Step& s, const Heads& h) { retu
 
 bool expanded_fits(const Cache& c, const Step& s, const Heads& h) {
     const Plan p = plan(c, s, h);
-    for (int64_t n : {p.own_groups, p.pre_groups, p.own_expand, p.pre_expand, p.merges})
+    for (int64_t n : {p.own_groups + p.pre_groups, p.own_expand + p.pre_expand, p.merges})
         if (n > kMostGroups) return false;
     return true;
 }
@@ -642,9 +650,12 @@ void launch_expanded(hipStream_t st, const Cache& c, const Step& s, const Heads&
         // the last set of heads may be smaller: its launches have the workgroups of its own heads
         auto of_heads = [&](int64_t groups) { return groups / p.heads * heads; };
         auto of_each = [&](int64_t groups, int each) { return groups / ((p.heads + each - 1) / each) * ((heads + each - 1) / each); };
-        if (c.prefix_len > 0)
-            launch_set(k, made(p.pre, p.o_pre_kv, p.o_pre_pe, p.o_pre_shift), of_each(p.pre_expand, p.pre_each), p.pre_each, of_heads(p.pre_groups), true);
-        launch_set(k, made(p.own, p.o_own_kv, p.o_own_pe, p.o_own_shift), of_each(p.own_expand, p.own_each), p.own_each, of_heads(p.own_groups), false);
+        const Both both{made(p.pre, p.o_pre_kv, p.o_pre_pe, p.o_pre_shift), made(p.own, p.o_own_kv, p.o_own_pe, p.o_own_shift), 0};
+        const int64_t pre_expand = c.prefix_len > 0 ? of_each(p.pre_expand, p.pre.each) : 0, own_expand = of_each(p.own_expand, p.own.each);
+        const int64_t pre_groups = of_heads(p.pre_groups), own_groups = of_heads(p.own_groups);
+        if (h.nope == 32) launch_nope<32>(k, both, pre_expand, own_expand, pre_groups, own_groups);
+        if (h.nope == 64) launch_nope<64>(k, both, pre_expand, own_expand, pre_groups, own_groups);
+        if (h.nope == 128) launch_nope<128>(k, both, pre_expand, own_expand, pre_groups, own_groups);
     }
     if (p.merges > 0) {
         const dim3 grid((unsigned)p.merges), block(256);
