@@ -19,7 +19,7 @@ struct Tile {
     static constexpr bool kHalf = kWidth % 64 != 0;
 };
 
-struct Run {  // one launch
+struct Run {  // the rows of the sequences over their own slots, or all rows over the prefix
     int H, row_tiles;  // tiles of 32 * MT rows of a sequence (of the prefix: of all)
     int per, ranges;   // slots of a range, ranges at most
     int part0;         // where the launch's parts are among a row's
@@ -27,6 +27,10 @@ struct Run {  // one launch
     float qscale;
     const uint16_t* a;  // [row, head, 2 * latent + rope], see absorb_kernel
     Parts parts;
+};
+struct Both {  // one launch: the first `before` workgroups have the prefix, the others the sequences
+    Run pre, own;
+    int before;
 };
 
 struct Place {
@@ -38,11 +42,11 @@ struct Place {
 // more than its compute units take at once and another none: 48 sequences of 80 to 6001 slots, 128 heads 143 us so
 // (and in three ranges, see split), 121 packed.
 template <int M>
-__device__ __forceinline__ bool place_of(const Cache& c, const Step& s, const Run& run, Place* at) {
+__device__ __forceinline__ bool place_of(const Cache& c, const Step& s, const Run& run, int block, int blocks, Place* at) {
     const int lane = threadIdx.x & 63;
-    int left = blockIdx.x;
+    int left = block;
     // two tiles of a range to one XCD, which then reads its slots once
-    if (run.row_tiles > 1 && (left | 15) < (int)gridDim.x) left = (left & ~15) + (left & 7) * 2 + (left >> 3 & 1);
+    if (run.row_tiles > 1 && (left | 15) < blocks) left = (left & ~15) + (left & 7) * 2 + (left >> 3 & 1);
     for (int kind = 0; kind < 3; ++kind)
         for (int first = 0; first < c.n_seq; first += 64) {
             int tiles = 0, full = 0, here = 0;
@@ -85,8 +89,8 @@ __device__ __forceinline__ bool place_of(const Cache& c, const Step& s, const Ru
 // 64 registers and the rows 136, which leaves two wavefronts to a SIMD.
 // References of the softmax are whole numbers, so that bringing sums or weights from one to another is exact.  The two wavefronts of a row
 // set theirs by their own halves; behind the barrier everybody sees both and goes on with the larger one.
-template <int DC, int DR, int MT, bool PREFIX, bool STREAM>
-__global__ __launch_bounds__(256 * MT, 2) void absorbed_kernel(Cache c, Step s, Run run) {
+template <int DC, int DR, int MT, bool STREAM>
+__global__ __launch_bounds__(256 * MT, 2) void absorbed_kernel(Cache c, Step s, Both both) {
     typedef Tile<DC, DR> T;
     constexpr int WAVES = 4 * MT, GROUPS = 2 * MT, SUB = MT, M = 32 * MT;
     constexpr int KEYS = T::kWidth / 32, LOW = DC / 32;               // products of a score: first halves, second ones
@@ -99,30 +103,35 @@ __global__ __launch_bounds__(256 * MT, 2) void absorbed_kernel(Cache c, Step s, 
     __shared__ float sm_ref[2][M], sm_sum[2][M];
     const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, grp = lane >> 5, c16 = lane & 15, g16 = lane >> 4;
     const int rows16 = wave % GROUPS, half = wave / GROUPS;
+    const bool prefix = (int)blockIdx.x < both.before;
+    const Run run = prefix ? both.pre : both.own;
+    const int block = prefix ? blockIdx.x : blockIdx.x - both.before;
     // of the prefix the ranges, each to its XCD; of a sequence the row tiles one behind the other, so that they read its slots together
-    Place at{0, run.row_tiles - 1 - (int)blockIdx.x / run.ranges, (int)blockIdx.x % run.ranges};
-    if (!PREFIX) {
+    Place at{0, run.row_tiles - 1 - block / run.ranges, block % run.ranges};
+    if (!prefix) {
         if (run.packed) {
-            if (!place_of<M>(c, s, run, &at)) return;
+            if (!place_of<M>(c, s, run, block, (int)gridDim.x - both.before, &at)) return;
         } else {
-            const int rest = blockIdx.x / c.n_seq;
-            at = Place{(int)blockIdx.x % c.n_seq, run.row_tiles - 1 - rest % run.row_tiles, rest / run.row_tiles};
+            const int rest = block / c.n_seq;
+            at = Place{block % c.n_seq, run.row_tiles - 1 - rest % run.row_tiles, rest / run.row_tiles};
         }
     }
     const int seq = __builtin_amdgcn_readfirstlane(at.seq), tile = __builtin_amdgcn_readfirstlane(at.tile), range = __builtin_amdgcn_readfirstlane(at.range);
-    Seq q;
-    if (PREFIX) q = Seq{0, s.n_rows, 0};
-    else q = kkv8::sequence(c.max_len, s, seq);
+    Seq q{0, s.n_rows, 0};
+    if (!prefix) q = kkv8::sequence(c.max_len, s, seq);
+    q.row0 = __builtin_amdgcn_readfirstlane(q.row0);
+    q.n_new = __builtin_amdgcn_readfirstlane(q.n_new);
+    q.cached = __builtin_amdgcn_readfirstlane(q.cached);
     const int rows = q.n_new * run.H, row0 = tile * M;
     if (row0 >= rows) return;
     const int first = range * run.per;
-    const int sees = PREFIX ? c.prefix_len : q.cached + (min(row0 + M, rows) - 1) / run.H + 1;  // slots that the last row sees
+    const int sees = prefix ? c.prefix_len : q.cached + (min(row0 + M, rows) - 1) / run.H + 1;  // slots that the last row sees
     const int end = min(first + run.per, sees);
     if (first >= end) return;
-    const uint16_t* C = PREFIX ? c.prefix : c.rows + (int64_t)seq * c.max_len * T::kWidth;
+    const uint16_t* C = prefix ? c.prefix : c.rows + (int64_t)seq * c.max_len * T::kWidth;
     const int mine = min(row0 + rows16 * 16 + c16, rows - 1);                    // the lane's row, for the scores
-    const int limit = min(PREFIX ? c.prefix_len : q.cached + mine / run.H + 1, end);  // slots of the range that it sees end here
-    const int all_see = PREFIX ? c.prefix_len : q.cached + row0 / run.H + 1;     // slots that every row sees
+    const int limit = min(prefix ? c.prefix_len : q.cached + mine / run.H + 1, end);  // slots of the range that it sees end here
+    const int all_see = prefix ? c.prefix_len : q.cached + row0 / run.H + 1;     // slots that every row sees
     const int64_t row_head = (int64_t)q.row0 * run.H + row0;
 
     // copies: a wavefront brings 8 slots x 8 units at a time, one quarter of a tile
@@ -194,7 +203,7 @@ const uint32_t from = cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, to = c
         // A latent that is not finite, in a slot that some row of the workgroup does not see, would reach that row as 0 times it.
         // In tiles where that can be, such slots give up their latents and get NaN in the part that only the scores read:
         // the rows that see them become NaN, as they have to, and no others.  Done by the wavefront that brought the slots.
-        if (!PREFIX && all_see < sees && j0 + SUB * 32 > all_see) {
+        if (all_see < sees && j0 + SUB * 32 > all_see) {
             const uint32_t at = lds_at + buf * STEP + sub * T::kBytes;
 #pragma unroll 1
             for (int slot = quarter * 8; slot < quarter * 8 + 8; ++slot) {
@@ -358,30 +367,51 @@ int64_t up256(int64_t v) { return (v + 255) & ~(int64_t)255; }
 // Tiles of 32 rows of a workgroup that has `rows` of them to share.
 int wide(int64_t rows) { return rows <= 32 ? 1 : 2; }
 
-// Ranges of `most` slots for `groups` workgroups each, of `mt` tiles of 32 rows: as many as take least, in slots of one workgroup alone: a round of
-// workgroups takes its range and 150 slots for its start and its end, a third more where two share a compute unit; a part costs finish_kernel
-// 16 where one wavefront adds a row's, 2 where eight do.  Whole calls with every sequence as long as its bound: 48 of 8000 slots, 128 heads, in three
-// ranges (288 workgroups for 256 compute units) 329 us, in eight 262; of 30000, 8 heads, in 11 (528 for 512 places) 365, in ten 275; 5 of 30000 in 103 83, in 43
-// 68; 1 of 701 in three ranges 20 us of attention, in eleven 12.5.
-void split(int64_t most, int64_t groups, int mt, bool few, int* per, int* ranges) {
-    const int64_t limit = min((most + 63) / 64, (int64_t)256);
+// When `n` workgroups of length `l` and then `m` shorter ones of length `k` end that have `places`: those that the last round of the
+// long ones leaves free are filled first.
+float ends(int64_t n, float l, int64_t m, float k, int64_t places) {
+    if (l < k) return ends(m, k, n, l, places);
+    const int64_t rounds = (n + places - 1) / places, free = rounds * places - n, fit = free * (int64_t)(l / k), left = m > fit ? m - fit : 0;
+    return (float)rounds * l + (float)((left + places - 1) / places) * k;
+}
+
+// Ranges of slots of the sequences and of the prefix.
+struct Split {
+    int own_per, own_ranges, pre_per, pre_ranges;
+};
+
+// As many ranges as take least, in slots of one workgroup alone: a workgroup takes its range and 150 slots for its start and its end, a third
+// more where two share a compute unit; a part costs finish_kernel 16 where one wavefront adds a row's, 2 where eight do.  Whole calls with every
+// sequence as long as its bound: 48 of 8000 slots, 128 heads, in three ranges (288 workgroups for 256 compute units) 329 us, in eight 262; of 30000, 8
+// heads, in 11 (528 for 512 places) 365, in ten 275; 5 of 30000 in 103 83, in 43 68; 1 of 701 in three ranges 20 us of attention, in eleven 12.5.
+// With a prefix in the same launch the two share the places: 64 sequences of 1 to 501 slots and a prefix of 4096, 32 heads, in launches of their own 42 and
+// 17 us of attention, together 54; 12 of 27 to 81 and 3967 whole calls of 61 and 51 us.
+Split split(int64_t own, int64_t own_groups, int64_t pre, int64_t pre_groups, int mt, bool few) {
+    const auto cut = [](int64_t most, int64_t n) { return ((most + n - 1) / n + 63) / 64 * 64; };
+    const auto limit = [](int64_t most, int64_t n) { return min((most + 63) / 64, n); };
+    const float part = few ? 2.f : 16.f;
     float least = 0.f;
-    *per = (int)((most + 63) / 64 * 64);
-    *ranges = 1;
-    for (int64_t n = 1; n <= limit; ++n) {
-        const float parts = (few ? 2.f : 16.f) * (float)n;
-        if (n > 1 && parts >= least) break;
-        const int64_t p = ((most + n - 1) / n + 63) / 64 * 64, r = (most + p - 1) / p;
-        if (r != n) continue;
-        const int64_t wgs = groups * n;
-        const float rounds = mt == 2 || wgs <= 256 ? (float)((wgs + 255) / 256) : 1.33f * (float)((wgs + 511) / 512);
-        const float cost = rounds * ((float)p + 150.f) + parts;
-        if (n == 1 || cost < least) {
-            least = cost;
-            *per = (int)p;
-            *ranges = (int)n;
+    Split best{};
+    for (int64_t a = 1; a <= max(limit(own, pre > 0 ? 32 : 256), (int64_t)1); ++a) {
+        const int64_t p = own > 0 ? cut(own, a) : 64;
+        if (own > 0 && (own + p - 1) / p != a) continue;
+        if (a > 1 && part * (float)a >= least) break;
+        for (int64_t b = pre > 0 ? 1 : 0; b <= limit(pre, own > 0 ? 64 : 256); ++b) {
+            const int64_t r = b > 0 ? cut(pre, b) : 64;
+            if (b > 0 && (pre + r - 1) / r != b) continue;
+            const float parts = part * (float)(a + b);
+            if (b > 1 && parts >= least) break;
+            const int64_t wgs = own_groups * a + pre_groups * b;
+            const int64_t places = mt == 2 || wgs <= 256 ? 256 : 512;
+            float cost = (places == 512 ? 1.33f : 1.f) * ends(pre_groups * b, (float)r + 150.f, own_groups * a, (float)p + 150.f, places);
+            cost += parts;
+            if (best.own_ranges == 0 || cost < least) {
+                least = cost;
+                best = Split{(int)p, (int)a, (int)r, (int)b};
+            }
         }
     }
+    return best;
 }
 
 // How a step is run, from its sizes and bounds.
@@ -398,19 +428,32 @@ Plan plan(const Cache& c, const Step& s, const Heads& h) {
     if (s.n_rows == 0) return p;
     const int64_t most = min((int64_t)s.max_cached + s.max_new, (int64_t)c.max_len);
     const int64_t rows = (int64_t)s.max_new * h.n, all = (int64_t)s.n_rows * h.n;
-    p.own_mt = wide(rows);
-    p.own_tiles = (int)((rows + p.own_mt * 32 - 1) / (p.own_mt * 32));
-    split(most, (int64_t)c.n_seq * p.own_tiles, p.own_mt, finish_few(h, s.n_rows), &p.parts.per, &p.own_ranges);
-    p.own_groups = (int64_t)c.n_seq * p.own_tiles * p.own_ranges;
-    p.parts.own = p.parts.all = p.own_ranges;
-    p.parts.pre_per = 1;
+    const bool few = finish_few(h, s.n_rows);
+    p.own_mt = p.pre_mt = wide(rows);
     if (c.prefix_len > 0) {
         p.pre_mt = wide(all);
+        // Few rows over few slots go with the prefix's, though half of a workgroup's rows are empty then: a launch of their own costs 8 us and more.
+        if (c.n_seq * most <= 1 << 17) p.own_mt = p.pre_mt;
         p.pre_tiles = (int)((all + p.pre_mt * 32 - 1) / (p.pre_mt * 32));
-        split(c.prefix_len, p.pre_tiles, p.pre_mt, finish_few(h, s.n_rows), &p.parts.pre_per, &p.pre_ranges);
-        p.pre_groups = (int64_t)p.pre_tiles * p.pre_ranges;
-        p.parts.all += p.pre_ranges;
     }
+    p.own_tiles = (int)((rows + p.own_mt * 32 - 1) / (p.own_mt * 32));
+    const int64_t groups = (int64_t)c.n_seq * p.own_tiles;
+    Split cut;
+    if (p.own_mt == p.pre_mt) {
+        cut = split(most, groups, c.prefix_len, p.pre_tiles, p.own_mt, few);
+    } else {
+        cut = split(most, groups, 0, 0, p.own_mt, few);
+        const Split pre = split(0, 0, c.prefix_len, p.pre_tiles, p.pre_mt, few);
+        cut.pre_per = pre.pre_per;
+        cut.pre_ranges = pre.pre_ranges;
+    }
+    p.parts.per = cut.own_per;
+    p.parts.pre_per = cut.pre_per;
+    p.own_ranges = p.parts.own = cut.own_ranges;
+    p.pre_ranges = cut.pre_ranges;
+    p.parts.all = p.own_ranges + p.pre_ranges;
+    p.own_groups = groups * p.own_ranges;
+    p.pre_groups = (int64_t)p.pre_tiles * p.pre_ranges;
     const int64_t items = all * p.parts.all;
     int64_t o = up256(items * c.latent * 4);
     p.o_ml = o;
@@ -421,42 +464,36 @@ Plan plan(const Cache& c, const Step& s, const Heads& h) {
     return p;
 }
 
-template <int DC, int DR, bool PREFIX>
-void launch_run(hipStream_t st, const Cache& c, const Step& s, const Run& run, int mt, int64_t groups) {
-    const dim3 grid((unsigned)groups);
+template <int DC, int DR>
+void launch_run(hipStream_t st, const Cache& c, const Step& s, Both both, int mt, int64_t pre_groups, int64_t own_groups) {
+    const dim3 grid((unsigned)(pre_groups + own_groups));
+    both.before = (int)pre_groups;
     if (mt == 2) {
-        hipLaunchKernelGGL((absorbed_kernel<DC, DR, 2, PREFIX, false>), grid, dim3(512), 0, st, c, s, run);
+        hipLaunchKernelGGL((absorbed_kernel<DC, DR, 2, false>), grid, dim3(512), 0, st, c, s, both);
         return;
     }
     // Caches beyond the last-level cache of 256 MiB, read once by every call, are read past it: 512 sequences of 513 slots (302 MB) 74 us with ordinary
     // copies, 66 so.
     const int64_t bytes = (int64_t)c.n_seq * min((int64_t)s.max_cached + s.max_new, (int64_t)c.max_len) * (DC + DR) * 2;
-    if (!PREFIX && run.row_tiles == 1 && bytes > (int64_t)256 << 20) hipLaunchKernelGGL((absorbed_kernel<DC, DR, 1, false, true>), grid, dim3(256), 0, st, c, s, run);
-    else hipLaunchKernelGGL((absorbed_kernel<DC, DR, 1, PREFIX, false>), grid, dim3(256), 0, st, c, s, run);
+    if (own_groups > 0 && both.own.row_tiles == 1 && bytes > (int64_t)256 << 20) hipLaunchKernelGGL((absorbed_kernel<DC, DR, 1, true>), grid, dim3(256), 0, st, c, s, both);
+    else hipLaunchKernelGGL((absorbed_kernel<DC, DR, 1, false>), grid, dim3(256), 0, st, c, s, both);
 }
 
 template <int DC, int DR>
-void launch_sizes(hipStream_t st, const Cache& c, const Step& s, const Plan& p, Run run) {
-    if (p.pre_groups > 0) {
-        run.row_tiles = p.pre_tiles;
-        run.per = p.parts.pre_per;
-        run.ranges = p.pre_ranges;
-        run.part0 = p.parts.own;
-        launch_run<DC, DR, true>(st, c, s, run, p.pre_mt, p.pre_groups);
+void launch_sizes(hipStream_t st, const Cache& c, const Step& s, const Plan& p, const Both& both) {
+    if (p.own_mt == p.pre_mt) {
+        launch_run<DC, DR>(st, c, s, both, p.own_mt, p.pre_groups, p.own_groups);
+    } else {
+        launch_run<DC, DR>(st, c, s, both, p.pre_mt, p.pre_groups, 0);
+        launch_run<DC, DR>(st, c, s, both, p.own_mt, 0, p.own_groups);
     }
-    run.row_tiles = p.own_tiles;
-    run.per = p.parts.per;
-    run.ranges = p.own_ranges;
-    run.part0 = 0;
-    run.packed = p.own_ranges > 1 && c.n_seq <= 256;
-    launch_run<DC, DR, false>(st, c, s, run, p.own_mt, p.own_groups);
 }
 
 }  // namespace
 
 bool absorbed_fits(const Cache& c, const Step& s, const Heads& h) {
     const Plan p = plan(c, s, h);
-    return p.own_groups <= kMostGroups && p.pre_groups <= kMostGroups && absorb_groups(c, h, s.n_rows) <= kMostGroups &&
+    return p.own_groups + p.pre_groups <= kMostGroups && absorb_groups(c, h, s.n_rows) <= kMostGroups &&
            finish_groups(h, s.n_rows) <= kMostGroups;
 }
 
@@ -473,12 +510,21 @@ void launch_absorbed(hipStream_t st, const Cache& c, const Step& s, const Heads&
     run.qscale = a.qscale;
     run.a = rows;
     run.parts = p.parts;
-    if (c.latent == 128 && c.rope == 32) launch_sizes<128, 32>(st, c, s, p, run);
-    if (c.latent == 128 && c.rope == 64) launch_sizes<128, 64>(st, c, s, p, run);
-    if (c.latent == 256 && c.rope == 32) launch_sizes<256, 32>(st, c, s, p, run);
-    if (c.latent == 256 && c.rope == 64) launch_sizes<256, 64>(st, c, s, p, run);
-    if (c.latent == 512 && c.rope == 32) launch_sizes<512, 32>(st, c, s, p, run);
-    if (c.latent == 512 && c.rope == 64) launch_sizes<512, 64>(st, c, s, p, run);
+    Both both{run, run, 0};
+    both.pre.row_tiles = p.pre_tiles;
+    both.pre.per = p.parts.pre_per;
+    both.pre.ranges = max(p.pre_ranges, 1);
+    both.pre.part0 = p.parts.own;
+    both.own.row_tiles = p.own_tiles;
+    both.own.per = p.parts.per;
+    both.own.ranges = p.own_ranges;
+    both.own.packed = p.own_ranges > 1 && c.n_seq <= 256;
+    if (c.latent == 128 && c.rope == 32) launch_sizes<128, 32>(st, c, s, p, both);
+    if (c.latent == 128 && c.rope == 64) launch_sizes<128, 64>(st, c, s, p, both);
+    if (c.latent == 256 && c.rope == 32) launch_sizes<256, 32>(st, c, s, p, both);
+    if (c.latent == 256 && c.rope == 64) launch_sizes<256, 64>(st, c, s, p, both);
+    if (c.latent == 512 && c.rope == 32) launch_sizes<512, 32>(st, c, s, p, both);
+    if (c.latent == 512 && c.rope == 64) launch_sizes<512, 64>(st, c, s, p, both);
     launch_finish(st, c, s, h, a.out, p.parts);
 }
 

@@ -94,7 +94,7 @@ Heads heads_of(const moe_latent_cache* c, const moe_latent_heads* h) {
 // slot (of 128 at a time) at 550 TFLOP/s, attention at 500.  Absorbed: attention at 700, and each row's way into the latent space and out of it at
 // 4.5 TB/s.  Measured, absorbed / expanded, 32 heads: 1 token behind 700 slots 26 / 46 us; 8 prompts of 128 tokens 102 / 35; 64 tokens behind
 // 4000 slots 67 / 79, 128 tokens 94 / 90; 64 sequences of 64 tokens behind 500 slots 595 / 612, of 128 1211 / 769; behind a prefix of 4000
-// slots and 100 of their own 64 sequences of 4 tokens 149 / 196, of 16 474 / 272.  Of 293 steps between, 5 took a form that is more than
+// slots and 100 of their own 64 sequences of 4 tokens 149 / 196, of 16 474 / 272.  Of 293 steps between, 6 took a form that is more than
 // 10 % slower than the other, by 19 % at most.
 bool expands(const Cache& c, const Step& s, const Heads& h, int form) {
     if (form != MOE_LATENT_AUTO) return form == MOE_LATENT_EXPANDED;
