@@ -91,21 +91,21 @@ Heads heads_of(const moe_latent_cache* c, const moe_latent_heads* h) {
 
 // Whether a step is better run expanded: by what either form takes in microseconds, from the step's bounds.  Both: launches, and steps over
 // slots that one wavefront takes one after the other; about half as long at the smallest sizes of a head.  Expanded: keys and values of every
-// slot (of 128 at a time) at 550 TFLOP/s, attention at 500.  Absorbed: attention at 700, and each row's way into the latent space and out of it at
-// 4.5 TB/s.  Measured, absorbed / expanded, 32 heads: 1 token behind 700 slots 26 / 46 us; 8 prompts of 128 tokens 102 / 35; 64 tokens behind
+// slot (of 128 at a time) at 550 TFLOP/s, attention at 500.  Absorbed: attention at 800, and each row's way into the latent space and out of it, with its share of
+// a workgroup's start and end, at 3 TB/s.  Measured, absorbed / expanded, 32 heads: 1 token behind 700 slots 26 / 46 us; 8 prompts of 128 tokens 102 / 35; 64 tokens behind
 // 4000 slots 67 / 79, 128 tokens 94 / 90; 64 sequences of 64 tokens behind 500 slots 595 / 612, of 128 1211 / 769; behind a prefix of 4000
-// slots and 100 of their own 64 sequences of 4 tokens 149 / 196, of 16 474 / 272.  Of 293 steps between, 6 took a form that is more than
-// 10 % slower than the other, by 19 % at most.
+// slots and 100 of their own 64 sequences of 4 tokens 149 / 196, of 16 474 / 272.  Of 354 steps between, 9 took a form that is more than
+// 10 % slower than the other, by 40 % at most.
 bool expands(const Cache& c, const Step& s, const Heads& h, int form) {
     if (form != MOE_LATENT_AUTO) return form == MOE_LATENT_EXPANDED;
     if (s.n_rows == 0) return false;
     const double most = (double)(s.max_cached + s.max_new < c.max_len ? s.max_cached + s.max_new : c.max_len), heads = h.n, rows = s.n_rows;
     const double pairs = rows * (c.prefix_len + most - 0.5 * s.max_new) * heads, slots = c.prefix_len + c.n_seq * std::ceil(most / 128) * 128;
     const double sizes = 0.5 + c.latent / 1024., in_turn = most + c.prefix_len;
-    const double expanded = sizes * (20 + 0.035 * std::fmin(in_turn, 600)) + slots * heads * 2 * c.latent * (h.nope + h.v) / 550e6 +
+    const double expanded = sizes * (20 + 0.028 * std::fmin(in_turn, 600)) + slots * heads * 2 * c.latent * (h.nope + h.v) / 550e6 +
                             pairs * 2 * (h.nope + c.rope + h.v) / 500e6;
     const double absorbed = sizes * (std::fmin(14 + 2 * std::log2(rows * heads), 36) + 0.004 * std::fmin(in_turn, 1024)) +
-                            pairs * 2 * (2 * c.latent + c.rope) / 700e6 + rows * heads * (16. * c.latent + 4 * c.rope) / 4.5e6;
+                            pairs * 2 * (2 * c.latent + c.rope) / 800e6 + rows * heads * (16. * c.latent + 4 * c.rope) / 3e6;
     return expanded < absorbed;
 }
 
