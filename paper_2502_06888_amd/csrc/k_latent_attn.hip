@@ -3,8 +3,9 @@
 //
 // A row of C has 1152 bytes (512 + 64) and takes part in 2 * (2 * 512 + 64) operations per row of A: bound by the bytes of
 // the cache up to about 60 rows of A, by the matrix cores and the LDS that feeds them beyond.  Measured: 512 sequences of 513 slots, 32 heads,
-// 302 MB in 61 us; 48 of 80 to 6001 slots, 128 heads, 121 us: a workgroup takes 64 slots in 4 us, of which the products are 1.3 and the reads
-// from LDS 1.4; the rest are the barriers between them, since the registers are full and nothing is left to run one tile's scores under another's sums.
+// 302 MB in 61 us; 48 of 80 to 6001 slots, 128 heads, 106 us; 16384 rows over 4000 slots 200 us: a workgroup of 64 rows takes 64 slots in 3.2
+// us, of which the products are 1.3 and the reads from LDS 1.4; the rest are the phases between barriers, since the registers are full and nothing is left to run
+// one step's scores under another's sums.
 #include "latent_device.h"
 
 namespace klat {
@@ -33,6 +34,15 @@ struct Both {  // one launch: the first `before` workgroups have the prefix, the
     int before;
 };
 
+// The lane, counted anew.  The loop below has no register to spare: what it needs of the lane now and then is made of this, where the compiler would
+// keep each address in a register of its own and then, short of them, read every key right before its products (48
+// sequences of 80 to 6001 slots, 128 heads 120 us, so 106).
+__device__ __forceinline__ int lane_now() {
+    int l;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(l));
+    return l;
+}
+
 struct Place {
     int seq, tile, range;
 };
@@ -40,7 +50,7 @@ struct Place {
 // Work of a workgroup among what the sequences have of it: whole ranges, then last ones of half a range and more, then the shorter ones, so that the
 // long ones start first and every XCD gets as many.  Laid out by the bounds, where a workgroup of a short sequence finds nothing to do, one XCD has
 // more than its compute units take at once and another none: 48 sequences of 80 to 6001 slots, 128 heads 143 us so
-// (and in three ranges, see split), 121 packed.
+// (and in three ranges, see split), packed 121.
 template <int M>
 __device__ __forceinline__ bool place_of(const Cache& c, const Step& s, const Run& run, int block, int blocks, Place* at) {
     const int lane = threadIdx.x & 63;
@@ -101,6 +111,7 @@ __global__ __launch_bounds__(256 * MT, 2) void absorbed_kernel(Cache c, Step s, 
     __shared__ __attribute__((aligned(16))) uint8_t lds[RING > SUMS ? RING : SUMS];
     __shared__ __attribute__((aligned(16))) uint8_t weights[SUB * M * 64];  // [tile][row][32 slots] bf16
     __shared__ float sm_ref[2][M], sm_sum[2][M];
+    __shared__ int sm_limit[M];  // slots of the range that a row sees end here
     const int lane = threadIdx.x & 63, wave = wave_number(), col = lane & 31, grp = lane >> 5, c16 = lane & 15, g16 = lane >> 4;
     const int rows16 = wave % GROUPS, half = wave / GROUPS;
     const bool prefix = (int)blockIdx.x < both.before;
@@ -130,16 +141,17 @@ __global__ __launch_bounds__(256 * MT, 2) void absorbed_kernel(Cache c, Step s, 
     if (first >= end) return;
     const uint16_t* C = prefix ? c.prefix : c.rows + (int64_t)seq * c.max_len * T::kWidth;
     const int mine = min(row0 + rows16 * 16 + c16, rows - 1);                    // the lane's row, for the scores
-    const int limit = min(prefix ? c.prefix_len : q.cached + mine / run.H + 1, end);  // slots of the range that it sees end here
+    if (g16 == 0 && half == 0) sm_limit[rows16 * 16 + c16] = min(prefix ? c.prefix_len : q.cached + mine / run.H + 1, end);
     const int all_see = prefix ? c.prefix_len : q.cached + row0 / run.H + 1;     // slots that every row sees
     const int64_t row_head = (int64_t)q.row0 * run.H + row0;
 
     // copies: a wavefront brings 8 slots x 8 units at a time, one quarter of a tile
     const uint32_t lds_at = lds_address(lds);
-    const int in8 = lane >> 3, quarter = wave & 3, sub = wave >> 2;
-    const uint32_t unit_at = (uint32_t)(((lane & 7) ^ twist(quarter * 8 + in8)) * 16);
+    const int quarter = wave & 3, sub = wave >> 2;
     const uint32_t copy_at = __builtin_amdgcn_readfirstlane(lds_at + sub * T::kBytes + quarter * 1024);
     auto copy = [&](int buf, int j0) {
+        const int l = lane_now(), in8 = l >> 3;
+        const uint32_t unit_at = (uint32_t)(((l & 7) ^ twist(quarter * 8 + in8)) * 16);
         const uint32_t slot = (uint32_t)min(j0 + sub * 32 + quarter * 8 + in8, end - 1);  // past the end the last one again
         const uint32_t at = slot * (T::kWidth * 2) + unit_at;
 #pragma unroll
@@ -176,23 +188,12 @@ const uint32_t from = cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, to = c
 #pragma unroll
     for (int r = 0; r < ROW_TILES; ++r) sums_ref[r] = kEmpty;
 
-    // the lane's places in a tile: units 4 * (f % 2) + g16 of its slot; four slots of 16 elements for the transposed reads
+    // the lane's places in a tile: units 4 * (f % 2) + g16 of its slot
     const int key_slot = half * 16 + c16;
-    uint32_t key_at[2], value_at[2][2];
+    uint32_t key_at[2];
 #pragma unroll
     for (int f = 0; f < 2; ++f) key_at[f] = lds_at + (uint32_t)(key_slot * 128 + ((4 * f + g16) ^ twist(key_slot)) * 16);
-#pragma unroll
-    for (int odd = 0; odd < 2; ++odd)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int slot = 8 * grp + 4 * j + (c16 >> 2), unit = odd * 4 + (g16 & 1) * 2 + (lane >> 1 & 1);
-            value_at[odd][j] = lds_at + (uint32_t)(slot * 128 + (unit ^ twist(slot)) * 16 + (lane & 1) * 8);
-        }
-    // weights: 64 bytes a row, its four units at an xor of the row
     const uint32_t weights_at = lds_address(weights);
-    const int my_row = rows16 * 16 + c16;
-    const uint32_t put_at = weights_at + (uint32_t)(my_row * 64 + ((half * 2 + (g16 >> 1)) ^ (my_row >> 2 & 3)) * 16 + (g16 & 1) * 8);
-    const uint32_t get_at = weights_at + (uint32_t)((tile32 * 32 + col) * 64), get_xor = (uint32_t)(col >> 2 & 3);
 
     const int steps = (end - first + SUB * 32 - 1) / (SUB * 32);
     for (int t = 0; t < steps; ++t) {
@@ -204,22 +205,23 @@ const uint32_t from = cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, to = c
         // In tiles where that can be, such slots give up their latents and get NaN in the part that only the scores read:
         // the rows that see them become NaN, as they have to, and no others.  Done by the wavefront that brought the slots.
         if (all_see < sees && j0 + SUB * 32 > all_see) {
+            const int l = lane_now();
             const uint32_t at = lds_at + buf * STEP + sub * T::kBytes;
 #pragma unroll 1
             for (int slot = quarter * 8; slot < quarter * 8 + 8; ++slot) {
-                const uint32_t to = at + (lane >> 3) * 4096 + slot * 128 + ((lane & 7) ^ twist(slot)) * 16;
+                const uint32_t to = at + (l >> 3) * 4096 + slot * 128 + ((l & 7) ^ twist(slot)) * 16;
                 // word by word: registers are short here
                 bool bad = false;
 #pragma unroll 1
-                for (int e = 0; e < 16 && lane * 8 < DC; e += 4) {
+                for (int e = 0; e < 16 && l * 8 < DC; e += 4) {
                     const uint32_t x = read_lds_word(to + e);
                     bad |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
                 }
                 if (__any(bad)) {
 #pragma unroll 1
                     for (int e = 0; e < 16; e += 4) {
-                        if (lane * 8 < DC) write_lds_word(to + e, 0u);
-                        if (lane == 0) write_lds_word(at + (DC / 64) * 4096 + slot * 128 + twist(slot) * 16 + e, 0x7fff7fffu);
+                        if (l * 8 < DC) write_lds_word(to + e, 0u);
+                        if (l == 0) write_lds_word(at + (DC / 64) * 4096 + slot * 128 + twist(slot) * 16 + e, 0x7fff7fffu);
                     }
                 }
             }
@@ -229,9 +231,9 @@ const uint32_t from = cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, to = c
         f32x4 z[2];
         z[0] = z[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
+        for (int f = 0; f < KEYS; ++f)
 #pragma unroll
-            for (int f = 0; f < KEYS; ++f) {
+            for (int u = 0; u < SUB; ++u) {
                 const u32x4 k = read_lds(key_at[f & 1] + buf * STEP + u * T::kBytes + (f >> 1) * 4096);
                 z[u] = mfma16(k, hi[f], z[u]);
                 if (f < LOW) z[SUB == 1 ? 1 : u] = mfma16(k, lo[f], z[SUB == 1 ? 1 : u]);
@@ -245,18 +247,20 @@ const uint32_t from = cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, to = c
         }
         __builtin_amdgcn_sched_group_barrier(0x8, 8, 0);
         if (SUB == 1) z[0] += z[1];
+        const int l = lane_now(), my_row = rows16 * 16 + (l & 15);
         float top = -__builtin_inff();
+        if (j0 + SUB * 32 > all_see || j0 + SUB * 32 > end) {
+            const int within = sm_limit[my_row] - j0 - half * 16 - 4 * (l >> 4);
 #pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-            const int within = limit - j0 - u * 32 - half * 16 - 4 * g16;
-            if (j0 + SUB * 32 > all_see || j0 + SUB * 32 > end) {
+            for (int u = 0; u < SUB; ++u)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (i >= within) z[u][i] = -__builtin_inff();
-            }
+                    if (i >= within - u * 32) z[u][i] = -__builtin_inff();
+        }
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) top = fmaxf(top, z[u][i]);
-        }
         top *= run.qscale;
         if (__any(top > ref + kRise)) {
             top = fmaxf(top, __shfl_xor(top, 16, 64));
@@ -271,6 +275,8 @@ const uint32_t from = cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, to = c
 #pragma unroll
                 for (int i = 0; i < 4; ++i) z[u][i] = of(z[u][i]);
         });
+        // weights: 64 bytes a row, its four units at an xor of the row
+        const uint32_t put_at = weights_at + (uint32_t)(my_row * 64 + ((half * 2 + (l >> 5)) ^ (my_row >> 2 & 3)) * 16 + (l >> 4 & 1) * 8);
         u32x2 w[SUB];
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {  // the sum is that of the weights as rounded: then one slot that has nearly all of it counts nearly exactly
@@ -279,10 +285,10 @@ const uint32_t from = cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, to = c
             sum += (bf_lo(w[u].x) + bf_hi(w[u].x)) + (bf_lo(w[u].y) + bf_hi(w[u].y));
             write_lds2(put_at + u * M * 64, w[u]);
         }
-        if (g16 == 0) sm_ref[half][my_row] = ref;
+        if ((l >> 4) == 0) sm_ref[half][my_row] = ref;
         __syncthreads();
         // the references of a wavefront's lanes: row `lane` of all (32 of them twice with MT = 1)
-        const float both0 = sm_ref[0][lane & (M - 1)], both1 = sm_ref[1][lane & (M - 1)];
+        const float both0 = sm_ref[0][l & (M - 1)], both1 = sm_ref[1][l & (M - 1)];
         if (__any(both0 != both1)) {  // the same for the whole workgroup: halves that are behind bring their weights up
             const float now = fmaxf(ref, sm_ref[half ^ 1][my_row]), f = __builtin_amdgcn_exp2f(ref - now);
             sum *= f;
@@ -296,7 +302,7 @@ const uint32_t from = cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, to = c
         bool moved = false;
 #pragma unroll
         for (int r = 0; r < ROW_TILES; ++r) {
-            const int row = (tile32 + r) * 32 + col;
+            const int row = (tile32 + r) * 32 + (l & 31);
             now[r] = fmaxf(sm_ref[0][row], sm_ref[1][row]);
             moved |= now[r] != sums_ref[r];
         }
@@ -314,12 +320,22 @@ const uint32_t from = cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, to = c
         // Blocks of values AHEAD - 1 of their products, with the weights of half a tile: the order is laid down, since the compiler,
         // short of registers, would wait for every read.
         constexpr int AHEAD = MT == 2 ? 2 : 3, ITEMS = 2 * SUB * COLS;
+        // four slots of 16 elements for the transposed reads
+        uint32_t value_at[2][2];
+#pragma unroll
+        for (int odd = 0; odd < 2; ++odd)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int slot = 8 * (l >> 5) + 4 * j + (l >> 2 & 3), unit = odd * 4 + (l >> 4 & 1) * 2 + (l >> 1 & 1);
+                value_at[odd][j] = lds_at + (uint32_t)(slot * 128 + (unit ^ twist(slot)) * 16 + (l & 1) * 8);
+            }
+        const uint32_t get_at = weights_at + (uint32_t)((tile32 * 32 + (l & 31)) * 64), get_xor = (uint32_t)(l >> 2 & 3);
         u32x4 p[2][ROW_TILES], v[AHEAD];
         auto fetch = [&](int n) {
             const int u = n / COLS >> 1, h = n / COLS & 1, b = n % COLS;
             if (b == 0) {
 #pragma unroll
-                for (int r = 0; r < ROW_TILES; ++r) p[h][r] = read_lds(get_at + u * M * 64 + r * 2048 + ((h * 2 + grp) ^ get_xor) * 16);
+                for (int r = 0; r < ROW_TILES; ++r) p[h][r] = read_lds(get_at + u * M * 64 + r * 2048 + ((h * 2 + (l >> 5)) ^ get_xor) * 16);
             }
             const int odd = COLS > 1 ? b & 1 : block0 & 1;  // block0 is even wherever there is more than one block
             const uint32_t at = buf * STEP + u * T::kBytes + ((block0 + b) >> 1) * 4096 + h * 2048;
@@ -338,7 +354,7 @@ const uint32_t from = cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, to = c
     }
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
-    if (g16 == 0) sm_sum[half][my_row] = sum;
+    if (g16 == 0) sm_sum[half][rows16 * 16 + c16] = sum;
     __syncthreads();  // the tiles are done with, too
 
     // The sums go through LDS, so that a row leaves in one piece; its 16-byte units lie at an xor of the row.
@@ -385,7 +401,7 @@ struct Split {
 // sequence as long as its bound: 48 of 8000 slots, 128 heads, in three ranges (288 workgroups for 256 compute units) 329 us, in eight 262; of 30000, 8
 // heads, in 11 (528 for 512 places) 365, in ten 275; 5 of 30000 in 103 83, in 43 68; 1 of 701 in three ranges 20 us of attention, in eleven 12.5.
 // With a prefix in the same launch the two share the places: 64 sequences of 1 to 501 slots and a prefix of 4096, 32 heads, in launches of their own 42 and
-// 17 us of attention, together 54; 12 of 27 to 81 and 3967 whole calls of 61 and 51 us.
+// 17 us of attention, together 54 (49 since); 12 of 27 to 81 and 3967 whole calls of 61 and 51 us.
 Split split(int64_t own, int64_t own_groups, int64_t pre, int64_t pre_groups, int mt, bool few) {
     const auto cut = [](int64_t most, int64_t n) { return ((most + n - 1) / n + 63) / 64 * 64; };
     const auto limit = [](int64_t most, int64_t n) { return min((most + 63) / 64, n); };
