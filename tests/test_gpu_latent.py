@@ -313,6 +313,18 @@ def test_offsets_beyond_32_bits(form):
     check(x.run(form), form, x.reference())
 
 
+@pytest.mark.parametrize("prefix", [0, 70])
+@pytest.mark.parametrize("heads", [2, 8])
+def test_bounds_beyond_the_last_level_cache(heads, prefix):
+    """Slots read past the last-level cache; with a prefix in the same launch (all rows in one tile) and in one of its own."""
+    n, max_len = 9, 1 << 15
+    x = Layer(99, [300, 0, 1, 63, 64, 65, 200, 31, 400], [1] * n, heads, (512, 64, 32, 32), prefix=prefix, slack=(0, 29000), max_len=420)
+    rows = torch.full((n, max_len, 576), NAN, dtype=torch.bfloat16, device=DEV)
+    rows[:, :420] = x.cache.rows
+    x.cache = L.LatentCache(rows, 64, x.cache.prefix)
+    check(x.run(ABSORBED), ABSORBED, x.reference())
+
+
 @pytest.mark.parametrize("form", FORMS)
 def test_replays_of_a_captured_step_follow_the_lengths(form):
     x = Layer(93, [50, 200], [3, 1], 20, WIDE, prefix=40, slack=(2, 100), max_len=420)
