@@ -14,7 +14,7 @@
  * Conventions: as in moe_kv8.h: status codes, caller-owned device memory and streams, calls enqueue, allocate nothing, keep
  * nothing and never wait (they can be captured); numbers per sequence are read on the device when the kernels run and brought
  * into the bounds the host gives; every tensor on one device, which need not be the current one; workspaces may be used again
- * by the next call on the same stream (not by two graphs that may run at once); a launch has at most 2^24 - 1 workgroups, a call that asks for
+ * by the next call on the same stream (not by two graphs that may run at once); a launch has less than 2^32 threads, a call that asks for
  * more is MOE_ERR_SHAPE.  The error text of a failed call is moe_latent_last_error() on the same thread.
  */
 #ifndef KLOTSKI_MOE_LATENT_H
@@ -63,7 +63,8 @@ typedef struct {
 moe_status moe_latent_append(void* stream, const moe_latent_cache* cache, const moe_kv8_step* step, const void* x,
                              int64_t x_row_stride, const void* norm, float eps, const moe_rope_config* rope);
 
-/* How moe_latent_attend computes: MOE_LATENT_AUTO takes the form that should be the faster one by the step's bounds. */
+/* How moe_latent_attend computes: MOE_LATENT_AUTO takes the form that should be the faster one by the step's bounds, and the other one where
+ * that would have too many workgroups. */
 typedef enum { MOE_LATENT_AUTO = 0, MOE_LATENT_ABSORBED = 1, MOE_LATENT_EXPANDED = 2 } moe_latent_form;
 
 /*

@@ -321,10 +321,12 @@ static int absorb_each(const Cache& c, const Heads& h, int n_rows) {
     return all > 2048 ? (int)((all + 2047) / 2048) : 1;
 }
 
-int64_t absorb_groups(const Cache& c, const Heads& h, int n_rows) {
+static int64_t absorb_groups(const Cache& c, const Heads& h, int n_rows) {
     const int64_t tiles = (n_rows + 31) / 32, of = absorb_each(c, h, n_rows) * absorb_waves(n_rows);
     return h.n * (c.latent / 128) * ((tiles + of - 1) / of);
 }
+
+bool absorb_fits(const Cache& c, const Heads& h, int n_rows) { return launchable(absorb_groups(c, h, n_rows), 64 * absorb_waves(n_rows)); }
 
 template <int NOPE>
 static void launch_absorb_nope(hipStream_t st, const Cache& c, const Heads& h, const Rows& q, int n_rows, uint16_t* out) {
@@ -353,10 +355,12 @@ static int finish_span(const Heads& h, int n_rows) {
     return span;
 }
 
-int64_t finish_groups(const Heads& h, int n_rows) {
+static int64_t finish_groups(const Heads& h, int n_rows) {
     const int span = finish_span(h, n_rows);
     return (int64_t)h.n * ((n_rows + span - 1) / span);
 }
+
+bool finish_fits(const Heads& h, int n_rows) { return launchable(finish_groups(h, n_rows), 512); }
 
 namespace {
 template <int DC, int DV>

@@ -509,8 +509,9 @@ void launch_sizes(hipStream_t st, const Cache& c, const Step& s, const Plan& p, 
 
 bool absorbed_fits(const Cache& c, const Step& s, const Heads& h) {
     const Plan p = plan(c, s, h);
-    return p.own_groups + p.pre_groups <= kMostGroups && absorb_groups(c, h, s.n_rows) <= kMostGroups &&
-           finish_groups(h, s.n_rows) <= kMostGroups;
+    const bool attention = p.own_mt == p.pre_mt ? launchable(p.own_groups + p.pre_groups, 256 * p.own_mt)
+                                                : launchable(p.own_groups, 256 * p.own_mt) && launchable(p.pre_groups, 256 * p.pre_mt);
+    return attention && absorb_fits(c, h, s.n_rows) && finish_fits(h, s.n_rows);
 }
 
 int64_t absorbed_workspace(const Cache& c, const Step& s, const Heads& h) { return plan(c, s, h).bytes; }

@@ -625,9 +625,8 @@ int64_t expanded_workspace(const Cache& c, const Step& s, const Heads& h) { retu
 
 bool expanded_fits(const Cache& c, const Step& s, const Heads& h) {
     const Plan p = plan(c, s, h);
-    for (int64_t n : {p.own_groups + p.pre_groups, p.own_expand + p.pre_expand, p.merges})
-        if (n > kMostGroups) return false;
-    return true;
+    return launchable(p.own_groups + p.pre_groups, 256) && launchable(p.own_expand + p.pre_expand, 128 * expand_waves(h.nope, h.v)) &&
+           launchable(p.merges, 256);
 }
 
 void launch_expanded(hipStream_t st, const Cache& c, const Step& s, const Heads& h, const Attend& a) {

@@ -110,6 +110,16 @@ bool expands(const Cache& c, const Step& s, const Heads& h, int form) {
 }
 
 bool fits(const Cache& c, const Step& s, const Heads& h, bool expanded) { return expanded ? expanded_fits(c, s, h) : absorbed_fits(c, s, h); }
+
+// The form of a step: what was asked for, else what should be faster, or the other one where that has more workgroups than a launch can.
+moe_status choose(const Cache& c, const Step& s, const Heads& h, int form, bool* expanded) {
+    *expanded = expands(c, s, h, form);
+    if (fits(c, s, h, *expanded)) return MOE_OK;
+    *expanded = !*expanded;
+    if (form == MOE_LATENT_AUTO && fits(c, s, h, *expanded)) return MOE_OK;
+    return fail(MOE_ERR_SHAPE, "too many workgroups: bring fewer sequences or tokens at once");
+}
+
 int64_t workspace_of(const Cache& c, const Step& s, const Heads& h, bool expanded) { return expanded ? expanded_workspace(c, s, h) : absorbed_workspace(c, s, h); }
 
 moe_status launched() {
@@ -165,8 +175,8 @@ moe_status moe_latent_attend_workspace_bytes(const moe_latent_cache* cache, cons
     const Cache c = cache_of(cache);
     const Step s = step_of(step);
     const Heads h = heads_of(cache, heads);
-    const bool expanded = expands(c, s, h, form);
-    if (!fits(c, s, h, expanded)) return fail(MOE_ERR_SHAPE, "too many workgroups: bring fewer sequences or tokens at once");
+    bool expanded;
+    TRY(choose(c, s, h, form, &expanded));
     *bytes_out = workspace_of(c, s, h, expanded);
     return MOE_OK;
 }
@@ -193,8 +203,8 @@ moe_status moe_latent_attend(void* stream, const moe_latent_cache* cache, const 
     TRY(check_rows(out, "out", out_row_stride, out_head_stride, &w));
     if (pieces_overlap(s.n_rows, h.n, out_row_stride, out_head_stride, h.v)) return fail(MOE_ERR_INVALID_ARG, "rows or heads of out overlap");
     if (q == out) return fail(MOE_ERR_INVALID_ARG, "out must not be q");
-    const bool expanded = expands(c, s, h, form);
-    if (!fits(c, s, h, expanded)) return fail(MOE_ERR_SHAPE, "too many workgroups: bring fewer sequences or tokens at once");
+    bool expanded;
+    TRY(choose(c, s, h, form, &expanded));
     const int64_t need = workspace_of(c, s, h, expanded);
     if (workspace_bytes < need) return fail(MOE_ERR_OOM, "workspace of %lld bytes, need %lld", (long long)workspace_bytes, (long long)need);
     TRY(w.on(workspace, "workspace", 256));

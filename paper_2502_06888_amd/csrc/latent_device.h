@@ -42,9 +42,9 @@ struct Parts {
 
 // Whether finish_kernel has all wavefronts of a workgroup share a row's parts.
 bool finish_few(const Heads& h, int n_rows);
-int64_t absorb_groups(const Cache& c, const Heads& h, int n_rows);
+bool absorb_fits(const Cache& c, const Heads& h, int n_rows);
 void launch_absorb(hipStream_t st, const Cache& c, const Heads& h, const Rows& q, int n_rows, uint16_t* out);
-int64_t finish_groups(const Heads& h, int n_rows);
+bool finish_fits(const Heads& h, int n_rows);
 void launch_finish(hipStream_t st, const Cache& c, const Step& s, const Heads& h, const RowsOut& out, const Parts& parts);
 
 }  // namespace klat

@@ -45,11 +45,12 @@ struct Attend {
     uint8_t* ws;
 };
 
-using kkv8::kMostGroups;
+// Whether a launch of `groups` workgroups of `threads` each counts its threads in 32 bits.
+constexpr bool launchable(int64_t groups, int threads) { return groups * threads < (int64_t)1 << 32; }
 
 void launch_append(hipStream_t st, const Cache& c, const Step& s, const Append& a);
 
-// The two forms: whether their launches stay within kMostGroups, what they need.
+// The two forms: whether all their launches are launchable, what they need.
 bool absorbed_fits(const Cache& c, const Step& s, const Heads& h);
 int64_t absorbed_workspace(const Cache& c, const Step& s, const Heads& h);
 void launch_absorbed(hipStream_t st, const Cache& c, const Step& s, const Heads& h, const Attend& a);
