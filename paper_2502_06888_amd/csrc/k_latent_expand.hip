@@ -31,6 +31,9 @@ __device__ __forceinline__ int shift_of(uint32_t largest) {
     return largest == 0 || (e >= -6 && e < 15) ? 0 : e - 8;
 }
 
+// Stands for the exponent of values that are all zero: they set no scale.
+constexpr int kNoValues = 1 << 20;
+
 // Keys and values of heads head0 .. head0 + heads - 1 of the sequences, or of the prefix.
 struct Made {
     int head0, heads, tiles;  // tiles of a sequence at most
@@ -219,7 +222,7 @@ __global__ __launch_bounds__(128 * expand_waves(NOPE, DV), expand_occupancy(DC, 
         const bool there = j0 + half * 64 < total;
         u32x4* to = m.kv + tile * TILE;
         const int down[2] = {plain ? 0 : shift_of(largest[0][half]), plain ? 0 : shift_of(largest[1][half])};
-        if (there && wave == 0 && lane == 0) m.shift[tile] = make_int2(down[0], down[1]);
+        if (there && wave == 0 && lane == 0) m.shift[tile] = make_int2(down[0], !plain && largest[1][half] == 0 ? kNoValues : down[1]);
         const float fk = power(-down[0]), fv = power(-down[1]);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -326,7 +329,8 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
     float ref = kEmpty, sum = 0.f;
-    int scale = down.y;  // exponent of the sums: the largest of the values' so far
+    int scale = 0;     // exponent of the row's sums: that of the values they were last made of
+    bool odd = false;  // whether any tile so far had one (the same for the wavefront)
     const int within = min(limit, end) - 4 * grp;
     int buf = 0;
     for (int j0 = first; j0 < end; j0 += kSlots, buf ^= 1) {
@@ -383,16 +387,7 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[b][i] *= f;
         }
-        if (now_down.y > scale) {
-            const float f = power(scale - now_down.y);
-            scale = now_down.y;
-#pragma unroll
-            for (int b = 0; b < VB; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[b][i] *= f;
-        }
-        const float lift = kLift + (float)(now_down.y - scale);  // weights carry what the values' exponent lacks
-        exponents(ref, -lift, by, [&](auto&& of) {
+        exponents(ref, -kLift, by, [&](auto&& of) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -411,7 +406,38 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[u][i] = pack_f16(p[2 * i], p[2 * i + 1]);
         }
-        sum = __builtin_fmaf(part, power(scale - now_down.y), sum);
+        sum += part;
+        // Sums go over to the exponent of the tile's values, up or down and exactly, where one of the tile's weights is not 0 in fp16, so that
+        // the weights keep their bits, and values that hardly count, or that the row does not see, change nothing for it.  Below sums that
+        // would leave 32 bits (2^64 times the tile's and more) the tile counts as 0.
+        const int tile_scale = __builtin_amdgcn_readfirstlane(now_down.y);
+        if (odd || tile_scale != 0) {
+            odd = true;
+            uint32_t any = 0, largest = 0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) any |= w[u][i];
+            any |= (uint32_t)__shfl_xor((int)any, 32, 64);
+            const bool moves = any != 0 && scale != tile_scale && tile_scale != kNoValues;
+            if (__any(moves)) {
+#pragma unroll
+                for (int b = 0; b < VB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) largest = max(largest, __float_as_uint(acc[b][i]) & 0x7fffffffu);
+                largest = max(largest, (uint32_t)__shfl_xor((int)largest, 32, 64));
+                const int to = !moves ? scale : largest == 0 ? tile_scale : max(tile_scale, scale + exponent(largest) - 100);
+#pragma unroll
+                for (int b = 0; b < VB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[b][i] = __builtin_amdgcn_ldexpf(acc[b][i], scale - to);
+                scale = to;
+                if (moves && to != tile_scale) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) w[u] = u32x4{0u, 0u, 0u, 0u};
+                }
+            }
+        }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
