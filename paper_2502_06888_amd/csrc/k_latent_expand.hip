@@ -447,12 +447,14 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
     const float up = power(scale);
     if (parts.all > 1) {
         if (r < rows) {
+            // a range's mean, not its sum: no larger than its values are
+            const float mean = sum == 0.f ? 0.f : 1.f / sum;
             const int64_t at = ((int64_t)(q.row0 + r) * h.n + m.head0 + head) * parts.all + m.part0 + range;
 #pragma unroll
             for (int b = 0; b < VB; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    *(f32x4*)(parts.acc + at * DV + b * 32 + row_of(4 * i, grp)) = f32x4{acc[b][4 * i] * up, acc[b][4 * i + 1] * up, acc[b][4 * i + 2] * up, acc[b][4 * i + 3] * up};
+                    *(f32x4*)(parts.acc + at * DV + b * 32 + row_of(4 * i, grp)) = f32x4{acc[b][4 * i] * mean * up, acc[b][4 * i + 1] * mean * up, acc[b][4 * i + 2] * mean * up, acc[b][4 * i + 3] * mean * up};
             if (grp == 0) parts.ml[at] = make_float2(ref, sum);
         }
         return;
@@ -480,7 +482,7 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
     }
 }
 
-// Rows whose slots were cut into parts: brought to the largest reference, added, divided.  One wavefront per row and 64 / (DV / 4) heads.
+// Rows whose slots were cut into parts: the parts' means with their shares of the weights, brought to the largest reference.  One wavefront per row and 64 / (DV / 4) heads.
 template <int DV>
 __global__ __launch_bounds__(256) void merge_kernel(Cache c, Step s, Heads h, RowsOut out, Parts parts) {
     constexpr int LANES = DV / 4, HEADS = 64 / LANES;
@@ -499,18 +501,21 @@ __global__ __launch_bounds__(256) void merge_kernel(Cache c, Step s, Heads h, Ro
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
     for (int k = 0; k < n; ++k) ref = fmaxf(ref, parts.ml[at + (k < own ? k : parts.own + k - own)].x);
     for (int k = 0; k < n; ++k) {
+        const float2 ml = parts.ml[at + (k < own ? k : parts.own + k - own)];
+        sum = __builtin_fmaf(ml.y, __builtin_amdgcn_exp2f(ml.x - ref), sum);
+    }
+    const float inv = 1.f / sum;
+    for (int k = 0; k < n; ++k) {
         const int64_t i = at + (k < own ? k : parts.own + k - own);
         const float2 ml = parts.ml[i];
-        const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-        sum = __builtin_fmaf(ml.y, f, sum);
+        const float f = ml.y * __builtin_amdgcn_exp2f(ml.x - ref) * inv;
         const f32x4 y = *(const f32x4*)(parts.acc + i * DV + lane % LANES * 4);
 #pragma unroll
         for (int j = 0; j < 4; ++j) x[j] = __builtin_fmaf(y[j], f, x[j]);
     }
-    const float inv = 1.f / sum;
     u32x2 w;
-    w.x = pack_bf16(x[0] * inv, x[1] * inv);
-    w.y = pack_bf16(x[2] * inv, x[3] * inv);
+    w.x = pack_bf16(x[0], x[1]);
+    w.y = pack_bf16(x[2], x[3]);
     *(u32x2*)(out.p + (int64_t)row * out.row + (int64_t)head * out.head + lane % LANES * 4) = w;
 }
 

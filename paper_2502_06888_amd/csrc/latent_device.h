@@ -36,7 +36,7 @@ __device__ __forceinline__ int twist(int slot) {
 struct Parts {
     int per, pre_per;  // slots of a range: of a sequence, of the prefix
     int own, all;      // parts of a row at most: of its sequence, with the prefix's
-    float* acc;        // [row, head, part, element] sums of weight * latent, or * value
+    float* acc;        // [row, head, part, element] sums of weight * latent, or means of the values
     float2* ml;        // [row, head, part] reference, sum of weights
 };
 

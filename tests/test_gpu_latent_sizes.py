@@ -51,3 +51,16 @@ def test_tiles_that_hardly_count_set_no_scale(sizes, low, form):
     x.q[..., :32] /= max(sizes)
     x.q[..., 32:] = 1.25
     check(on_device(x).run(form), form, x.reference())
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("size", [1e34, 1e-24])
+def test_sums_in_ranges_of_values_of_any_size(size, form):
+    """Positive values under nearly equal scores: the sum of a range is far larger than its mean."""
+    x = Layer(203, [5000, 17], [1, 2], 4, DIMS, prefix=3001, max_len=5100)
+    for rows in (x.rows, x.prefix):
+        rows[..., :128] = rows[..., :128].abs() * size
+    x.w_v = x.w_v.abs()
+    x.h = L.LatentHeads(x.w_k.to(DEV), x.w_v.to(DEV))
+    x.q[..., :32] /= size
+    check(on_device(x).run(form), form, x.reference())
