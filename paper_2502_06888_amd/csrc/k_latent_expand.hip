@@ -25,10 +25,11 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { return __buil
 __device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(clampi(e, -126, 127) + 127) << 23); }
 // Exponent of a magnitude given by its bits, 0 for zero and what is not finite.
 __device__ __forceinline__ int exponent(uint32_t bits) { return bits == 0 || bits >= 0x7f800000u ? 0 : max((int)(bits >> 23), 1) - 127; }
-// Exponent by which a tile is brought into the range of fp16.
+// Exponent by which a tile, or the first part of a query, is brought into the range of fp16; 0 from 2^LEAST to 2^15.
+template <int LEAST>
 __device__ __forceinline__ int shift_of(uint32_t largest) {
     const int e = exponent(largest);
-    return largest == 0 || (e >= -6 && e < 15) ? 0 : e - 8;
+    return largest == 0 || (e >= LEAST && e < 15) ? 0 : e - 8;
 }
 
 // Stands for the exponent of values that are all zero: they set no scale.
@@ -221,7 +222,7 @@ __global__ __launch_bounds__(128 * expand_waves(NOPE, DV), expand_occupancy(DC, 
         const int64_t tile = ((int64_t)seq * m.heads + head) * m.tiles + pair * 2 + half;
         const bool there = j0 + half * 64 < total;
         u32x4* to = m.kv + tile * TILE;
-        const int down[2] = {plain ? 0 : shift_of(largest[0][half]), plain ? 0 : shift_of(largest[1][half])};
+        const int down[2] = {plain ? 0 : shift_of<-6>(largest[0][half]), plain ? 0 : shift_of<-6>(largest[1][half])};
         if (there && wave == 0 && lane == 0) m.shift[tile] = make_int2(down[0], !plain && largest[1][half] == 0 ? kNoValues : down[1]);
         const float fk = power(-down[0]), fv = power(-down[1]);
 #pragma unroll
@@ -294,7 +295,7 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
     int2 down = shift[first / kSlots];
 
     u32x4 qf[KF], qp[PF];
-    float factor;
+    int query_scale;  // exponent taken off the row's first part
     {
         const uint16_t* p = a.q.p + (int64_t)(q.row0 + mine) * a.q.row + (int64_t)(m.head0 + head) * a.q.head + grp * 8;
         uint32_t top = 0;
@@ -307,17 +308,12 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
 #pragma unroll
         for (int f = 0; f < PF; ++f) qp[f] = *(const u32x4*)(p + NOPE + f * 16);
         top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
-        const int e = exponent(top);
-        const float by = power(-e);
-        factor = fminf(a.qscale * power(e), 3.40282347e38f);
+        query_scale = shift_of<-2>(top);
 #pragma unroll
         for (int f = 0; f < KF; ++f)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) qf[f][i] = pack_f16(bf_lo(qf[f][i]) * by, bf_hi(qf[f][i]) * by);
-#pragma unroll
-        for (int f = 0; f < PF; ++f)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) qp[f][i] = pack_bf16(bf_lo(qp[f][i]) * by, bf_hi(qp[f][i]) * by);
+            for (int i = 0; i < 4; ++i)
+                qf[f][i] = pack_f16(__builtin_amdgcn_ldexpf(bf_lo(qf[f][i]), -query_scale), __builtin_amdgcn_ldexpf(bf_hi(qf[f][i]), -query_scale));
 #pragma unroll
         for (int f = 0; f < KF; ++f) asm volatile("" : "+v"(qf[f]));  // waited for here, not in the loop
 #pragma unroll
@@ -328,6 +324,7 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
     for (int b = 0; b < VB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
+    const bool queries_scaled = __any(query_scale != 0);
     float ref = kEmpty, sum = 0.f;
     int scale = 0;     // exponent of the row's sums: that of the values they were last made of
     bool odd = false;  // whether any tile so far had one (the same for the wavefront)
@@ -348,21 +345,20 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
 #pragma unroll
             for (int i = 0; i < 16; ++i) z[t][i] = 0.f;
 #pragma unroll
-            for (int f = 0; f < PF; ++f) z[t] = mfma32(lds[buf][Z::kTile + (t * PF + f) * 64 + lane], qp[f], z[t]);
+            for (int f = 0; f < KF; ++f) z[t] = mfma32h(lds[buf][(t * KF + f) * 64 + lane], qf[f], z[t]);
         }
-        float by = factor;
-        if (now_down.x != 0) {
-            const float f = power(-now_down.x);
-            by = fminf(factor * power(now_down.x), 3.40282347e38f);
+        // What was taken off queries and keys comes back, before the part that carries the position is added as it is.
+        const int key_scale = __builtin_amdgcn_readfirstlane(now_down.x);
+        if (queries_scaled || key_scale != 0) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) z[t][i] *= f;
+                for (int i = 0; i < 16; ++i) z[t][i] = __builtin_amdgcn_ldexpf(z[t][i], query_scale + key_scale);
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int f = 0; f < KF; ++f) z[t] = mfma32h(lds[buf][(t * KF + f) * 64 + lane], qf[f], z[t]);
+            for (int f = 0; f < PF; ++f) z[t] = mfma32(lds[buf][Z::kTile + (t * PF + f) * 64 + lane], qp[f], z[t]);
         if (j0 + kSlots > wave_least || j0 + kSlots > end) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -375,7 +371,7 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, z[t][i]);
-        top *= by;
+        top *= a.qscale;
         if (__any(top > ref + kRise)) {
             top = fmaxf(top, __shfl_xor(top, 32, 64));
             const float now = top > ref + kRise ? ceilf(top) : ref;
@@ -387,7 +383,7 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[b][i] *= f;
         }
-        exponents(ref, -kLift, by, [&](auto&& of) {
+        exponents(ref, -kLift, a.qscale, [&](auto&& of) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll

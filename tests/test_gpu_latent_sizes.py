@@ -64,3 +64,29 @@ def test_sums_in_ranges_of_values_of_any_size(size, form):
     x.h = L.LatentHeads(x.w_k.to(DEV), x.w_v.to(DEV))
     x.q[..., :32] /= size
     check(on_device(x).run(form), form, x.reference())
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("q,latents", [(1e-20, 1e-20), (1e-25, 1e-25), (1e-14, 1e-25), (1e25, 1e-25), (1e-25, 1e25), (3e-38, 1.0), (1e-38, 1e30)])
+def test_queries_and_latents_of_any_size(q, latents, form):
+    """Small or large together, beside a part with the position that is neither, in tiles of which rows see a part."""
+    x = Layer(204, [10, 90, 0], [60, 3, 70], 4, DIMS)
+    x.rows[..., :128] *= latents
+    x.q[..., :32] *= q
+    check(on_device(x).run(form), form, x.reference())
+
+
+@pytest.mark.parametrize("form", [EXPANDED])
+@pytest.mark.parametrize("q,latents", [(1.0, 1e-30), (1e-10, 1e-30)])
+def test_latents_whose_shares_are_below_the_absorbed_forms_range(q, latents, form):
+    x = Layer(205, [10, 90, 0], [60, 3, 70], 4, DIMS)
+    x.rows[..., :128] *= latents
+    x.q[..., :32] *= q
+    check(on_device(x).run(form), form, x.reference())
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("sizes", [(1e20, 1e-20, 1e-20), (1e-20, 1e20, 1e-20), (1e18, 0.0, 1e-18)])
+def test_tiles_beyond_what_sums_can_hold_beside_each_other(sizes, form):
+    """Under queries as small as the smallest keys, sums of a large tile with those of one less than 2^-100 of it."""
+    test_tiles_of_no_values_and_of_sizes_far_apart(sizes, form)
