@@ -22,14 +22,15 @@ __device__ __forceinline__ f32x16 mfma32h(const u32x4 a, const u32x4 b, const f3
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), f16x2)); }
-__device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(clampi(e, -126, 127) + 127) << 23); }
+__device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 .. 127
 // Exponent of a magnitude given by its bits, 0 for zero and what is not finite.
 __device__ __forceinline__ int exponent(uint32_t bits) { return bits == 0 || bits >= 0x7f800000u ? 0 : max((int)(bits >> 23), 1) - 127; }
 // Exponent by which a tile, or the first part of a query, is brought into the range of fp16; 0 from 2^LEAST to 2^15.
+// Not below -120, so that both it and its negative are exponents of numbers of 32 bits: the smallest normal ones are 2^-6 then.
 template <int LEAST>
 __device__ __forceinline__ int shift_of(uint32_t largest) {
     const int e = exponent(largest);
-    return largest == 0 || (e >= LEAST && e < 15) ? 0 : e - 8;
+    return largest == 0 || (e >= LEAST && e < 15) ? 0 : max(e - 8, -120);
 }
 
 // Stands for the exponent of values that are all zero: they set no scale.
@@ -456,7 +457,7 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
         return;
     }
     // The rows go through the buffers, which are done with, so that each leaves in one piece; 16-byte pieces lie at an xor of the row.
-    const float inv = up / sum;
+    const float inv = 1.f / sum;
     constexpr int PPR = DV / 8;  // pieces of a row
     __syncthreads();
     u32x4* out = &lds[0][0] + wave * 32 * PPR;
@@ -466,8 +467,8 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             u32x2 x;
-            x.x = pack_bf16(acc[b][4 * i] * inv, acc[b][4 * i + 1] * inv);
-            x.y = pack_bf16(acc[b][4 * i + 2] * inv, acc[b][4 * i + 3] * inv);
+            x.x = pack_bf16(acc[b][4 * i] * inv * up, acc[b][4 * i + 1] * inv * up);
+            x.y = pack_bf16(acc[b][4 * i + 2] * inv * up, acc[b][4 * i + 3] * inv * up);
             ((u32x2*)(out + col * PPR + ((b * 4 + i) ^ (col % PPR))))[grp] = x;
         }
 #pragma unroll

@@ -90,3 +90,16 @@ def test_latents_whose_shares_are_below_the_absorbed_forms_range(q, latents, for
 def test_tiles_beyond_what_sums_can_hold_beside_each_other(sizes, form):
     """Under queries as small as the smallest keys, sums of a large tile with those of one less than 2^-100 of it."""
     test_tiles_of_no_values_and_of_sizes_far_apart(sizes, form)
+
+
+@pytest.mark.parametrize("cached,prefix", [([100, 700], 200), ([30, 5], 0)])
+def test_the_smallest_values(cached, prefix):
+    """Values of 2^-120 to 2^-119, each one latent, so that no product on the way is smaller."""
+    x = Layer(206, cached, [40, 2], 4, DIMS, prefix=prefix)
+    one = torch.eye(32, 128, dtype=torch.bfloat16)
+    x.w_k = x.w_v = one.expand(4, 32, 128).contiguous()
+    x.h = L.LatentHeads(x.w_k.to(DEV), x.w_v.to(DEV))
+    g = torch.Generator().manual_seed(7)
+    for rows in [x.rows] if prefix == 0 else [x.rows, x.prefix]:
+        rows[..., :128] = (1 + torch.randint(0, 128, rows[..., :128].shape, generator=g) / 128).to(torch.bfloat16) * 2.0 ** -120
+    check(on_device(x).run(EXPANDED), EXPANDED, x.reference())
