@@ -269,7 +269,7 @@ const uint32_t from = cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, to = c
             sum *= __builtin_amdgcn_exp2f(ref - now);
             ref = now;
         }
-        exponents(ref, kAbove, run.qscale, [&](auto&& of) {
+        exponents_of_rows(ref, kAbove, run.qscale, [&](auto&& of) {
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
 #pragma unroll

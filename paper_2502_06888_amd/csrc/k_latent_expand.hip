@@ -384,7 +384,7 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[b][i] *= f;
         }
-        exponents(ref, -kLift, a.qscale, [&](auto&& of) {
+        exponents_of_rows(ref, -kLift, a.qscale, [&](auto&& of) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll

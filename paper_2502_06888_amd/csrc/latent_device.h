@@ -32,6 +32,22 @@ __device__ __forceinline__ int twist(int slot) {
     return (slot >> 1 & 1) << 2 | ((q ^ q >> 1) & 1) << 1 | q >> 1;
 }
 
+// Scores to exponents of the weights (attn_device.h), each lane's by its own reference: over a prefix rows of several sequences share a
+// wavefront, and one with huge scores, or with none, must not change how the others' are rounded.
+template <class T>
+__device__ __forceinline__ void exponents_of_rows(float reference, float above, float factor, T&& each) {
+    const float less = reference + above;
+    const bool far = fabsf(reference) > kFar;
+    if (!__any(far)) {
+        each([&](float score) { return __builtin_fmaf(score, factor, -less); });
+    } else {
+        each([&](float score) {
+            const float near = __builtin_fmaf(score, factor, -less);
+            return far ? apart(score, factor, reference) - above : near;
+        });
+    }
+}
+
 // Sums, cut into parts: a row's slots into ranges of `per`, the prefix into ranges of its own, behind them.
 struct Parts {
     int per, pre_per;  // slots of a range: of a sequence, of the prefix
