@@ -496,10 +496,12 @@ __global__ __launch_bounds__(256) void merge_kernel(Cache c, Step s, Heads h, Ro
     const int64_t at = ((int64_t)row * h.n + head) * parts.all;
     float ref = kEmpty, sum = 0.f;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < n; ++k) ref = fmaxf(ref, parts.ml[at + (k < own ? k : parts.own + k - own)].x);
+#pragma unroll 4
     for (int k = 0; k < n; ++k) {
         const float2 ml = parts.ml[at + (k < own ? k : parts.own + k - own)];
-        sum = __builtin_fmaf(ml.y, __builtin_amdgcn_exp2f(ml.x - ref), sum);
+        const float now = fmaxf(ref, ml.x);
+        sum = __builtin_fmaf(ml.y, __builtin_amdgcn_exp2f(ml.x - now), sum * __builtin_amdgcn_exp2f(ref - now));
+        ref = now;
     }
     const float inv = 1.f / sum;
     for (int k = 0; k < n; ++k) {
