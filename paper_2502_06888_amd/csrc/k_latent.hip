@@ -36,9 +36,21 @@ __global__ __launch_bounds__(256) void append_kernel(Cache c, Step s, Append a) 
         for (int i = 0; i < 4; ++i) sum += bf_lo(v[i]) * bf_lo(v[i]) + bf_hi(v[i]) * bf_hi(v[i]);
 #pragma unroll
         for (int m = 32; m > 0; m /= 2) sum += __shfl_xor(sum, m, 64);
-        const float inv = 1.f / sqrtf(sum / (float)c.latent + a.eps);
+        const float square = sum / (float)c.latent + a.eps;
+        if (square >= 0x1p-80f && sum <= 3.40282347e38f) {
+            const float inv = 1.f / sqrtf(square);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = pack_bf16(bf_lo(v[i]) * inv * bf_lo(g[i]), bf_hi(v[i]) * inv * bf_hi(g[i]));
+            for (int i = 0; i < 4; ++i) v[i] = pack_bf16(bf_lo(v[i]) * inv * bf_lo(g[i]), bf_hi(v[i]) * inv * bf_hi(g[i]));
+        } else {  // squares beyond the range of 32 bits, or below it, from which eps does not keep them
+            double all = 0.;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) all += (double)bf_lo(v[i]) * bf_lo(v[i]) + (double)bf_hi(v[i]) * bf_hi(v[i]);
+#pragma unroll
+            for (int m = 32; m > 0; m /= 2) all += __shfl_xor(all, m, 64);
+            const double inv = 1. / sqrt(all / c.latent + a.eps);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = pack_bf16((float)(bf_lo(v[i]) * inv * bf_lo(g[i])), (float)(bf_hi(v[i]) * inv * bf_hi(g[i])));
+        }
     }
     if (mine) *(u32x4*)(to + lane * 8) = v;
     if (turns) {
