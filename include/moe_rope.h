@@ -27,7 +27,8 @@ extern "C" {
  *   original_len L > 0: by parts, r_i = L * w_i / (2 pi) being the turns over the original length,
  *     g_i = (r_i - low_turns) / (high_turns - low_turns) cut to 0..1, and w_i * (g_i + (1 - g_i) / factor): pairs that turn often keep
  *     their frequency, those that turn less than low_turns are squeezed (arXiv 2309.00071).
- * Angles are formed in 64 bits and reduced there; sine and cosine are exact to about a step of 32 bits at any position.
+ * Angles are formed and reduced in 64 bits and more; sine and cosine are exact to about a step of 32 bits as long as |position| * w_i is at
+ * most 2^31, which theta and factor of 1 and more see to at any position.
  */
 typedef struct {
     int32_t rot_dim;      /* elements of a head that turn: even, 2..256 */

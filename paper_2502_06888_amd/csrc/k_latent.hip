@@ -55,7 +55,7 @@ __global__ __launch_bounds__(256) void append_kernel(Cache c, Step s, Append a) 
     if (mine) *(u32x4*)(to + lane * 8) = v;
     if (turns) {
         const int position = (s.next_position != nullptr ? s.next_position[seq] : c.prefix_len + q.cached) + token;
-        const float2 cs = krope::turn(a.turns.per_position[pair], position);
+        const float2 cs = krope::turn(a.turns, pair, position);
         const float cosine = cs.x * a.turns.magnitude, sine = cs.y * a.turns.magnitude;
         e = pack_bf16(krope::turned(bf_lo(e), bf_lo(partner), cosine, second ? sine : -sine), 0.f);
     }

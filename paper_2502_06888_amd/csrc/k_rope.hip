@@ -32,7 +32,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(Rotate r, int rows_each) {
     extern __shared__ float2 table[];  // [row of the workgroup][pair]
     const int pairs = r.rot / 2, row0 = blockIdx.x * rows_each, rows = min(rows_each, r.n_rows - row0);
     for (int i = threadIdx.x; i < rows * pairs; i += 256) {
-        const float2 cs = turn(r.turns.per_position[i % pairs], r.positions[row0 + i / pairs]);
+        const float2 cs = turn(r.turns, i % pairs, r.positions[row0 + i / pairs]);
         table[i] = make_float2(cs.x * r.turns.magnitude, cs.y * r.turns.magnitude);
     }
     __syncthreads();

@@ -12,9 +12,11 @@ namespace krope {
 
 constexpr int kMostPairs = 128;
 
-// Turns per position of each pair, w_i / (2 pi).  Passed by value: 1 KiB of kernel arguments, nothing to own or to free.
+// Turns per position of each pair, w_i / (2 pi): 53 bits and the next 11, without which positions near 2^31 would be 2^-22 of a quarter turn off.
+// Passed by value: 1.5 KiB of kernel arguments, nothing to own or to free.
 struct Turns {
     double per_position[kMostPairs];
+    float rest[kMostPairs];
     float magnitude;
 };
 
@@ -32,7 +34,9 @@ inline Turns turns_of(const moe_rope_config& c) {
             keep = (c.original_len * w / two_pi - c.low_turns) / ((long double)c.high_turns - c.low_turns);
             keep = keep < 0.0L ? 0.0L : keep > 1.0L ? 1.0L : keep;
         }
-        t.per_position[i] = (double)(w * (keep + (1.0L - keep) / c.factor) / two_pi);
+        const long double turns = w * (keep + (1.0L - keep) / c.factor) / two_pi;
+        t.per_position[i] = (double)turns;
+        t.rest[i] = (float)(turns - (long double)t.per_position[i]);
     }
     return t;
 }
@@ -51,11 +55,13 @@ inline moe_status check_config(const moe_rope_config* c, kcall::CallError& e) {
     return MOE_OK;
 }
 
-// Cosine and sine of `position` times `per_position` turns.  The turns are reduced to quarters in 64 bits, so that the
-// 32-bit rest is at most half a quarter: an angle is off by less than 2^-25 of a quarter turn, whatever the position.
-__device__ __forceinline__ float2 turn(double per_position, int position) {
-    const double t = (double)position * per_position;
-    const double quarters = (t - rint(t)) * 4.0, whole = rint(quarters);
+// Cosine and sine of `position` times a pair's turns.  Whole turns are taken off the exact product, the turns' last bits are added, and the rest is
+// reduced to quarters, so that in 32 bits it is at most half of one: an angle is off by less than 2^-25 of a quarter turn at any position
+// where w_i is at most 1 (of less than 2^31 radians where it is not).
+__device__ __forceinline__ float2 turn(const Turns& turns, int pair, int position) {
+    const double at = (double)position, per = turns.per_position[pair];
+    const double part = __builtin_fma(at, (double)turns.rest[pair], __builtin_fma(at, per, -rint(at * per)));
+    const double quarters = part * 4.0, whole = rint(quarters);
     float s, c;
     sincospif((float)(quarters - whole) * 0.5f, &s, &c);
     const int q = (int)whole & 3;
