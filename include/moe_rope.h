@@ -54,6 +54,7 @@ typedef struct {
 /*
  * moe_rope_rotate -- turns the rows of q and, unless null, of k by their positions, in one launch.
  *   dtype: moe_dtype of all rows; head_dim: 2..1024; n_rows: 0..2^24.
+ *   out of the one shares no element with in or out of the other.
  *   positions: int32 [n_rows], of any sign.  Negative ones turn back: the transposed rotation, which is also the gradient's, is that
  *     of the negated positions.
  * Products are formed in 32 bits and rounded once.  Rows and parts whose addresses and strides are multiples of 16 bytes move 16 bytes at

@@ -43,6 +43,8 @@ moe_status moe_rope_rotate(void* stream, const moe_rope_config* cfg, int32_t dty
     if (!q) return fail(MOE_ERR_INVALID_ARG, "q is null");
     const unsigned size = dtype == MOE_F32 ? 4 : 2;
     Where w{&g_error};
+    if (k && k->n_heads > 0 && q->n_heads > 0 && n_rows > 0 && (q->out == k->out || q->out == k->in || k->out == q->in))
+        return fail(MOE_ERR_INVALID_ARG, "q and k are written to the same memory, or one over the other's input");
     TRY(check_rows(q, "q", n_rows, head_dim, size, &w));
     if (k) TRY(check_rows(k, "k", n_rows, head_dim, size, &w));
     if (n_rows == 0 || (q->n_heads == 0 && (!k || k->n_heads == 0))) return MOE_OK;
