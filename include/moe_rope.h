@@ -39,7 +39,7 @@ typedef struct {
     double factor;        /* > 0; 1: unscaled */
     double low_turns;     /* only with original_len > 0: 0 <= low_turns < high_turns */
     double high_turns;
-    double magnitude;     /* factor of what turns; 1: lengths stay */
+    double magnitude;     /* factor of what turns, finite in 32 bits; 1: lengths stay */
 } moe_rope_config;
 
 /* Rows of heads: element (row, head, i) at row * row_stride + head * head_stride + i. */

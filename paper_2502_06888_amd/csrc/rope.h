@@ -49,7 +49,7 @@ inline moe_status check_config(const moe_rope_config* c, kcall::CallError& e) {
     if (c->original_len < 0 || c->original_len > (1 << 30)) return e.fail(MOE_ERR_INVALID_ARG, "original_len outside 0..2^30");
     if (!(c->theta > 0) || std::isinf(c->theta)) return e.fail(MOE_ERR_INVALID_ARG, "theta must be finite and > 0");
     if (!(c->factor > 0) || std::isinf(c->factor)) return e.fail(MOE_ERR_INVALID_ARG, "factor must be finite and > 0");
-    if (!std::isfinite(c->magnitude)) return e.fail(MOE_ERR_INVALID_ARG, "magnitude must be finite");
+    if (!std::isfinite((float)c->magnitude)) return e.fail(MOE_ERR_INVALID_ARG, "magnitude must be finite in 32 bits");
     if (c->original_len > 0 && (!(c->low_turns >= 0) || !(c->high_turns > c->low_turns) || std::isinf(c->high_turns)))
         return e.fail(MOE_ERR_INVALID_ARG, "low_turns must be >= 0 and less than high_turns, both finite");
     return MOE_OK;

@@ -1,4 +1,4 @@
-"""Calls of the rotation that the host refuses: rows of q and k in the same memory."""
+"""Calls of the rotation that the host refuses: rows of q and k in the same memory, a magnitude that 32 bits do not hold."""
 import ctypes as C
 
 import pytest
@@ -27,3 +27,10 @@ def test_both_may_be_read_from_one_tensor():
     rows = [P.MoeRopeRows(t[0].data_ptr(), t[i].data_ptr(), 2, 0, 128, 64, 128, 64) for i in (1, 2)]
     assert lib.moe_rope_rotate(None, P.Rope(32).ref, B.MOE_BF16, 2, 64, None, C.byref(rows[0]), C.byref(rows[1])) == B.MOE_ERR_INVALID_ARG
     assert b"not device memory" in lib.moe_rope_last_error()
+
+
+@pytest.mark.parametrize("magnitude", [1e39, -1e300])
+def test_a_magnitude_beyond_32_bits_is_refused(magnitude):
+    lib, rows = P.load_library(), P.MoeRopeRows(16, 16, 1, 0, 64, 64, 64, 64)
+    assert lib.moe_rope_rotate(None, P.Rope(32, magnitude=magnitude).ref, B.MOE_BF16, 2, 64, None, C.byref(rows), None) == B.MOE_ERR_INVALID_ARG
+    assert b"magnitude" in lib.moe_rope_last_error()
