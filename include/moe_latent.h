@@ -75,9 +75,11 @@ typedef enum { MOE_LATENT_AUTO = 0, MOE_LATENT_ABSORBED = 1, MOE_LATENT_EXPANDED
  *     no two (row, head) of out share an element, and q and out share none.
  *   softmax_scale: 0 stands for 1 / sqrt(nope_dim + rope_dim).
  * Rows of no sequence are left as they were.  Scores, the softmax's statistics and sums are kept in 32 bits.  Rounded on
- * the way: in the absorbed form the softmax weights to bf16, a and u to two bf16 (16 bits together); in the expanded one the softmax
- * weights, keys, values and the queries' nope_dim elements to fp16 times a power of two, finite ones to finite ones.  A latent that is
- * not finite reaches the rows that see it, all their elements, and no others.
+ * the way: in the absorbed form the softmax weights to bf16, a and u to two bf16 (16 bits together; latents below 2^-80 have fewer); in the
+ * expanded one the softmax weights, keys, values and the queries' nope_dim elements to fp16 times a power of two, finite ones to finite
+ * ones.  The keys, and the values, of 64 slots of a sequence share that power for a head, a query's elements do, and a row's weights:
+ * each is off by 2^-11 of itself, or by 2^-19 of the largest of them where that is more.  A latent that is not finite reaches the rows that
+ * see it, all their elements, and no others.
  * The result of a sequence does not depend on what the others hold; how its sums are split follows from the numbers in the structs and
  * its own length.
  * workspace: moe_latent_attend_workspace_bytes() of device memory, 256-byte aligned; it depends on sizes and bounds only.

@@ -326,7 +326,8 @@ void launch_append(hipStream_t st, const Cache& c, const Step& s, const Append& 
     hipLaunchKernelGGL(append_kernel, dim3((unsigned)((s.n_rows + 3) / 4)), dim3(256), 0, st, c, s, a);
 }
 
-// Wavefronts of a workgroup, and tiles of 32 rows of each: about 2048 wavefronts, which are eight per compute unit.
+// Wavefronts of a workgroup, and tiles of 32 rows of each: about 2048 wavefronts, two for each SIMD.  With nope 128 (198 registers and 64 for the
+// products) a SIMD holds one at a time, otherwise both.
 static int absorb_waves(int n_rows) { return n_rows > 64 ? 4 : 1; }
 static int absorb_each(const Cache& c, const Heads& h, int n_rows) {
     const int64_t all = (int64_t)h.n * (c.latent / 128) * ((n_rows + 31) / 32);

@@ -3,9 +3,10 @@
 //
 // A row of C has 1152 bytes (512 + 64) and takes part in 2 * (2 * 512 + 64) operations per row of A: bound by the bytes of
 // the cache up to about 60 rows of A, by the matrix cores and the LDS that feeds them beyond.  Measured: 512 sequences of 513 slots, 32 heads,
-// 302 MB in 61 us; 48 of 80 to 6001 slots, 128 heads, 106 us; 16384 rows over 4000 slots 200 us: a workgroup of 64 rows takes 64 slots in 3.2
-// us, of which the products are 1.3 and the reads from LDS 1.4; the rest are the phases between barriers, since the registers are full and nothing is left to run
-// one step's scores under another's sums.
+// 302 MB in 61 us; 48 of 80 to 6001 slots, 128 heads, 105 us; 16384 rows over 4000 slots 200 us: a workgroup of 64 rows takes 64 slots in 3.2
+// us, of which the products are 1.3 and the reads from LDS 1.4; the rest are the phases between barriers, which all wavefronts go through together.
+// Each holds rows and sums both, so its registers are full and it cannot run one step's scores under another's sums; wavefronts that only
+// score beside others that only sum have not been tried.
 #include "latent_device.h"
 
 namespace klat {
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(256 * MT, 2) void absorbed_kernel(Cache c, Step s, 
 #pragma unroll
         for (int g = 0; g < T::kGroups; ++g) {
             const bool cut = T::kHalf && g == T::kGroups - 1;  // the row ends within the group
-const uint32_t from = cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, to = copy_at + buf * STEP + g * 4096;
+            const uint32_t from = cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, to = copy_at + buf * STEP + g * 4096;
             if constexpr (STREAM) stream_to_lds((const uint8_t*)C + g * 128, from, to);
             else copy_to_lds((const uint8_t*)C + g * 128, from, to);
         }
@@ -278,8 +279,10 @@ const uint32_t from = cut ? slot * (T::kWidth * 2) + (unit_at & 63) : at, to = c
         // weights: 64 bytes a row, its four units at an xor of the row
         const uint32_t put_at = weights_at + (uint32_t)(my_row * 64 + ((half * 2 + (l >> 5)) ^ (my_row >> 2 & 3)) * 16 + (l >> 4 & 1) * 8);
         u32x2 w[SUB];
+        // Rounded to bf16: the products take both factors in one type, and the latents are read as they lie in the cache.  The sum is that of the
+        // weights as rounded: then one slot that has nearly all of it counts nearly exactly.
 #pragma unroll
-        for (int u = 0; u < SUB; ++u) {  // the sum is that of the weights as rounded: then one slot that has nearly all of it counts nearly exactly
+        for (int u = 0; u < SUB; ++u) {
             w[u].x = pack_bf16(__builtin_amdgcn_exp2f(z[u][0]), __builtin_amdgcn_exp2f(z[u][1]));
             w[u].y = pack_bf16(__builtin_amdgcn_exp2f(z[u][2]), __builtin_amdgcn_exp2f(z[u][3]));
             sum += (bf_lo(w[u].x) + bf_hi(w[u].x)) + (bf_lo(w[u].y) + bf_hi(w[u].y));

@@ -5,7 +5,8 @@
 // Keys and values are kept as fp16, whose 11 bits leave the outputs as exact as their own rounding to bf16 does: over 3000 slots
 // keys and values rounded to bf16 put them 4.3e-3 from 64 bits, as fp16 1.7e-3.  fp16 reaches from 2^-14 to 65504; what is outside is brought in
 // by exact powers of two: one for each row of queries, one for the keys and one for the values of each head and tile of 64
-// slots, 0 wherever the tile's largest lies in 2^-6 .. 2^15.  The part that carries the position stays bf16, as it came.
+// slots, 1 wherever the largest lies in 2^-6 .. 2^15 (of queries 2^-2 .. 2^15).  What is far below the largest of its tile, or row, falls below
+// 2^-14 and so is off by 2^-25: by 2^-19 (2^-23) of the largest at most.  The part that carries the position stays bf16, as it came.
 #include "latent_device.h"
 
 namespace klat {
@@ -47,7 +48,7 @@ struct Made {
     int per, ranges, row_tiles, part0;
 };
 // One launch: the first `before` workgroups have the prefix, the others the sequences.  (One behind the other, the smaller launch leaves most
-// compute units alone: 5 prompts over a prefix of 8001 slots, 57 and 24 us of expand_kernel, 146 and 18 of expanded_kernel; in one 78 and 154.)
+// compute units alone: 5 prompts over a prefix of 8001 slots, 57 and 24 us of expand_kernel, 146 and 18 of expanded_kernel; in one 78 and 157.)
 struct Both {
     Made pre, own;
     int before;
@@ -254,7 +255,7 @@ __global__ __launch_bounds__(128 * expand_waves(NOPE, DV), expand_occupancy(DC, 
 
 // Attention of 128 rows (32 a wavefront) of one head: scores and sums transposed, so that a lane has one row, its softmax needs no
 // exchange but one between two lanes, and the weights are the second operand of the sums as they stand.  Tiles come in turn into two
-// buffers, without registers.  2 prompts of about 4000 tokens, 32 heads: 335 GFLOP in 356 us, 0.94 PFLOP/s, 76 % of what a large library product reaches;
+// buffers, without registers.  2 prompts of about 4000 tokens, 32 heads: 335 GFLOP in 359 us, 0.93 PFLOP/s, 75 % of what a large library product reaches;
 // matrix cores half busy, the clock at the card's power limit.
 template <int NOPE, int DV, int DR>
 __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads h, Attend a, Both both, Parts parts) {
@@ -450,8 +451,12 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
 #pragma unroll
             for (int b = 0; b < VB; ++b)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    *(f32x4*)(parts.acc + at * DV + b * 32 + row_of(4 * i, grp)) = f32x4{acc[b][4 * i] * mean * up, acc[b][4 * i + 1] * mean * up, acc[b][4 * i + 2] * mean * up, acc[b][4 * i + 3] * mean * up};
+                for (int i = 0; i < 4; ++i) {
+                    f32x4 y;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) y[j] = acc[b][4 * i + j] * mean * up;
+                    *(f32x4*)(parts.acc + at * DV + b * 32 + row_of(4 * i, grp)) = y;
+                }
             if (grp == 0) parts.ml[at] = make_float2(ref, sum);
         }
         return;
@@ -479,7 +484,8 @@ __global__ __launch_bounds__(256, 2) void expanded_kernel(Cache c, Step s, Heads
     }
 }
 
-// Rows whose slots were cut into parts: the parts' means with their shares of the weights, brought to the largest reference.  One wavefront per row and 64 / (DV / 4) heads.
+// Rows whose slots were cut into parts: the parts' means with their shares of the weights, brought to the largest reference.  One wavefront per
+// row and 64 / (DV / 4) heads.
 template <int DV>
 __global__ __launch_bounds__(256) void merge_kernel(Cache c, Step s, Heads h, RowsOut out, Parts parts) {
     constexpr int LANES = DV / 4, HEADS = 64 / LANES;
